@@ -295,6 +295,100 @@ int softmax_cross_entropy(const float *Z, int32_t ldz, const int32_t *labels,
                           int32_t classes, int32_t batch, float *dZ, int32_t lddz,
                           float *loss_out, void *stream);
 
+/* ---- clipped gradients -----------------------------------------------------------------
+ * The gradients of many layers (dvalues and dbias of sparse_linear_backward) as one list of n arrays, each of
+ * counts[t] >= 0 entries.  The lists themselves (pointers and counts) are HOST arrays, read before the call returns;
+ * what they point to is on the device, and may be null where counts[t] is 0.  With
+ *     norm = sqrt( sum over all arrays and entries of grad^2 )      (added up in 64 bits)
+ *     c    = min(1, max_norm / norm),                               max_norm > 0 (infinite: no clipping, only the norm)
+ * gradient_norm leaves the norm in *norm_out.
+ * gradient_clip writes clipped[t][k] = c * grads[t][k]; clipped[t] may be grads[t] itself.
+ * sgd_update_clipped makes the step of sgd_update_values (nesterov == 0) or sgd_update_values_nesterov with c * grad in the
+ * place of grad, on all arrays; an array that is in the list more than once is stepped as often, in the order of the list.
+ * Where the norm is infinite or NaN (a gradient is, or the norm lies beyond fp32) no factor makes a usable step: the last two
+ * then change nothing, and *norm_out tells.  norm_out: one device float (may be NULL but in gradient_norm).
+ * The result does not depend on the order in which work-groups run.  Written arrays must not overlap each other in part or
+ * other inputs.  After the caller's update of values[] of a layer, sparse_linear_sync_values applies as ever.
+ * workspace: device scratch, 8-byte aligned, of at least gradient_norm_workspace_bytes(n); it needs no clearing, and calls that share one
+ * must not overlap in time. */
+size_t gradient_norm_workspace_bytes(int32_t n);
+int gradient_norm(int32_t n, const float *const *grads, const int64_t *counts, void *workspace,
+                  size_t workspace_bytes, float *norm_out, void *stream);
+int gradient_clip(int32_t n, const float *const *grads, float *const *clipped, const int64_t *counts,
+                  float max_norm, void *workspace, size_t workspace_bytes, float *norm_out, void *stream);
+int sgd_update_clipped(int32_t n, float *const *values, float *const *velocities, const float *const *grads,
+                       const int64_t *counts, float lr, float momentum, float max_norm, int32_t nesterov,
+                       void *workspace, size_t workspace_bytes, float *norm_out, void *stream);
+
+/* ---- mixtures of sparse layers --------------------------------------------------------
+ * A mixture sends every column (example) to the k experts that a router picks for it, and adds up their results with the
+ * router's weights.  The experts are sparse layers; the router's logits Z (experts, ldz) are any layer's output.
+ *     expert_route     which experts, with which weights             -> chosen, weights (k, ldk)
+ *     expert_place     each choice's place in its expert's block     -> placement
+ *     expert_dispatch  columns of X to the blocks Xe                 (experts, features, lde)
+ *     sparse_linear_forward on block e of Xe, with `capacity` for the batch, for every expert e
+ *     expert_combine   the experts' results Ye back to columns       Y (features, ldy)
+ * and for training, in reverse: expert_combine_backward, sparse_linear_backward on every block, expert_combine without
+ * weights on the blocks' dX (the gradient of X), expert_route_backward.
+ * Block e of an operand (experts, features, lde) starts at e * features * lde; it is an operand (features, lde) of the calls
+ * above with `capacity` columns, lde >= capacity.  Sizes are known before the router has run: nothing waits for the device, and the whole
+ * sequence may be captured.  1 <= experts <= 1024, 1 <= k <= 32; batch * k < 2^30.
+ * Inputs and outputs of one call must not overlap. */
+enum {
+    NERVA_EXPERT_SIGMOID = 1,       /* scores are sigmoids of the logits, else their softmax over all experts       */
+    NERVA_EXPERT_RENORMALISE = 2,   /* weights are divided by their sum over the column's choices                   */
+    NERVA_EXPERT_GROUP_PAIR = 4     /* a group's score is the sum of its two best keys, else its best key           */
+};
+/* With score s_e and key q_e = s_e + bias[e] (bias for balance, may be NULL; without it and without NERVA_EXPERT_GROUP_PAIR the
+ * logit itself is the key, which orders alike), the experts of a column are, best first, the k of largest key; among equal
+ * keys the lower expert comes first.  With groups > 1 the experts are cut into so many groups of consecutive ones (at most 64,
+ * of equal size) and only those of the top_groups groups of largest score may be chosen (ties as above).  Keys are formed and compared
+ * in 64 bits.  Weights come from the scores, without the bias:
+ *     weights[j,c] = scale * s_e, or scale * s_e / (sum of s over the column's choices).
+ * An expert whose logit is -inf (or whose key is -inf or NaN) is never chosen; a column with fewer than k experts left
+ * gets chosen = -1 and weight 0 for the rest.  A NaN logit (or +inf under the softmax) is not chosen either and makes all weights of its
+ * column NaN.  k <= (experts / groups) * top_groups. */
+int expert_route(const float *Z, int32_t ldz, const float *bias, int32_t experts, int32_t batch, int32_t k,
+                 int32_t groups, int32_t top_groups, int32_t flags, float scale,
+                 int32_t *chosen, float *weights, int32_t ldk, void *stream);
+/* Gradient of the logits from that of the weights, with the choices held fixed; flags and scale as in expert_route.  All of
+ * dZ (experts, lddz) is written; experts that were not chosen get 0, but under a softmax that is not renormalised.  Choices outside
+ * 0 .. experts-1 are left out, and their dweights are not read. */
+int expert_route_backward(const float *Z, int32_t ldz, const int32_t *chosen, const float *dweights, int32_t ldk,
+                          int32_t experts, int32_t batch, int32_t k, int32_t flags, float scale,
+                          float *dZ, int32_t lddz, void *stream);
+
+/* Places.  Choice (j, c) takes place slots[j,c] = the number of choices of the same expert before it, in the order of columns and, inside a
+ * column, of choices; from `capacity` on there is none (slots = -1: the choice is dropped), nor for a choice outside 0 .. experts-1.
+ * counts[e] is the number of choices of expert e, dropped ones included.  slots (k, ldk) and counts[experts] may be NULL.
+ * placement: device memory of expert_placement_bytes(), 16-byte aligned, that the calls below read; it holds for the same
+ * experts, batch, k and capacity only.  (expert_placement_bytes is 0 for sizes that are refused.) */
+size_t expert_placement_bytes(int32_t experts, int32_t batch, int32_t k);
+int expert_place(const int32_t *chosen, int32_t ldk, int32_t experts, int32_t batch, int32_t k, int32_t capacity,
+                 int32_t *slots, int32_t *counts, void *placement, size_t placement_bytes, void *stream);
+
+/* Xe[e, f, place] = X[f, c] for every choice that has a place, 0 in the other places below `capacity`. */
+int expert_dispatch(const float *X, int32_t ldx, const void *placement, size_t placement_bytes, int32_t features,
+                    int32_t experts, int32_t batch, int32_t k, int32_t capacity, float *Xe, int32_t lde, void *stream);
+
+/* Y[f, c] = sum over the column's choices that have a place of weights[j, c] * Ye[e, f, place], in the order of the experts; 0 where
+ * none has.  weights == NULL: all 1, which makes this the backward pass of expert_dispatch.  Places that hold no column are
+ * not read. */
+int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t placement_bytes, const float *weights,
+                   int32_t ldk, int32_t features, int32_t experts, int32_t batch, int32_t k, int32_t capacity,
+                   float *Y, int32_t ldy, void *stream);
+
+/* Backward pass of expert_combine:
+ *     dYe[e, f, place] = weights[j, c] * dY[f, c], 0 in places that hold no column      (skipped if NULL)
+ *     dweights[j, c]   = sum_f Ye[e, f, place] * dY[f, c], 0 for choices without a place (skipped if NULL)
+ * Ye and dYe have the same lde; dweights has the ldk of weights.  workspace: device scratch, 16-byte aligned, of
+ * expert_combine_workspace_bytes(), for dweights (may be NULL without). */
+size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k);
+int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32_t lddy, const void *placement,
+                            size_t placement_bytes, const float *weights, int32_t ldk, int32_t features, int32_t experts,
+                            int32_t batch, int32_t k, int32_t capacity, float *dYe, float *dweights,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- MLP training step ---------------------------------------------------------------
  * mlp_create chains n_layers layers (layer l's cols = layer l-1's rows; hidden layers
  * ReLU, last layer NERVA_ACT_NONE) and binds the momentum buffers: velocities[l] is
@@ -351,6 +445,15 @@ int mlp_workspace_layout(const nerva_mlp *mlp, int32_t batch, int64_t *layout_ho
 int mlp_train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels,
                    int32_t batch, float lr, float momentum, void *workspace,
                    size_t workspace_bytes, float *loss_out, void *stream);
+
+/* mlp_train_step with the gradients of all layers, weights and biases, clipped together to max_norm (see
+ * sgd_update_clipped, also for a norm that is not finite: the weights and momentum buffers then stay as they were).  The gradients are formed
+ * as with NERVA_MLP_UNFUSED and can be read from the workspace afterwards, unclipped, at g_l and db_l.  workspace: at least
+ * mlp_clipped_workspace_bytes().  norm_out: one device float (may be NULL). */
+size_t mlp_clipped_workspace_bytes(const nerva_mlp *mlp, int32_t batch);
+int mlp_train_step_clipped(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels, int32_t batch,
+                           float lr, float momentum, float max_norm, void *workspace, size_t workspace_bytes,
+                           float *loss_out, float *norm_out, void *stream);
 
 /* mlp_train_step for callers that cannot allocate device memory or keep a workspace of their own --
  * code under HIP graph capture, tight training loops, harnesses that forbid hipMalloc.  The same

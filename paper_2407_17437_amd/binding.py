@@ -29,6 +29,7 @@ NERVA_WAVES_PER_BLOCK = 16
 (NERVA_TABLE_WAVES, NERVA_TABLE_HUGE_ROWS, NERVA_TABLE_SHORT_ROWS, NERVA_TABLE_LONG_WAVES, NERVA_TABLE_STAGED_ROWS, NERVA_TABLE_STAGED_ENDS) = range(6)
 NERVA_ROUTE_FORWARD_STRIPS, NERVA_ROUTE_BACKWARD_HOT_ROWS = 1, 2
 NERVA_STATIC_WORKSPACE_BYTES = 32 << 20
+NERVA_EXPERT_SIGMOID, NERVA_EXPERT_RENORMALISE, NERVA_EXPERT_GROUP_PAIR = 1, 2, 4
 NERVA_HUGE_FLAG = 0x40000000
 
 EXPORTS = [
@@ -37,6 +38,9 @@ EXPORTS = [
     "sparse_linear_forward", "sparse_linear_backward", "sgd_update_values", "sgd_update_values_nesterov",
     "softmax_cross_entropy", "mlp_create", "mlp_destroy", "mlp_rebind_velocity", "mlp_workspace_bytes",
     "mlp_workspace_layout", "mlp_train_step", "mlp_train_step_static", "mlp_forward", "nerva_copy_f32",
+    "gradient_norm_workspace_bytes", "gradient_norm", "gradient_clip", "sgd_update_clipped", "mlp_clipped_workspace_bytes", "mlp_train_step_clipped",
+    "expert_route", "expert_route_backward", "expert_placement_bytes", "expert_place", "expert_dispatch", "expert_combine",
+    "expert_combine_workspace_bytes", "expert_combine_backward",
     "mlp_profile_enable", "mlp_profile_read", "mlp_profile_slot_name", "sparse_linear_partition", "sparse_linear_routes",
 ]
 
@@ -82,6 +86,20 @@ def _load() -> ctypes.CDLL:
         "mlp_train_step": (ctypes.c_int, [vp, vp, i32, vp, i32, f32, f32, vp, sz, vp, vp]),
         "mlp_train_step_static": (ctypes.c_int, [vp, vp, i32, vp, i32, f32, f32, vp, vp]),
         "mlp_forward": (ctypes.c_int, [vp, vp, i32, i32, vp, sz, vp]),
+        "gradient_norm_workspace_bytes": (sz, [i32]),
+        "gradient_norm": (ctypes.c_int, [i32, vp, vp, vp, sz, vp, vp]),
+        "gradient_clip": (ctypes.c_int, [i32, vp, vp, vp, f32, vp, sz, vp, vp]),
+        "sgd_update_clipped": (ctypes.c_int, [i32, vp, vp, vp, vp, f32, f32, f32, i32, vp, sz, vp, vp]),
+        "mlp_clipped_workspace_bytes": (sz, [vp, i32]),
+        "mlp_train_step_clipped": (ctypes.c_int, [vp, vp, i32, vp, i32, f32, f32, f32, vp, sz, vp, vp, vp]),
+        "expert_route": (ctypes.c_int, [vp, i32, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, i32, vp]),
+        "expert_route_backward": (ctypes.c_int, [vp, i32, vp, vp, i32, i32, i32, i32, i32, f32, vp, i32, vp]),
+        "expert_placement_bytes": (sz, [i32, i32, i32]),
+        "expert_place": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]),
+        "expert_dispatch": (ctypes.c_int, [vp, i32, vp, sz, i32, i32, i32, i32, i32, vp, i32, vp]),
+        "expert_combine": (ctypes.c_int, [vp, i32, vp, sz, vp, i32, i32, i32, i32, i32, i32, vp, i32, vp]),
+        "expert_combine_workspace_bytes": (sz, [i32, i32, i32]),
+        "expert_combine_backward": (ctypes.c_int, [vp, i32, vp, i32, vp, sz, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]),
         "nerva_copy_f32": (ctypes.c_int, [vp, vp, i64, vp]),
         "sparse_linear_partition": (ctypes.c_int, [vp, i32, i32, vp, vp]),
         "sparse_linear_routes": (ctypes.c_int, [vp, i32, vp]),
@@ -131,6 +149,9 @@ try:
     from . import _fastcall  # built beside the library where torch's headers are
     _fastcall.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "sparse_linear_forward", "sparse_linear_backward", "sgd_update_values", "sgd_update_values_nesterov", "mlp_train_step", "mlp_forward")))
+    _fastcall.bind_mixtures(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "expert_route", "expert_route_backward", "expert_place", "expert_dispatch", "expert_combine", "expert_combine_backward", "gradient_norm",
+        "gradient_clip", "sgd_update_clipped")))
 except ImportError:
     from .calls import Calls
     _fastcall = Calls(lib, _stream)
@@ -327,6 +348,92 @@ def mlp_forward(mlp: int, X, ldx: Optional[int], batch: int, workspace, stream=N
         _check(rc)
 
 
+def mlp_train_step_clipped(mlp: int, X, ldx: Optional[int], labels, batch: int, lr: float, momentum: float, max_norm: float, workspace, loss_out, norm_out,
+                           stream=None) -> None:
+    """X as in mlp_train_step; workspace: a tensor of at least mlp_clipped_workspace_bytes."""
+    xp = X if isinstance(X, int) else _ptr(X)
+    _check(lib.mlp_train_step_clipped(mlp, xp, _ld(X) if ldx is None else ldx, labels if isinstance(labels, int) else _ptr(labels), batch, lr, momentum, max_norm,
+                                      _ptr(workspace), workspace.nbytes, _ptr(loss_out), _ptr(norm_out), _stream(stream)))
+
+
+def mlp_clipped_workspace_bytes(mlp: int, batch: int) -> int:
+    return int(lib.mlp_clipped_workspace_bytes(mlp, batch))
+
+
+# Clipped gradients: the lists hold contiguous float32 tensors of any shape, whose lengths are the counts of the C calls.
+
+def gradient_norm_workspace_bytes(n: int) -> int:
+    return int(lib.gradient_norm_workspace_bytes(n))
+
+
+def gradient_norm(grads, workspace, norm_out, stream=None) -> None:
+    rc = _fastcall.norm(grads, workspace, norm_out, stream)
+    if rc:
+        _check(rc)
+
+
+def gradient_clip(grads, clipped, max_norm: float, workspace, norm_out, stream=None) -> None:
+    rc = _fastcall.clip(grads, clipped, max_norm, workspace, norm_out, stream)
+    if rc:
+        _check(rc)
+
+
+def sgd_update_clipped(values, velocities, grads, lr: float, momentum: float, max_norm: float, nesterov: bool, workspace, norm_out, stream=None) -> None:
+    rc = _fastcall.update_clipped(values, velocities, grads, lr, momentum, max_norm, nesterov, workspace, norm_out, stream)
+    if rc:
+        _check(rc)
+
+
+# Mixtures: leading dimensions are the tensors' own; the types, shapes and devices of the tensors are checked against the sizes of the call.
+
+def expert_route(Z, bias, experts: int, batch: int, k: int, groups: int, top_groups: int, flags: int, scale: float, chosen, weights, stream=None) -> None:
+    rc = _fastcall.route(Z, bias, experts, batch, k, groups, top_groups, flags, scale, chosen, weights, stream)
+    if rc:
+        _check(rc)
+
+
+def expert_route_backward(Z, chosen, dweights, experts: int, batch: int, k: int, flags: int, scale: float, dZ, stream=None) -> None:
+    rc = _fastcall.route_backward(Z, chosen, dweights, experts, batch, k, flags, scale, dZ, stream)
+    if rc:
+        _check(rc)
+
+
+def expert_placement_bytes(experts: int, batch: int, k: int) -> int:
+    n = int(lib.expert_placement_bytes(experts, batch, k))
+    if n == 0:
+        raise NervaError(NERVA_ERR_ARGUMENT, last_error())
+    return n
+
+
+def expert_place(chosen, experts: int, batch: int, k: int, capacity: int, slots, counts, placement, stream=None) -> None:
+    rc = _fastcall.place(chosen, experts, batch, k, capacity, slots, counts, placement, stream)
+    if rc:
+        _check(rc)
+
+
+def expert_dispatch(X, placement, features: int, experts: int, batch: int, k: int, capacity: int, Xe, stream=None) -> None:
+    rc = _fastcall.dispatch(X, placement, features, experts, batch, k, capacity, Xe, stream)
+    if rc:
+        _check(rc)
+
+
+def expert_combine(Ye, placement, weights, features: int, experts: int, batch: int, k: int, capacity: int, Y, stream=None) -> None:
+    rc = _fastcall.combine(Ye, placement, weights, features, experts, batch, k, capacity, Y, stream)
+    if rc:
+        _check(rc)
+
+
+def expert_combine_workspace_bytes(features: int, batch: int, k: int) -> int:
+    return int(lib.expert_combine_workspace_bytes(features, batch, k))
+
+
+def expert_combine_backward(Ye, dY, placement, weights, features: int, experts: int, batch: int, k: int, capacity: int, dYe, dweights, workspace,
+                            stream=None) -> None:
+    rc = _fastcall.combine_backward(Ye, dY, placement, weights, features, experts, batch, k, capacity, dYe, dweights, workspace, stream)
+    if rc:
+        _check(rc)
+
+
 def mlp_profile_enable(mlp: int, max_steps: int) -> None:
     _check(lib.mlp_profile_enable(mlp, max_steps))
 
@@ -363,6 +470,14 @@ def to_dense(array, device="cuda", ld: Optional[int] = None) -> torch.Tensor:
     out = dense(t.shape[0], t.shape[1], device, ld)
     out.copy_(t)
     return out
+
+
+def expert_blocks(experts: int, features: int, capacity: int, device="cuda", ld: Optional[int] = None) -> torch.Tensor:
+    """(experts, features, capacity) fp32 view of an (experts, features, ld) allocation, padding as in `dense`: block e is an operand of
+    the experts' layers."""
+    ld = padded_ld(capacity) if ld is None else ld
+    full = torch.full((experts, features, ld), float("nan"), dtype=torch.float32, device=device)
+    return full[:, :, :capacity]
 
 
 class SparseLinear:
@@ -421,10 +536,11 @@ class MLP:
         self.max_batch = max_batch
         self.handle = mlp_create([l.handle for l in self.layers], [l.velocity for l in self.layers],
                                  [l.bias_velocity for l in self.layers], max_batch, flags)
-        nbytes = mlp_workspace_bytes(self.handle, max_batch)
+        nbytes = mlp_clipped_workspace_bytes(self.handle, max_batch)
         # NaN-filled so that a read of something never written cannot pass unnoticed
         self.workspace = torch.full((nbytes // 4,), float("nan"), dtype=torch.float32, device=device)
         self.loss = torch.zeros(1, dtype=torch.float32, device=device)
+        self.norm = torch.zeros(1, dtype=torch.float32, device=device)
         self._layout_batch = None
         self._layout = None
 
@@ -452,12 +568,16 @@ class MLP:
         mlp_rebind_velocity(self.handle, l, self.layers[l].velocity)
         # the workspace layout holds one float per stored entry of every layer: it moves with nnz
         self._layout_batch = None
-        nbytes = mlp_workspace_bytes(self.handle, self.max_batch)
+        nbytes = mlp_clipped_workspace_bytes(self.handle, self.max_batch)
         if nbytes // 4 > self.workspace.numel():
             self.workspace = torch.full((nbytes // 4,), float("nan"), dtype=torch.float32, device=self.workspace.device)
 
     def train_step(self, X, labels, batch: int, lr: float, momentum: float, ldx: Optional[int] = None):
         mlp_train_step(self.handle, X, ldx, labels, batch, lr, momentum, self.workspace, self.loss)
+
+    def train_step_clipped(self, X, labels, batch: int, lr: float, momentum: float, max_norm: float, ldx: Optional[int] = None):
+        """The gradients' norm before clipping is left in `norm`."""
+        mlp_train_step_clipped(self.handle, X, ldx, labels, batch, lr, momentum, max_norm, self.workspace, self.loss, self.norm)
 
     def forward(self, X, batch: int, ldx: Optional[int] = None):
         rc = _fastcall.mlp_forward(self.handle, X, ldx, batch, self.workspace, None)

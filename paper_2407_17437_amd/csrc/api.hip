@@ -15,6 +15,7 @@
 #include <mutex>
 #include <vector>
 
+#include "experts.h"
 #include "kernels.h"
 
 using namespace nerva;
@@ -1666,8 +1667,9 @@ int mlp_forward(nerva_mlp *mlp, const float *X, int32_t ldx, int32_t batch, void
     return forward_chain(mlp, X, ldx, batch, static_cast<char *>(workspace), L, as_stream(stream), mlp->layers.size());
 }
 
+// clip: the gradients of all layers are formed first, and the step is made with what their norm leaves of them
 static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels, int32_t batch, float lr,
-                      float momentum, void *workspace, const Layout &L, float *loss_out, void *stream);
+                      float momentum, void *workspace, const Layout &L, float *loss_out, void *stream, const ClipArgs *clip = nullptr);
 
 int mlp_train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels, int32_t batch, float lr,
                    float momentum, void *workspace, size_t workspace_bytes, float *loss_out, void *stream)
@@ -1699,14 +1701,51 @@ int mlp_train_step_static(nerva_mlp *mlp, const float *X, int32_t ldx, const int
     return train_step(mlp, X, ldx, labels, batch, lr, momentum, ws, L, loss_out, stream);
 }
 
+// Every layer's arrays as one list, the last layer's first: the order in which mlp_train_step updates them.
+static int step_clipped(nerva_mlp *mlp, char *ws, const Layout &L, const ClipArgs &clip, hipStream_t s)
+{
+    const int n = static_cast<int>(mlp->layers.size());
+    constexpr int kInline = 64;
+    float *w_[kInline], *v_[kInline];
+    const float *g_[kInline];
+    int64_t c_[kInline];
+    float **w = w_, **v = v_;
+    const float **g = g_;
+    int64_t *c = c_;
+    char *more = nullptr;
+    if (2 * n > kInline) {
+        more = static_cast<char *>(malloc(static_cast<size_t>(2 * n) * 32));
+        if (!more) return fail(NERVA_ERR_ARGUMENT, "out of host memory");
+        w = reinterpret_cast<float **>(more);
+        v = w + 2 * n;
+        g = const_cast<const float **>(v + 2 * n);
+        c = reinterpret_cast<int64_t *>(g + 2 * n);
+    }
+    int k = 0;
+    for (int l = n - 1; l >= 0; --l) {
+        const nerva_layer *ly = mlp->layers[l];
+        w[k] = ly->values; v[k] = mlp->vel[l]; g[k] = reinterpret_cast<const float *>(ws + L[l].g); c[k++] = ly->nnz;
+        if (!ly->bias) continue;
+        w[k] = ly->bias; v[k] = mlp->bias_vel[l]; g[k] = reinterpret_cast<const float *>(ws + L[l].db); c[k++] = ly->rows;
+    }
+    const ArrayList list{k, w, v, g, nullptr, c};
+    hipError_t e;
+    {
+        Timed tm(mlp->prof, s, "norm+momentum", 0);
+        e = launch_clipped(list, clip, s);
+    }
+    free(more);
+    return e == hipSuccess ? static_cast<int>(NERVA_OK) : hip_fail(e, "launch_clipped");
+}
+
 static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels, int32_t batch, float lr,
-                      float momentum, void *workspace, const Layout &L, float *loss_out, void *stream)
+                      float momentum, void *workspace, const Layout &L, float *loss_out, void *stream, const ClipArgs *clip)
 {
     int rc = NERVA_OK;
     hipStream_t s = as_stream(stream);
     char *ws = static_cast<char *>(workspace);
     const int n = static_cast<int>(mlp->layers.size());
-    const bool fused = !(mlp->flags & NERVA_MLP_UNFUSED);
+    const bool fused = !(mlp->flags & NERVA_MLP_UNFUSED) && !clip;
     const int nesterov = (mlp->flags & NERVA_MLP_NESTEROV) ? 1 : 0;
     auto A = [&](int l) { return reinterpret_cast<float *>(ws + L[l].A); };
     auto dZ = [&](int l) { return reinterpret_cast<float *>(ws + L[l].dZ); };
@@ -1919,6 +1958,19 @@ static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t
         if ((rc = flush_sampled()) != NERVA_OK) return rc;
     } else {
         const bool as_chain = n > (head ? 2 : 1) && !use_dense(mlp->layers[1], batch) && !use_dense(mlp->layers[0], batch) && chain_shape_ok(make_T(1), make_S(1), make_S(0));
+        // the copies of a layer's values that later steps read
+        auto refresh = [&](int l) -> int {
+            nerva_layer *ly = mlp->layers[l];
+            if (l > 0) {
+                Timed tm(mlp->prof, s, "mirror_refresh", l);
+                HIP_TRY(launch_gather(ly->values_t, ly->values, ly->perm, ly->nnz, s));
+            }
+            if (ly->dense_on) {
+                Timed tm(mlp->prof, s, "dense_refresh", l);
+                HIP_TRY(refresh_dense_copies(ly, s));
+            }
+            return NERVA_OK;
+        };
         for (int l = n - 1; l >= 0; --l) {
             nerva_layer *ly = mlp->layers[l];
             if (l > 0 && !(head && l == n - 1)) {
@@ -1939,22 +1991,20 @@ static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t
                 Timed tm(mlp->prof, s, "sddmm", l);
                 HIP_TRY(launch_sddmm(g, s));
             }
-            {
+            if (!clip) {
                 Timed tm(mlp->prof, s, "momentum_values", l);
                 HIP_TRY(launch_momentum(ly->values, mlp->vel[l], g.g, ly->nnz, lr, momentum, nesterov, s));
             }
-            if (ly->bias) {
+            if (!clip && ly->bias) {
                 Timed tm(mlp->prof, s, "momentum_bias", l);
                 HIP_TRY(launch_momentum(ly->bias, mlp->bias_vel[l], g.db, ly->rows, lr, momentum, nesterov, s));
             }
-            if (l > 0) {
-                Timed tm(mlp->prof, s, "mirror_refresh", l);
-                HIP_TRY(launch_gather(ly->values_t, ly->values, ly->perm, ly->nnz, s));
-            }
-            if (ly->dense_on) {
-                Timed tm(mlp->prof, s, "dense_refresh", l);
-                HIP_TRY(refresh_dense_copies(ly, s));
-            }
+            if (!clip && (rc = refresh(l)) != NERVA_OK) return rc;
+        }
+        if (clip) {
+            if ((rc = step_clipped(mlp, ws, L, *clip, s)) != NERVA_OK) return rc;
+            for (int l = n - 1; l >= 0; --l)
+                if ((rc = refresh(l)) != NERVA_OK) return rc;
         }
     }
     if (mlp->prof.on && mlp->prof.step < mlp->prof.max_steps) {
@@ -1964,6 +2014,245 @@ static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t
         HIP_TRY(hipEventRecord(e, s));
         ++mlp->prof.step;
     }
+    return NERVA_OK;
+}
+
+// ---- clipped gradients ------------------------------------------------------------------------
+
+size_t gradient_norm_workspace_bytes(int32_t n) { return n < 0 ? 0 : static_cast<size_t>(norm_workspace_bytes(n)); }
+
+// (values, velocities: nullptr where a call has none)
+static int check_list(int32_t n, const void *values, const void *velocities, const float *const *grads, const int64_t *counts, bool update,
+                      const void *workspace, size_t workspace_bytes)
+{
+    if (n < 0) return fail(NERVA_ERR_ARGUMENT, "n is negative");
+    if (n > 0 && (!grads || !counts || (update && (!values || !velocities)))) return fail(NERVA_ERR_ARGUMENT, "null list");
+    for (int32_t t = 0; t < n; ++t) {
+        if (counts[t] < 0) return fail(NERVA_ERR_ARGUMENT, "array %d has a negative length", t);
+        if (counts[t] == 0) continue;
+        if (!grads[t]) return fail(NERVA_ERR_ARGUMENT, "gradient %d is null", t);
+        if (values && !static_cast<float *const *>(values)[t]) return fail(NERVA_ERR_ARGUMENT, "array %d is null", t);
+        if (velocities && !static_cast<float *const *>(velocities)[t]) return fail(NERVA_ERR_ARGUMENT, "velocity %d is null", t);
+        if (counts[t] > INT64_C(1) << 40) return fail(NERVA_ERR_SHAPE, "array %d has %lld entries, more than 2^40", t, (long long)counts[t]);
+    }
+    if (!workspace) return fail(NERVA_ERR_ARGUMENT, "workspace is null");
+    if (reinterpret_cast<uintptr_t>(workspace) % 8) return fail(NERVA_ERR_WORKSPACE, "workspace must be 8-byte aligned");
+    if (workspace_bytes < static_cast<size_t>(norm_workspace_bytes(n)))
+        return fail(NERVA_ERR_WORKSPACE, "workspace has %zu bytes, %lld needed", workspace_bytes, (long long)norm_workspace_bytes(n));
+    return NERVA_OK;
+}
+
+static int check_max_norm(float max_norm)
+{
+    return max_norm > 0.f ? static_cast<int>(NERVA_OK) : fail(NERVA_ERR_ARGUMENT, "max_norm must be positive (got %g)", static_cast<double>(max_norm));
+}
+
+int gradient_norm(int32_t n, const float *const *grads, const int64_t *counts, void *workspace, size_t workspace_bytes,
+                  float *norm_out, void *stream)
+{
+    const int rc = check_list(n, nullptr, nullptr, grads, counts, false, workspace, workspace_bytes);
+    if (rc != NERVA_OK) return rc;
+    if (!norm_out) return fail(NERVA_ERR_ARGUMENT, "norm_out is null");
+    const ArrayList l{n, nullptr, nullptr, grads, nullptr, counts};
+    HIP_TRY(launch_norm(l, static_cast<double *>(workspace), norm_out, as_stream(stream)));
+    return NERVA_OK;
+}
+
+int gradient_clip(int32_t n, const float *const *grads, float *const *clipped, const int64_t *counts, float max_norm,
+                  void *workspace, size_t workspace_bytes, float *norm_out, void *stream)
+{
+    if (n > 0 && !clipped) return fail(NERVA_ERR_ARGUMENT, "null list");
+    int rc = check_list(n, clipped, nullptr, grads, counts, false, workspace, workspace_bytes);
+    if (rc == NERVA_OK) rc = check_max_norm(max_norm);
+    if (rc != NERVA_OK) return rc;
+    const ArrayList l{n, nullptr, nullptr, grads, clipped, counts};
+    const ClipArgs c{0.f, 0.f, max_norm, 0, static_cast<double *>(workspace), norm_out};
+    HIP_TRY(launch_clipped(l, c, as_stream(stream)));
+    return NERVA_OK;
+}
+
+int sgd_update_clipped(int32_t n, float *const *values, float *const *velocities, const float *const *grads, const int64_t *counts,
+                       float lr, float momentum, float max_norm, int32_t nesterov, void *workspace, size_t workspace_bytes,
+                       float *norm_out, void *stream)
+{
+    int rc = check_list(n, values, velocities, grads, counts, true, workspace, workspace_bytes);
+    if (rc == NERVA_OK) rc = check_max_norm(max_norm);
+    if (rc != NERVA_OK) return rc;
+    const ArrayList l{n, values, velocities, grads, nullptr, counts};
+    const ClipArgs c{lr, momentum, max_norm, nesterov != 0, static_cast<double *>(workspace), norm_out};
+    HIP_TRY(launch_clipped(l, c, as_stream(stream)));
+    return NERVA_OK;
+}
+
+size_t mlp_clipped_workspace_bytes(const nerva_mlp *mlp, int32_t batch)
+{
+    const size_t step = mlp_workspace_bytes(mlp, batch);
+    return step ? step + static_cast<size_t>(norm_workspace_bytes(2 * static_cast<int64_t>(mlp->layers.size()))) : 0;
+}
+
+int mlp_train_step_clipped(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t *labels, int32_t batch, float lr,
+                           float momentum, float max_norm, void *workspace, size_t workspace_bytes, float *loss_out,
+                           float *norm_out, void *stream)
+{
+    Layout L;
+    int rc = check_step_args(mlp, X, ldx, batch, workspace, workspace_bytes, L);
+    if (rc == NERVA_OK) rc = check_max_norm(max_norm);
+    if (rc != NERVA_OK) return rc;
+    if (!labels) return fail(NERVA_ERR_ARGUMENT, "labels is null");
+    const size_t need = static_cast<size_t>(L.bytes) + static_cast<size_t>(norm_workspace_bytes(2 * static_cast<int64_t>(mlp->layers.size())));
+    if (workspace_bytes < need) return fail(NERVA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    const ClipArgs clip{lr, momentum, max_norm, (mlp->flags & NERVA_MLP_NESTEROV) ? 1 : 0,
+                        reinterpret_cast<double *>(static_cast<char *>(workspace) + L.bytes), norm_out};
+    return train_step(mlp, X, ldx, labels, batch, lr, momentum, workspace, L, loss_out, stream, &clip);
+}
+
+// ---- mixtures -----------------------------------------------------------------------------------
+
+static int check_experts(int32_t experts, int32_t batch, int32_t k, int32_t ldk)
+{
+    if (experts < 1 || experts > kExpertsMax) return fail(NERVA_ERR_ARGUMENT, "experts = %d is not in 1 .. %d", experts, kExpertsMax);
+    if (k < 1 || k > kChoicesMax) return fail(NERVA_ERR_ARGUMENT, "k = %d is not in 1 .. %d", k, kChoicesMax);
+    const int rc = check_batch(batch, ldk, "ldk");
+    if (rc != NERVA_OK) return rc;
+    if (static_cast<int64_t>(batch) * k > INT32_MAX / 2) return fail(NERVA_ERR_SHAPE, "%d choices for each of %d columns are not supported", k, batch);
+    return NERVA_OK;
+}
+
+static int check_route(int32_t experts, int32_t batch, int32_t k, int32_t ldk, int32_t flags, float scale)
+{
+    const int rc = check_experts(experts, batch, k, ldk);
+    if (rc != NERVA_OK) return rc;
+    if (flags & ~(NERVA_EXPERT_SIGMOID | NERVA_EXPERT_RENORMALISE | NERVA_EXPERT_GROUP_PAIR)) return fail(NERVA_ERR_ARGUMENT, "unknown flags 0x%x", flags);
+    if (!(scale - scale == 0.f)) return fail(NERVA_ERR_ARGUMENT, "scale must be finite");
+    return NERVA_OK;
+}
+
+int expert_route(const float *Z, int32_t ldz, const float *bias, int32_t experts, int32_t batch, int32_t k, int32_t groups,
+                 int32_t top_groups, int32_t flags, float scale, int32_t *chosen, float *weights, int32_t ldk, void *stream)
+{
+    if (!Z || !chosen || !weights) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    int rc = check_route(experts, batch, k, ldk, flags, scale);
+    if (rc == NERVA_OK) rc = check_batch(batch, ldz, "ldz");
+    if (rc != NERVA_OK) return rc;
+    if (groups < 1 || groups > kGroupsMax || experts % groups) return fail(NERVA_ERR_ARGUMENT, "%d experts cannot be cut into %d groups (at most %d)", experts, groups, kGroupsMax);
+    if (top_groups < 1 || top_groups > groups) return fail(NERVA_ERR_ARGUMENT, "top_groups = %d is not in 1 .. %d", top_groups, groups);
+    if (k > experts / groups * top_groups) return fail(NERVA_ERR_ARGUMENT, "%d choices among %d experts", k, experts / groups * top_groups);
+    if (groups == 1) flags &= ~NERVA_EXPERT_GROUP_PAIR;   // (all experts are one group: no score to form)
+    const RouteArgs a{Z, ldz, bias, experts, batch, k, groups, top_groups, flags, scale, chosen, weights, ldk};
+    HIP_TRY(launch_route(a, as_stream(stream)));
+    return NERVA_OK;
+}
+
+int expert_route_backward(const float *Z, int32_t ldz, const int32_t *chosen, const float *dweights, int32_t ldk, int32_t experts,
+                          int32_t batch, int32_t k, int32_t flags, float scale, float *dZ, int32_t lddz, void *stream)
+{
+    if (!Z || !chosen || !dweights || !dZ) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    int rc = check_route(experts, batch, k, ldk, flags, scale);
+    if (rc == NERVA_OK) rc = check_batch(batch, ldz, "ldz");
+    if (rc == NERVA_OK) rc = check_batch(batch, lddz, "lddz");
+    if (rc != NERVA_OK) return rc;
+    const RouteBackwardArgs a{Z, ldz, chosen, dweights, ldk, experts, batch, k, flags, scale, dZ, lddz};
+    HIP_TRY(launch_route_backward(a, as_stream(stream)));
+    return NERVA_OK;
+}
+
+size_t expert_placement_bytes(int32_t experts, int32_t batch, int32_t k)
+{
+    if (check_experts(experts, batch, k, batch) != NERVA_OK) return 0;
+    return static_cast<size_t>(placement_of(nullptr, experts, batch, k).bytes);
+}
+
+// the parts of a caller's placement
+static int check_placement(const void *placement, size_t placement_bytes, int32_t experts, int32_t batch, int32_t k, int32_t capacity, Placement &p)
+{
+    if (!placement) return fail(NERVA_ERR_ARGUMENT, "placement is null");
+    if (capacity < 1 || capacity >= (1 << 30)) return fail(NERVA_ERR_ARGUMENT, "capacity must be positive (got %d)", capacity);
+    p = placement_of(const_cast<void *>(placement), experts, batch, k);
+    if (reinterpret_cast<uintptr_t>(placement) % 16) return fail(NERVA_ERR_WORKSPACE, "placement must be 16-byte aligned");
+    if (placement_bytes < static_cast<size_t>(p.bytes)) return fail(NERVA_ERR_WORKSPACE, "placement has %zu bytes, %lld needed", placement_bytes, (long long)p.bytes);
+    return NERVA_OK;
+}
+
+int expert_place(const int32_t *chosen, int32_t ldk, int32_t experts, int32_t batch, int32_t k, int32_t capacity, int32_t *slots,
+                 int32_t *counts, void *placement, size_t placement_bytes, void *stream)
+{
+    if (!chosen) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    PlaceArgs a{chosen, ldk, experts, batch, k, capacity, slots, counts, Placement{}};
+    int rc = check_experts(experts, batch, k, ldk);
+    if (rc == NERVA_OK) rc = check_placement(placement, placement_bytes, experts, batch, k, capacity, a.p);
+    if (rc != NERVA_OK) return rc;
+    HIP_TRY(launch_place(a, as_stream(stream)));
+    return NERVA_OK;
+}
+
+static int check_exchange(ExchangeArgs &a, const void *placement, size_t placement_bytes, int32_t ldc, const char *ldc_name, int32_t ldb)
+{
+    if (a.features <= 0) return fail(NERVA_ERR_ARGUMENT, "features must be positive (got %d)", a.features);
+    int rc = check_experts(a.experts, a.batch, a.k, a.batch);
+    if (rc == NERVA_OK) rc = check_placement(placement, placement_bytes, a.experts, a.batch, a.k, a.capacity, a.p);
+    if (rc == NERVA_OK) rc = check_batch(a.batch, ldc, ldc_name);
+    if (rc != NERVA_OK) return rc;
+    if (ldb < a.capacity || ldb >= (1 << 30)) return fail(NERVA_ERR_SHAPE, "lde = %d does not hold a capacity of %d", ldb, a.capacity);
+    // one work-group per tile of columns and few rows
+    if (static_cast<int64_t>(a.features) * (a.p.tiles + 1) > INT32_MAX) return fail(NERVA_ERR_SHAPE, "%d features of %d columns are not supported", a.features, a.batch);
+    a.ldc = ldc;
+    a.ldb = ldb;
+    return NERVA_OK;
+}
+
+int expert_dispatch(const float *X, int32_t ldx, const void *placement, size_t placement_bytes, int32_t features, int32_t experts,
+                    int32_t batch, int32_t k, int32_t capacity, float *Xe, int32_t lde, void *stream)
+{
+    if (!X || !Xe) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    ExchangeArgs a{};
+    a.columns = X; a.out_blocks = Xe;
+    a.features = features; a.experts = experts; a.batch = batch; a.k = k; a.capacity = capacity;
+    const int rc = check_exchange(a, placement, placement_bytes, ldx, "ldx", lde);
+    if (rc != NERVA_OK) return rc;
+    HIP_TRY(launch_dispatch(a, as_stream(stream)));
+    return NERVA_OK;
+}
+
+int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t placement_bytes, const float *weights, int32_t ldk,
+                   int32_t features, int32_t experts, int32_t batch, int32_t k, int32_t capacity, float *Y, int32_t ldy, void *stream)
+{
+    if (!Ye || !Y) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    ExchangeArgs a{};
+    a.blocks = Ye; a.out_columns = Y; a.weights = weights; a.ldk = ldk;
+    a.features = features; a.experts = experts; a.batch = batch; a.k = k; a.capacity = capacity;
+    int rc = check_exchange(a, placement, placement_bytes, ldy, "ldy", lde);
+    if (rc == NERVA_OK && weights) rc = check_batch(batch, ldk, "ldk");
+    if (rc != NERVA_OK) return rc;
+    HIP_TRY(launch_combine(a, as_stream(stream)));
+    return NERVA_OK;
+}
+
+size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k)
+{
+    if (features <= 0 || batch <= 0 || k < 1 || k > kChoicesMax) return 0;
+    return static_cast<size_t>((features + kPartialRows - 1) / kPartialRows) * static_cast<size_t>(batch) * static_cast<size_t>(k) * 4;
+}
+
+int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32_t lddy, const void *placement, size_t placement_bytes,
+                            const float *weights, int32_t ldk, int32_t features, int32_t experts, int32_t batch, int32_t k, int32_t capacity,
+                            float *dYe, float *dweights, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!dY || (!dYe && !dweights)) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    if (dweights && !Ye) return fail(NERVA_ERR_ARGUMENT, "dweights needs the experts' results Ye");
+    ExchangeArgs a{};
+    a.columns = dY; a.blocks = Ye; a.out_blocks = dYe; a.weights = weights; a.dweights = dweights; a.ldk = ldk;
+    a.features = features; a.experts = experts; a.batch = batch; a.k = k; a.capacity = capacity;
+    int rc = check_exchange(a, placement, placement_bytes, lddy, "lddy", lde);
+    if (rc == NERVA_OK && (weights || dweights)) rc = check_batch(batch, ldk, "ldk");
+    if (rc != NERVA_OK) return rc;
+    if (dweights) {
+        const size_t need = expert_combine_workspace_bytes(features, batch, k);
+        if (!workspace) return fail(NERVA_ERR_ARGUMENT, "dweights needs a workspace");
+        if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(NERVA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+        if (workspace_bytes < need) return fail(NERVA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+        a.partial = static_cast<float *>(workspace);
+    }
+    HIP_TRY(launch_combine_backward(a, as_stream(stream)));
     return NERVA_OK;
 }
 

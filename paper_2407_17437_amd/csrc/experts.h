@@ -1,0 +1,119 @@
+// Internal launch interface between the C ABI (api.hip) and the kernels of mixtures (experts.hip) and of clipped
+// gradients (clip.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace nerva {
+
+// ---- routing (experts.hip) ----------------------------------------------------------------
+struct RouteArgs {
+    const float *Z;
+    int64_t ldz;
+    const float *bias;     // [experts] or nullptr
+    int32_t experts, batch, k, groups, top_groups, flags;
+    float scale;
+    int32_t *chosen;       // (k, ldk)
+    float *weights;        // (k, ldk)
+    int64_t ldk;
+};
+struct RouteBackwardArgs {
+    const float *Z;
+    int64_t ldz;
+    const int32_t *chosen;
+    const float *dweights;
+    int64_t ldk;
+    int32_t experts, batch, k, flags;
+    float scale;
+    float *dZ;
+    int64_t lddz;
+};
+hipError_t launch_route(const RouteArgs &a, hipStream_t s);
+hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s);
+
+// ---- places of columns in the experts' blocks -----------------------------------------------
+// The batch is cut into tiles of kPlaceTile columns.  Every tile has a list of its choices: those that have a place, by expert
+// and then by place, followed by those that have none.  An entry is {place or -1, column in the tile | choice << 10 | expert << 15}.
+constexpr int32_t kPlaceTile = 1024;
+constexpr int32_t kPlaceSub = 256;           // columns per work-group that assigns places
+constexpr int32_t kExpertsMax = 1024;        // 10 bits (and one more for "no expert")
+constexpr int32_t kChoicesMax = 32;          // 5 bits
+constexpr int32_t kGroupsMax = 64;           // one per lane
+
+struct Placement {
+    int32_t *filled;       // [experts] places that hold a column
+    int32_t *listed;       // [tiles] entries with a place
+    int32_t *before;       // [(subs + 1) * experts] choices of an expert per run of kPlaceSub columns
+    int2 *lists;           // [batch * k]: tile t's from t * kPlaceTile * k on
+    int32_t tiles, subs;
+    int64_t bytes;
+};
+// the parts of a caller's buffer (which may be nullptr, for its size)
+inline Placement placement_of(void *memory, int32_t experts, int32_t batch, int32_t k)
+{
+    Placement p{};
+    p.tiles = (batch + kPlaceTile - 1) / kPlaceTile;
+    p.subs = (batch + kPlaceSub - 1) / kPlaceSub;
+    const int64_t lists = static_cast<int64_t>(batch) * k * 8;
+    char *m = static_cast<char *>(memory);
+    p.lists = reinterpret_cast<int2 *>(m);
+    p.filled = reinterpret_cast<int32_t *>(m + lists);
+    p.listed = p.filled + experts;
+    p.before = p.listed + p.tiles;
+    p.bytes = (lists + 4 * (experts + p.tiles + static_cast<int64_t>(p.subs + 1) * experts) + 15) / 16 * 16;
+    return p;
+}
+
+struct PlaceArgs {
+    const int32_t *chosen;
+    int64_t ldk;
+    int32_t experts, batch, k, capacity;
+    int32_t *slots;        // (k, ldk) or nullptr
+    int32_t *counts;       // [experts] or nullptr
+    Placement p;
+};
+hipError_t launch_place(const PlaceArgs &a, hipStream_t s);
+
+// Columns to blocks and back.  Block e of an operand (experts, features, ld) starts at e * features * ld.
+struct ExchangeArgs {
+    const float *columns;  // (features, ldc): X of the dispatch, dY of the combine's backward pass
+    float *out_columns;    // (features, ldc): Y of the combine
+    int64_t ldc;
+    const float *blocks;   // Ye
+    float *out_blocks;     // Xe, dYe
+    int64_t ldb;
+    const float *weights;  // (k, ldk) or nullptr: all 1
+    float *dweights;       // (k, ldk) or nullptr
+    int64_t ldk;
+    float *partial;        // [row groups * batch * k]
+    int32_t features, experts, batch, k, capacity;
+    Placement p;
+};
+constexpr int32_t kPartialRows = 16;         // rows of the operands whose products one entry of `partial` adds up
+hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s);
+hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s);
+hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s);
+
+// ---- norm over many arrays (clip.hip) -------------------------------------------------------
+constexpr int32_t kNormBlocks = 512;         // work-groups that the arrays are shared out to, and one more for each array
+inline int64_t norm_workspace_bytes(int64_t arrays) { return (8 * (kNormBlocks + arrays) + 255) / 256 * 256; }
+
+struct ArrayList {
+    int32_t n;
+    float *const *values;            // updated arrays, or nullptr
+    float *const *velocities;
+    const float *const *grads;
+    float *const *clipped;           // scaled gradients, or nullptr
+    const int64_t *counts;
+};
+struct ClipArgs {
+    float lr, momentum, max_norm;
+    int32_t nesterov;
+    double *partial;
+    float *norm_out;                 // or nullptr
+};
+hipError_t launch_norm(const ArrayList &l, double *partial, float *norm_out, hipStream_t s);
+// the norm, then the momentum step (l.values) or the scaled gradients (l.clipped)
+hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s);
+
+}  // namespace nerva

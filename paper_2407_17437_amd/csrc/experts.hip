@@ -1,0 +1,682 @@
+// Mixtures of sparse layers: routing of columns to experts, places in the experts' blocks, and the exchange of columns
+// with the blocks in both directions, forward and backward.
+#include "../../include/nerva_sparse.h"
+#include "device.h"
+#include "experts.h"
+
+namespace nerva {
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+
+// Reductions over a wave in which lanes that a step leaves out keep what they have (dpp() of device.h gives them 0).
+template <int CTRL, int ROW_MASK = 0xF>
+__device__ __forceinline__ float dpp_keep(float x)
+{
+    const int v = __builtin_bit_cast(int, x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, CTRL, ROW_MASK, 0xF, false));
+}
+template <int CTRL, int ROW_MASK = 0xF>
+__device__ __forceinline__ double dpp_keep(double x)
+{
+    const uint64_t v = __builtin_bit_cast(uint64_t, x);
+    const int lo = static_cast<int>(v), hi = static_cast<int>(v >> 32);
+    const uint32_t l = __builtin_amdgcn_update_dpp(lo, lo, CTRL, ROW_MASK, 0xF, false);
+    const uint32_t h = __builtin_amdgcn_update_dpp(hi, hi, CTRL, ROW_MASK, 0xF, false);
+    return __builtin_bit_cast(double, static_cast<uint64_t>(h) << 32 | l);
+}
+__device__ __forceinline__ float read_lane(float x, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); }
+__device__ __forceinline__ double read_lane(double x, int lane)
+{
+    const uint64_t v = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+
+// largest over the wave (no lane holds NaN), wave-uniform
+template <typename T>
+__device__ __forceinline__ T wave_max(T x)
+{
+    x = larger(x, dpp_keep<0xB1>(x));        // quad_perm [1,0,3,2]
+    x = larger(x, dpp_keep<0x4E>(x));        // quad_perm [2,3,0,1]
+    x = larger(x, dpp_keep<0x141>(x));       // row_half_mirror
+    x = larger(x, dpp_keep<0x140>(x));       // row_mirror
+    x = larger(x, dpp_keep<0x142, 0xA>(x));  // row_bcast15 into rows 1 and 3
+    x = larger(x, dpp_keep<0x143, 0xC>(x));  // row_bcast31 into rows 2 and 3
+    return read_lane(x, 63);
+}
+// sum over the wave in one fixed order
+__device__ __forceinline__ double wave_sum(double x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) { return group_sum<kWave>(x); }
+
+// logarithm of the sigmoid, which does not run out of range where the sigmoid itself does
+__device__ __forceinline__ float log_sigmoid(float z) { return fminf(z, 0.f) - log1pf(expf(-fabsf(z))); }
+
+// ---- routing -----------------------------------------------------------------------------------
+// A work-group takes `cols` columns: their logits come to LDS row by row, then a wave works on one column at a time,
+// lane l holding the experts l, l + 64, ...  The k choices are k rounds of a maximum over the wave; among equal keys
+// the lowest expert is found from ballots.
+//
+// Keys.  Softmax and sigmoid rise with the logit, so without a bias the logits themselves are the keys.  With a bias, or where
+// a group's score is a sum, the scores are, in 64 bits: two biased scores that differ by less than 32 bits
+// tell apart are common among a few hundred experts, and the choice must not depend on how a sum was rounded.
+template <int R, typename Key>
+__global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const int cols)
+{
+    extern __shared__ __align__(16) char lds_raw[];
+    const int E = a.experts, k = a.k;
+    const int waves = blockDim.x / kWave, lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int pitch = cols + 1;                                         // (a column's logits fall on different banks)
+    float *tile = reinterpret_cast<float *>(lds_raw);                   // [E][pitch]
+    const int tile_floats = (E * pitch + 3) / 4 * 4;
+    int32_t *out_e = reinterpret_cast<int32_t *>(tile + tile_floats);   // [cols][k]
+    float *out_w = reinterpret_cast<float *>(out_e + cols * k);
+    Key *keys = reinterpret_cast<Key *>(lds_raw + (tile_floats + 2 * cols * k + 3) / 4 * 16) + wv * E;   // [waves][E], with groups only
+
+    const int c0 = blockIdx.x * cols, here = min(cols, a.batch - c0);
+    for (int i = threadIdx.x; i < E * cols; i += blockDim.x) {
+        const int e = i / cols, c = i - e * cols;
+        if (c < here) tile[e * pitch + c] = a.Z[static_cast<int64_t>(e) * a.ldz + c0 + c];
+    }
+    __syncthreads();
+
+    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, pair = a.flags & NERVA_EXPERT_GROUP_PAIR;
+    const int size = E / a.groups;
+    const Key kNone = -static_cast<Key>(kInf);
+    for (int c = wv; c < here; c += waves) {
+        float z[R];
+        float top = -kInf;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int e = lane + i * kWave;
+            z[i] = e < E ? tile[e * pitch + c] : -kInf;
+            const bool off = !(z[i] == z[i]) || (!sigmoid && z[i] == kInf);
+            bad |= off;
+            if (off) z[i] = -kInf;                                      // not to be chosen
+            top = fmaxf(top, z[i]);
+        }
+        bad = __ballot(bad) != 0;
+        Key key[R];
+        float sum = 0.f;
+        if constexpr (sizeof(Key) == 8) {
+            double total = 1.0;
+            if (!sigmoid) {
+                top = wave_max(top);
+                total = 0.0;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    key[i] = z[i] == -kInf ? 0.0 : exp(static_cast<double>(z[i]) - static_cast<double>(top));
+                    total += key[i];
+                }
+                total = wave_sum(total);
+                sum = static_cast<float>(total);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int e = lane + i * kWave;
+                Key q = sigmoid ? 1.0 / (1.0 + exp(-static_cast<double>(z[i]))) : key[i] / total;
+                if (a.bias && e < E) q += static_cast<double>(a.bias[e]);
+                key[i] = z[i] == -kInf || !(q == q) ? kNone : q;
+            }
+        } else {
+            if (!sigmoid && !renormalise) {
+                top = wave_max(top);
+#pragma unroll
+                for (int i = 0; i < R; ++i) sum += z[i] == -kInf ? 0.f : expf(z[i] - top);
+                sum = wave_sum(sum);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) key[i] = z[i];
+        }
+
+        if (a.groups > 1) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (lane + i * kWave < E) keys[lane + i * kWave] = key[i];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            Key best = kNone, second = kNone;
+            if (lane < a.groups)
+                for (int i = 0; i < size; ++i) {
+                    const Key q = keys[lane * size + i];
+                    second = q > best ? best : larger(second, q);
+                    best = larger(best, q);
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            Key score = pair && second > kNone ? best + second : best;
+            uint64_t open = 0;
+            for (int t = 0; t < a.top_groups; ++t) {
+                const Key m = wave_max(score);
+                if (!(m > kNone)) break;
+                const int g = __builtin_ctzll(__ballot(score == m));
+                open |= 1ull << g;
+                if (lane == g) score = kNone;
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (!(open >> (min(lane + i * kWave, E - 1) / size) & 1)) key[i] = kNone;
+        }
+
+        // lane j ends up with the j-th choice
+        int mine = -1;
+        for (int j = 0; j < k; ++j) {
+            Key m = key[0];
+#pragma unroll
+            for (int i = 1; i < R; ++i) m = larger(m, key[i]);
+            m = wave_max(m);
+            if (!(m > kNone)) break;
+            int e = -1;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const uint64_t at = __ballot(key[i] == m);
+                if (e < 0 && at) {
+                    e = __builtin_ctzll(at) + i * kWave;
+                    if (lane == (e & (kWave - 1))) key[i] = kNone;
+                }
+            }
+            if (lane == j) mine = e;
+        }
+
+        const float zm = mine >= 0 ? tile[mine * pitch + c] : -kInf;
+        float w = 0.f;
+        if (renormalise) {
+            const float l = mine < 0 ? -kInf : sigmoid ? log_sigmoid(zm) : zm;
+            const float high = wave_max(l);
+            const float u = mine < 0 ? 0.f : expf(l - high);
+            w = u / wave_sum(u);
+        } else {
+            w = sigmoid ? 1.f / (1.f + expf(-zm)) : expf(zm - top) / sum;
+        }
+        w = mine >= 0 ? w * a.scale : 0.f;
+        if (bad) w = __builtin_nanf("");
+        if (lane < k) {
+            out_e[c * k + lane] = mine;
+            out_w[c * k + lane] = w;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < cols * k; i += blockDim.x) {
+        const int j = i / cols, c = i - j * cols;
+        if (c >= here) continue;
+        a.chosen[j * a.ldk + c0 + c] = out_e[c * k + j];
+        a.weights[j * a.ldk + c0 + c] = out_w[c * k + j];
+    }
+}
+
+// Gradient of the logits.  With u = weight / scale, d the gradients of the column's weights:
+//     renormalised    dL_j = scale u_j (d_j - sum_i u_i d_i),  dz = dL for softmax, dL (1 - s) for sigmoid
+//     softmax         dz_e = scale p_e ([e chosen] d_e - sum_i p_i d_i), over all experts
+//     sigmoid         dz_e = scale s_e (1 - s_e) d_e
+// A lane owns a column and keeps its k choices in registers; the waves of a work-group share the experts, whose rows are
+// written whole, zeros included.
+constexpr int kBackWaves = 8;
+template <int K>
+__global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(const RouteBackwardArgs a)
+{
+    __shared__ float red[2][kBackWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int own = blockIdx.x * kWave + lane, c = min(own, a.batch - 1);
+    const int E = a.experts;
+    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE;
+    int e[K];
+    float g[K], z[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        e[j] = j < a.k ? a.chosen[j * a.ldk + c] : -1;
+        if (e[j] < 0 || e[j] >= E) e[j] = -1;
+        g[j] = e[j] >= 0 ? a.dweights[j * a.ldk + c] : 0.f;
+        z[j] = e[j] >= 0 ? a.Z[static_cast<int64_t>(e[j]) * a.ldz + c] : -kInf;
+    }
+    const bool full = !sigmoid && !renormalise;
+    float top = -kInf, inv = 0.f, all = 0.f;
+    if (full) {
+        float m = -kInf;
+        for (int i = wv; i < E; i += kBackWaves) m = fmaxf(m, a.Z[static_cast<int64_t>(i) * a.ldz + c]);
+        red[0][wv][lane] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kBackWaves; ++w) top = fmaxf(top, red[0][w][lane]);
+        float s = 0.f;
+        for (int i = wv; i < E; i += kBackWaves) {
+            const float x = a.Z[static_cast<int64_t>(i) * a.ldz + c];
+            s += x == -kInf ? 0.f : expf(x - top);
+        }
+        red[1][wv][lane] = s;
+        __syncthreads();
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kBackWaves; ++w) s += red[1][w][lane];
+        inv = 1.f / s;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            g[j] = e[j] >= 0 ? a.scale * g[j] * (expf(z[j] - top) * inv) : 0.f;
+            all += g[j];
+        }
+    } else if (renormalise) {
+        float l[K], high = -kInf, s = 0.f, mean = 0.f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            l[j] = e[j] < 0 ? -kInf : sigmoid ? log_sigmoid(z[j]) : z[j];
+            high = fmaxf(high, l[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            l[j] = e[j] >= 0 ? expf(l[j] - high) : 0.f;
+            s += l[j];
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            l[j] = e[j] >= 0 ? l[j] / s : 0.f;
+            mean = fmaf(l[j], g[j], mean);
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            g[j] = e[j] >= 0 ? a.scale * l[j] * (g[j] - mean) : 0.f;
+            if (sigmoid && e[j] >= 0) g[j] *= 1.f / (1.f + expf(z[j]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (e[j] >= 0) g[j] *= a.scale * (1.f / (1.f + expf(-z[j]))) * (1.f / (1.f + expf(z[j])));
+    }
+    if (own >= a.batch) return;
+    for (int i = wv; i < E; i += kBackWaves) {
+        float d = 0.f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) d += e[j] == i ? g[j] : 0.f;
+        if (full) {
+            const float x = a.Z[static_cast<int64_t>(i) * a.ldz + c];
+            if (!(x == -kInf)) d -= expf(x - top) * inv * all;
+        }
+        a.dZ[static_cast<int64_t>(i) * a.lddz + c] = d;
+    }
+}
+
+template <int R, typename Key>
+hipError_t route_go(const RouteArgs &a, int cols, int waves, size_t lds, hipStream_t s)
+{
+    hipLaunchKernelGGL((route_kernel<R, Key>), dim3((a.batch + cols - 1) / cols), dim3(waves * kWave), lds, s, a, cols);
+    return hipGetLastError();
+}
+
+// ---- places --------------------------------------------------------------------------------------
+constexpr int kPlaceThreads = 512;
+constexpr int kPlaceWaves = kPlaceThreads / kWave;
+constexpr int kSubsPerTile = kPlaceTile / kPlaceSub;
+
+__device__ __forceinline__ int expert_at(const PlaceArgs &a, int c, int j)
+{
+    const int e = a.chosen[j * a.ldk + c];
+    return e >= 0 && e < a.experts ? e : a.experts;   // (one more for "no expert")
+}
+
+// choices of every expert in one run of kPlaceSub columns
+__global__ __launch_bounds__(kPlaceThreads) void place_count_kernel(const PlaceArgs a)
+{
+    __shared__ int32_t n[kExpertsMax + 1];
+    for (int e = threadIdx.x; e <= a.experts; e += kPlaceThreads) n[e] = 0;
+    __syncthreads();
+    const int c0 = blockIdx.x * kPlaceSub, here = min(kPlaceSub, a.batch - c0);
+    for (int i = threadIdx.x; i < here * a.k; i += kPlaceThreads) {
+        const int j = i / here;
+        atomicAdd(&n[expert_at(a, c0 + i - j * here, j)], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += kPlaceThreads) a.p.before[static_cast<int64_t>(blockIdx.x) * a.experts + e] = n[e];
+}
+
+// exclusive scan of x over the work-group's threads; *total: the sum
+__device__ __forceinline__ int block_scan(int x, int *lds, int *total)
+{
+    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x >> 6;
+    int s = x;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int y = __shfl_up(s, d, kWave);
+        if (lane >= d) s += y;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) lds[wv] = s;
+    __syncthreads();
+    int off = 0, all = 0;
+    for (int w = 0; w < kPlaceWaves; ++w) {
+        off += w < wv ? lds[w] : 0;
+        all += lds[w];
+    }
+    *total = all;
+    return off + s - x;
+}
+
+// Places of one run of kPlaceSub columns.  A choice's place is the number of choices of its expert before it, in the order of columns
+// and, in a column, of choices: those of the runs before (added up here from their counts), of the run's earlier rounds of one choice per
+// thread, of the waves before in the round, and of the lanes before in the wave (the lanes that hold the same expert, from one
+// ballot per bit of its number).
+__global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
+{
+    __shared__ int32_t next[kExpertsMax + 1];     // the expert's next place
+    __shared__ int32_t kept_at[kExpertsMax + 1];  // list position of a place: kept_at + place, or ...
+    __shared__ int32_t lost_at[kExpertsMax + 1];  // ... lost_at + place, of places beyond the capacity
+    __shared__ int32_t scan[kPlaceWaves];
+    extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in this round
+    const int E = a.experts, E1 = E + 1;
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int sub = blockIdx.x, tile = sub / kSubsPerTile;
+    const int tile_sub = tile * kSubsPerTile, tile_end = min(tile_sub + kSubsPerTile, a.p.subs);
+    const int c0 = sub * kPlaceSub, here = min(kPlaceSub, a.batch - c0);
+
+    // choices per expert: before the tile, before this run, in the tile
+    if (a.p.subs == 1) {   // (nobody has counted)
+        for (int e = threadIdx.x; e < E1; e += kPlaceThreads) next[e] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < here * a.k; i += kPlaceThreads) {
+            const int j = i / here;
+            atomicAdd(&next[expert_at(a, c0 + i - j * here, j)], 1);
+        }
+        __syncthreads();
+    }
+    int kept_total = 0, lost_total = 0, mine_total = 0;
+    const int per = (E1 + kPlaceThreads - 1) / kPlaceThreads;   // consecutive experts per thread
+    int kept[(kExpertsMax + 1 + kPlaceThreads - 1) / kPlaceThreads], lost[sizeof kept / sizeof *kept], at[sizeof kept / sizeof *kept], now[sizeof kept / sizeof *kept];
+    const int first = threadIdx.x * per;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof kept / sizeof *kept); ++i) {
+        kept[i] = lost[i] = at[i] = now[i] = 0;
+        const int e = first + i;
+        if (i >= per || e >= E) continue;
+        int before = 0, inside = 0, mine = 0;
+        if (a.p.subs == 1) {
+            inside = next[e];
+        } else {
+            const int32_t *n = a.p.before + e;
+            for (int q = 0; q < tile_sub; ++q) before += n[static_cast<int64_t>(q) * E];
+            for (int q = tile_sub; q < tile_end; ++q) {
+                const int x = n[static_cast<int64_t>(q) * E];
+                inside += x;
+                mine += q < sub ? x : 0;
+            }
+        }
+        at[i] = before;
+        now[i] = before + mine;
+        kept[i] = min(a.capacity, before + inside) - min(a.capacity, before);
+        lost[i] = inside - kept[i];
+        mine_total += mine;
+        kept_total += kept[i];
+        lost_total += lost[i];
+        if (tile == a.p.tiles - 1 && sub == tile_sub) {   // one work-group knows the whole batch
+            if (a.counts) a.counts[e] = before + inside;
+            a.p.filled[e] = min(a.capacity, before + inside);
+        }
+    }
+    int kept_all, lost_all, mine_all;
+    int kept_off = block_scan(kept_total, scan, &kept_all);
+    int lost_off = block_scan(lost_total, scan, &lost_all);
+    (void)block_scan(mine_total, scan, &mine_all);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof kept / sizeof *kept); ++i) {
+        const int e = first + i;
+        if (i >= per || e >= E) continue;
+        next[e] = now[i];
+        kept_at[e] = kept_off - min(a.capacity, at[i]);
+        lost_at[e] = kept_all + lost_off - max(a.capacity, at[i]);
+        kept_off += kept[i];
+        lost_off += lost[i];
+    }
+    // choices of no expert come last, counted from the tile's start
+    if (threadIdx.x == 0) {
+        next[E] = (sub - tile_sub) * kPlaceSub * a.k - mine_all;
+        lost_at[E] = kept_all + lost_all;
+        if (sub == tile_sub) a.p.listed[tile] = kept_all;
+    }
+    for (int i = threadIdx.x; i < kPlaceWaves * E1; i += kPlaceThreads) by_wave[i] = 0;
+    __syncthreads();
+
+    int bits = 0;
+    while (E >> bits) ++bits;
+    int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
+    for (int r = 0; r < here * a.k; r += kPlaceThreads) {
+        const int i = r + threadIdx.x;
+        const bool on = i < here * a.k;
+        const int cl = i / a.k, j = i - cl * a.k;
+        const int e = on ? expert_at(a, c0 + cl, j) : 0;
+        uint64_t same = __ballot(on);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t has = __ballot(e >> b & 1);
+            same &= e >> b & 1 ? has : ~has;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (on && rank == 0) by_wave[wv * E1 + e] = __popcll(same);
+        __syncthreads();
+        for (int x = threadIdx.x; x < E1; x += kPlaceThreads) {
+            int p = next[x];
+            for (int w = 0; w < kPlaceWaves; ++w) {
+                const int n = by_wave[w * E1 + x];
+                by_wave[w * E1 + x] = p;
+                p += n;
+            }
+            next[x] = p;
+        }
+        __syncthreads();
+        int place = 0;
+        if (on) place = by_wave[wv * E1 + e] + rank;
+        __syncthreads();
+        for (int x = threadIdx.x; x < kPlaceWaves * E1; x += kPlaceThreads) by_wave[x] = 0;
+        __syncthreads();
+        if (!on) continue;
+        const bool has = e < E && place < a.capacity;
+        if (a.slots) a.slots[j * a.ldk + c0 + cl] = has ? place : -1;
+        const int column = c0 + cl - tile * kPlaceTile;
+        list[(has ? kept_at[e] : lost_at[e]) + place] = make_int2(has ? place : -1, column | j << 10 | e << 15);
+    }
+}
+
+// ---- exchange --------------------------------------------------------------------------------------
+struct Entry {
+    int place, column, choice, expert;
+};
+__device__ __forceinline__ Entry entry_of(int2 x) { return Entry{x.x, x.y & 1023, x.y >> 10 & 31, x.y >> 15}; }
+// whether an entry lies in this call's operands: a placement made for other sizes must not lead outside
+__device__ __forceinline__ bool inside(const Entry &t, const ExchangeArgs &a, int here)
+{
+    return static_cast<uint32_t>(t.place) < static_cast<uint32_t>(a.capacity) && t.column < here && t.choice < a.k && t.expert < a.experts;
+}
+
+// Columns to blocks: dispatch (kGrad false), or the combine's backward pass (kGrad true), which weighs the columns and takes their products
+// with the blocks' results.  A work-group keeps kRows rows of one tile's columns in LDS and walks through the tile's list, whose
+// neighbours lie next to each other in a block; one more work-group per group of rows clears the empty places.
+constexpr int kMoveThreads = 512;
+template <int kRows, bool kGrad>
+__global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeArgs a)
+{
+    extern __shared__ float rows[];   // [kRows][width]
+    const int tiles = a.p.tiles;
+    const int group = blockIdx.x / (tiles + 1), tile = blockIdx.x - group * (tiles + 1);
+    const int f0 = group * kRows, nf = min(kRows, a.features - f0);
+    if (tile == tiles) {
+        if (!a.out_blocks) return;
+        const int lane = threadIdx.x & (kWave - 1);
+        for (int e = wave_in_block(); e < a.experts; e += kMoveThreads / kWave) {
+            const int n = min(max(a.p.filled[e], 0), a.capacity);
+            float *block = a.out_blocks + (static_cast<int64_t>(e) * a.features + f0) * a.ldb;
+            for (int r = 0; r < nf; ++r, block += a.ldb)
+                for (int p = n + lane; p < a.capacity; p += kWave) block[p] = 0.f;
+        }
+        return;
+    }
+    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0), width = min(kPlaceTile, a.batch);
+    const float *in = a.columns + static_cast<int64_t>(f0) * a.ldc + c0;
+    for (int r = 0; r < nf; ++r, in += a.ldc)
+        for (int c = threadIdx.x; c < here; c += kMoveThreads) rows[r * width + c] = in[c];
+    __syncthreads();
+    const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
+    const int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
+    float *partial = kGrad ? a.partial + static_cast<int64_t>(group) * a.batch * a.k + static_cast<int64_t>(tile) * kPlaceTile * a.k : nullptr;
+    for (int i = threadIdx.x; i < kept; i += kMoveThreads) {
+        const Entry t = entry_of(list[i]);
+        if (!inside(t, a, here)) continue;
+        const int64_t at = (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
+        float *out = a.out_blocks + at;
+        if constexpr (kGrad) {
+            const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
+            const float *y = a.blocks + at;
+            float dot = 0.f;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                if (r >= nf) break;
+                const float d = rows[r * width + t.column];
+                if (a.dweights) dot = fmaf(y[r * a.ldb], d, dot);
+                if (a.out_blocks) out[r * a.ldb] = w * d;
+            }
+            if (a.dweights) partial[i] = dot;
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                if (r >= nf) break;
+                out[r * a.ldb] = rows[r * width + t.column];
+            }
+        }
+    }
+}
+
+// gradients of the weights from the products of every group of rows, added up in the order of the rows
+__global__ __launch_bounds__(256) void weight_gradient_kernel(const ExchangeArgs a, const int groups)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, total = static_cast<int64_t>(a.batch) * a.k;
+    if (i >= total) return;
+    const int tile = static_cast<int>(i / (static_cast<int64_t>(kPlaceTile) * a.k));
+    const int64_t from = static_cast<int64_t>(tile) * kPlaceTile * a.k;
+    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0);
+    const Entry t = entry_of(a.p.lists[i]);
+    if (t.column >= here || t.choice >= a.k) return;
+    double sum = 0.0;   // (hundreds of sums, each read once: 64 bits cost nothing)
+    if (i - from < a.p.listed[tile])
+        for (int g = 0; g < groups; ++g) sum += a.partial[g * total + i];
+    a.dweights[t.choice * a.ldk + c0 + t.column] = static_cast<float>(sum);
+}
+
+// Blocks to columns, Y = sum of the kept choices' results times their weights.  A wave keeps kRows rows of one tile's columns in
+// LDS, for itself alone, and adds the tile's list to them, entry by entry: reads of the blocks are as wide as the list's runs.
+constexpr int kCombineWaves = 4;
+template <int kRows>
+__global__ __launch_bounds__(kCombineWaves * kWave) void combine_kernel(const ExchangeArgs a)
+{
+    extern __shared__ float rows[];   // [waves][kRows][width]
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int tiles = a.p.tiles;
+    const int group = blockIdx.x / tiles, tile = blockIdx.x - group * tiles;
+    const int f0 = (group * kCombineWaves + wv) * kRows, nf = min(kRows, a.features - f0);
+    if (nf <= 0) return;              // (no barrier below: waves share nothing)
+    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0), width = min(kPlaceTile, a.batch);
+    float *sum = rows + wv * kRows * width;
+    for (int i = lane; i < kRows * width; i += kWave) sum[i] = 0.f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
+    const int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
+    for (int i = lane; i < kept; i += kWave) {
+        const Entry t = entry_of(list[i]);
+        if (!inside(t, a, here)) continue;
+        const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
+        const float *y = a.blocks + (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
+        float v[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) v[r] = r < nf ? y[r * a.ldb] : 0.f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            __hip_atomic_fetch_add(&sum[r * width + t.column], w * v[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    float *out = a.out_columns + static_cast<int64_t>(f0) * a.ldc + c0;
+    for (int r = 0; r < nf; ++r, out += a.ldc)
+        for (int c = lane; c < here; c += kWave) out[c] = sum[r * width + c];
+}
+
+template <int kRows, bool kGrad>
+hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
+{
+    const int groups = (a.features + kRows - 1) / kRows, width = a.batch < kPlaceTile ? a.batch : kPlaceTile;
+    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(static_cast<uint32_t>(groups) * (a.p.tiles + 1)), dim3(kMoveThreads), kRows * width * sizeof(float), s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_route(const RouteArgs &a, hipStream_t s)
+{
+    const bool wide = a.bias || (a.flags & NERVA_EXPERT_GROUP_PAIR);
+    int cols = a.batch >= 8192 ? 32 : a.batch >= 2048 ? 16 : a.batch >= 512 ? 8 : 4;
+    auto bytes = [&](int c) {
+        const int waves = c < 16 ? c : 16;
+        const size_t tile = static_cast<size_t>((a.experts * (c + 1) + 3) / 4 * 4 + 2 * c * a.k + 3) / 4 * 16;
+        return tile + (a.groups > 1 ? static_cast<size_t>(waves) * a.experts * (wide ? 8 : 4) : 0);
+    };
+    while (cols > 4 && bytes(cols) > 64 * 1024) cols /= 2;
+    const int waves = cols < 16 ? cols : 16;
+    const size_t lds = bytes(cols);
+    if (a.experts <= 64) return wide ? route_go<1, double>(a, cols, waves, lds, s) : route_go<1, float>(a, cols, waves, lds, s);
+    if (a.experts <= 128) return wide ? route_go<2, double>(a, cols, waves, lds, s) : route_go<2, float>(a, cols, waves, lds, s);
+    if (a.experts <= 256) return wide ? route_go<4, double>(a, cols, waves, lds, s) : route_go<4, float>(a, cols, waves, lds, s);
+    if (a.experts <= 512) return wide ? route_go<8, double>(a, cols, waves, lds, s) : route_go<8, float>(a, cols, waves, lds, s);
+    return wide ? route_go<16, double>(a, cols, waves, lds, s) : route_go<16, float>(a, cols, waves, lds, s);
+}
+
+template <int K>
+static void route_backward_go(const RouteBackwardArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL(route_backward_kernel<K>, dim3((a.batch + kWave - 1) / kWave), dim3(kBackWaves * kWave), 0, s, a);
+}
+
+hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s)
+{
+    if (a.k <= 1) route_backward_go<1>(a, s);
+    else if (a.k <= 2) route_backward_go<2>(a, s);
+    else if (a.k <= 4) route_backward_go<4>(a, s);
+    else if (a.k <= 8) route_backward_go<8>(a, s);
+    else if (a.k <= 16) route_backward_go<16>(a, s);
+    else route_backward_go<32>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_place(const PlaceArgs &a, hipStream_t s)
+{
+    if (a.p.subs > 1) {
+        hipLaunchKernelGGL(place_count_kernel, dim3(a.p.subs), dim3(kPlaceThreads), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(place_kernel, dim3(a.p.subs), dim3(kPlaceThreads), kPlaceWaves * (a.experts + 1) * sizeof(int32_t), s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s) { return dispatch_go<16, false>(a, s); }
+
+hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s)
+{
+    constexpr int kRows = 2;
+    const int groups = (a.features + kRows * kCombineWaves - 1) / (kRows * kCombineWaves), width = a.batch < kPlaceTile ? a.batch : kPlaceTile;
+    hipLaunchKernelGGL(combine_kernel<kRows>, dim3(static_cast<uint32_t>(groups) * a.p.tiles), dim3(kCombineWaves * kWave),
+                       kCombineWaves * kRows * width * sizeof(float), s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s)
+{
+    static_assert(kPartialRows == 16, "rows of one work-group");
+    hipError_t e = dispatch_go<kPartialRows, true>(a, s);
+    if (e != hipSuccess || !a.dweights) return e;
+    const int64_t total = static_cast<int64_t>(a.batch) * a.k;
+    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + 255) / 256)), dim3(256), 0, s, a, (a.features + kPartialRows - 1) / kPartialRows);
+    return hipGetLastError();
+}
+
+}  // namespace nerva
