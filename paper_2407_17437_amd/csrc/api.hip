@@ -2230,7 +2230,8 @@ int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t p
 size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k)
 {
     if (features <= 0 || batch <= 0 || k < 1 || k > kChoicesMax) return 0;
-    return static_cast<size_t>((features + kPartialRows - 1) / kPartialRows) * static_cast<size_t>(batch) * static_cast<size_t>(k) * 4;
+    const int32_t rows = partial_rows(features, batch);
+    return static_cast<size_t>((features + rows - 1) / rows) * static_cast<size_t>(batch) * static_cast<size_t>(k) * 4;
 }
 
 int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32_t lddy, const void *placement, size_t placement_bytes,

@@ -32,35 +32,42 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s);
 hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s);
 
 // ---- places of columns in the experts' blocks -----------------------------------------------
-// The batch is cut into tiles of kPlaceTile columns.  Every tile has a list of its choices: those that have a place, by expert
-// and then by place, followed by those that have none.  An entry is {place or -1, column in the tile | choice << 10 | expert << 15}.
-constexpr int32_t kPlaceTile = 1024;
+// The batch is cut into tiles of columns.  Every tile has a list of its choices: those that have a place, by expert and then by place,
+// followed by those that have none.  An entry is {place or -1, column in the tile | choice << 10 | expert << 15 | turn << 26}.
+// Entries that 64 lanes take at a time and that belong to one column get turns 0, 1, ... in their order; an expert's entries lie
+// next to each other in its block.
+// Tiles: as many columns as give an expert some kPlaceRun consecutive entries, a multiple of kPlaceSub.  Longer tiles would only
+// take local memory and parallelism from the kernels that hold a tile's columns.
+constexpr int32_t kPlaceTileMax = 1024;
 constexpr int32_t kPlaceSub = 256;           // columns per work-group that assigns places
-constexpr int32_t kExpertsMax = 1024;        // 10 bits (and one more for "no expert")
+constexpr int32_t kPlaceRun = 64;
+constexpr int32_t kExpertsMax = 1024;        // 11 bits, with "no expert"
 constexpr int32_t kChoicesMax = 32;          // 5 bits
 constexpr int32_t kGroupsMax = 64;           // one per lane
 
 struct Placement {
     int32_t *filled;       // [experts] places that hold a column
     int32_t *listed;       // [tiles] entries with a place
-    int32_t *before;       // [(subs + 1) * experts] choices of an expert per run of kPlaceSub columns
-    int2 *lists;           // [batch * k]: tile t's from t * kPlaceTile * k on
-    int32_t tiles, subs;
+    int32_t *before;       // [subs * experts] choices of an expert per run of kPlaceSub columns
+    int2 *lists;           // [batch * k]: tile t's from t * tile * k on
+    int32_t tile, tiles, subs;
     int64_t bytes;
 };
 // the parts of a caller's buffer (which may be nullptr, for its size)
 inline Placement placement_of(void *memory, int32_t experts, int32_t batch, int32_t k)
 {
     Placement p{};
-    p.tiles = (batch + kPlaceTile - 1) / kPlaceTile;
+    p.tile = kPlaceSub;
+    while (p.tile < kPlaceTileMax && p.tile * k < kPlaceRun * experts && p.tile <= batch / 4) p.tile *= 2;
+    p.tiles = (batch + p.tile - 1) / p.tile;
     p.subs = (batch + kPlaceSub - 1) / kPlaceSub;
-    const int64_t lists = static_cast<int64_t>(batch) * k * 8;
     char *m = static_cast<char *>(memory);
+    const int64_t lists = static_cast<int64_t>(batch) * k;
     p.lists = reinterpret_cast<int2 *>(m);
-    p.filled = reinterpret_cast<int32_t *>(m + lists);
+    p.filled = reinterpret_cast<int32_t *>(p.lists + lists);
     p.listed = p.filled + experts;
     p.before = p.listed + p.tiles;
-    p.bytes = (lists + 4 * (experts + p.tiles + static_cast<int64_t>(p.subs + 1) * experts) + 15) / 16 * 16;
+    p.bytes = (8 * lists + 4 * (experts + p.tiles + static_cast<int64_t>(p.subs) * experts) + 15) / 16 * 16;
     return p;
 }
 
@@ -89,7 +96,16 @@ struct ExchangeArgs {
     int32_t features, experts, batch, k, capacity;
     Placement p;
 };
-constexpr int32_t kPartialRows = 16;         // rows of the operands whose products one entry of `partial` adds up
+// Rows of the operands that one work-group moves: as many as leave the GPU two work-groups per compute unit.
+inline int32_t move_rows(int32_t features, int64_t tiles, int32_t most)
+{
+    int32_t rows = most;
+    while (rows > 4 && (features + rows - 1) / rows * tiles < 512) rows /= 2;
+    return rows;
+}
+// ... of the combine's backward pass, whose products over so many rows make one entry of `partial` (without the placement's tiles: the
+// workspace is asked for without the experts)
+inline int32_t partial_rows(int32_t features, int32_t batch) { return move_rows(features, (batch + kPlaceTileMax - 1) / kPlaceTileMax, 16); }
 hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s);

@@ -1,6 +1,8 @@
 // Mixtures of sparse layers: routing of columns to experts, places in the experts' blocks, and the exchange of columns
 // with the blocks in both directions, forward and backward.
 #include "../../include/nerva_sparse.h"
+#include <type_traits>
+
 #include "device.h"
 #include "experts.h"
 
@@ -311,7 +313,6 @@ hipError_t route_go(const RouteArgs &a, int cols, int waves, size_t lds, hipStre
 // ---- places --------------------------------------------------------------------------------------
 constexpr int kPlaceThreads = 512;
 constexpr int kPlaceWaves = kPlaceThreads / kWave;
-constexpr int kSubsPerTile = kPlaceTile / kPlaceSub;
 
 __device__ __forceinline__ int expert_at(const PlaceArgs &a, int c, int j)
 {
@@ -356,6 +357,21 @@ __device__ __forceinline__ int block_scan(int x, int *lds, int *total)
     return off + s - x;
 }
 
+// Turns of the 64 entries from i on (one wave): how many of the lanes before hold the same column, from one ballot per bit of it.
+__device__ __forceinline__ void set_turns(int2 *list, int i, int kept)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool on = i + lane < kept;
+    const int word = on ? list[i + lane].y : 0;
+    uint64_t same = __ballot(on);
+    for (int b = 0; b < 10; ++b) {
+        const uint64_t has = __ballot(word >> b & 1);
+        same &= word >> b & 1 ? has : ~has;
+    }
+    const int turn = __popcll(same & ((1ull << lane) - 1));
+    if (on && turn > 0) list[i + lane].y = static_cast<int>(static_cast<uint32_t>(word) | static_cast<uint32_t>(turn) << 26);
+}
+
 // Places of one run of kPlaceSub columns.  A choice's place is the number of choices of its expert before it, in the order of columns
 // and, in a column, of choices: those of the runs before (added up here from their counts), of the run's earlier rounds of one choice per
 // thread, of the waves before in the round, and of the lanes before in the wave (the lanes that hold the same expert, from one
@@ -369,8 +385,8 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
     extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in this round
     const int E = a.experts, E1 = E + 1;
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
-    const int sub = blockIdx.x, tile = sub / kSubsPerTile;
-    const int tile_sub = tile * kSubsPerTile, tile_end = min(tile_sub + kSubsPerTile, a.p.subs);
+    const int subs_per_tile = a.p.tile / kPlaceSub, sub = blockIdx.x, tile = sub / subs_per_tile;
+    const int tile_sub = tile * subs_per_tile, tile_end = min(tile_sub + subs_per_tile, a.p.subs);
     const int c0 = sub * kPlaceSub, here = min(kPlaceSub, a.batch - c0);
 
     // choices per expert: before the tile, before this run, in the tile
@@ -442,18 +458,20 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
 
     int bits = 0;
     while (E >> bits) ++bits;
-    int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
-    for (int r = 0; r < here * a.k; r += kPlaceThreads) {
-        const int i = r + threadIdx.x;
-        const bool on = i < here * a.k;
-        const int cl = i / a.k, j = i - cl * a.k;
+    int2 *list = a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k;
+    const int wave_columns = kWave / a.k;   // whole columns per wave, a lane for each of their choices
+    const int lane_column = lane / a.k, j = lane - lane_column * a.k;
+    for (int r = 0; r < here; r += kPlaceWaves * wave_columns) {
+        const int cl = r + wv * wave_columns + lane_column;
+        const bool on = lane_column < wave_columns && cl < here;
         const int e = on ? expert_at(a, c0 + cl, j) : 0;
         uint64_t same = __ballot(on);
         for (int b = 0; b < bits; ++b) {
             const uint64_t has = __ballot(e >> b & 1);
             same &= e >> b & 1 ? has : ~has;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
+        const uint64_t below = (1ull << lane) - 1;
+        const int rank = __popcll(same & below);
         if (on && rank == 0) by_wave[wv * E1 + e] = __popcll(same);
         __syncthreads();
         for (int x = threadIdx.x; x < E1; x += kPlaceThreads) {
@@ -474,138 +492,272 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
         if (!on) continue;
         const bool has = e < E && place < a.capacity;
         if (a.slots) a.slots[j * a.ldk + c0 + cl] = has ? place : -1;
-        const int column = c0 + cl - tile * kPlaceTile;
+        const int column = c0 + cl - tile * a.p.tile;
         list[(has ? kept_at[e] : lost_at[e]) + place] = make_int2(has ? place : -1, column | j << 10 | e << 15);
     }
+    if (subs_per_tile > 1) return;   // (place_turns_kernel follows)
+    __syncthreads();
+    for (int i = wv * kWave; i < kept_all; i += kPlaceThreads) set_turns(list, i, kept_all);
+}
+
+// the same for tiles that several work-groups have listed
+__global__ __launch_bounds__(kPlaceThreads) void place_turns_kernel(const PlaceArgs a, const int blocks_per_tile)
+{
+    const int tile = blockIdx.x / blocks_per_tile, i = (blockIdx.x - tile * blocks_per_tile) * kPlaceThreads + wave_in_block() * kWave;
+    const int kept = a.p.listed[tile];
+    if (i < kept) set_turns(a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k, i, kept);
 }
 
 // ---- exchange --------------------------------------------------------------------------------------
 struct Entry {
-    int place, column, choice, expert;
+    int place, column, choice, expert, turn;
 };
-__device__ __forceinline__ Entry entry_of(int2 x) { return Entry{x.x, x.y & 1023, x.y >> 10 & 31, x.y >> 15}; }
+__device__ __forceinline__ Entry entry_of(int2 x)
+{
+    return Entry{x.x, x.y & 1023, x.y >> 10 & 31, x.y >> 15 & 2047, static_cast<int>(static_cast<uint32_t>(x.y) >> 26)};
+}
 // whether an entry lies in this call's operands: a placement made for other sizes must not lead outside
 __device__ __forceinline__ bool inside(const Entry &t, const ExchangeArgs &a, int here)
 {
     return static_cast<uint32_t>(t.place) < static_cast<uint32_t>(a.capacity) && t.column < here && t.choice < a.k && t.expert < a.experts;
 }
 
+// Work-groups are numbered tile by tile and then by rows, and every XCD gets one run of consecutive ones: the runs of one row that
+// neighbouring tiles read or write share cache lines, which then meet in one L2.
+__device__ __forceinline__ int xcd_run(int block, int blocks) { return (block & 7) * (blocks >> 3) + (block >> 3); }   // (blocks: a multiple of 8)
+
+// Rows of a matrix to LDS, `pitch` (a multiple of 4) apart: all of a thread's reads are in flight before the first is written.
+__device__ __forceinline__ void stage_rows(float *lds, int pitch, const float *in, int64_t ld, int n, int columns)
+{
+    const int threads = blockDim.x;
+    if (columns < 4) {
+        for (int i = threadIdx.x; i < n * columns; i += threads) lds[i / columns * pitch + i % columns] = in[i / columns * ld + i % columns];
+        return;
+    }
+    const int per_row = (columns + 3) >> 2, total = n * per_row;
+    for (int i = threadIdx.x; i < total; i += 4 * threads) {
+        float4 x[4];
+        int at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = min(i + u * threads, total - 1), r = j / per_row, c = four_columns(4 * (j - r * per_row), columns);
+            x[u] = ld4(in + r * ld + c);
+            at[u] = r * pitch + c;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            float *p = lds + at[u];
+            if ((at[u] & 3) == 0) {
+                *reinterpret_cast<float4 *>(p) = x[u];
+            } else {   // (a row's last four, where its length is no multiple of 4)
+                p[0] = x[u].x;
+                p[1] = x[u].y;
+                p[2] = x[u].z;
+                p[3] = x[u].w;
+            }
+        }
+    }
+}
+__device__ __host__ __forceinline__ int pitch_of(int batch, int tile) { return ((batch < tile ? batch : tile) + 3) / 4 * 4; }
+
 // Columns to blocks: dispatch (kGrad false), or the combine's backward pass (kGrad true), which weighs the columns and takes their products
 // with the blocks' results.  A work-group keeps kRows rows of one tile's columns in LDS and walks through the tile's list, whose
-// neighbours lie next to each other in a block; one more work-group per group of rows clears the empty places.
-constexpr int kMoveThreads = 512;
+// neighbours lie next to each other in a block.  The empty places are cleared on the way, a share of the experts by each tile's work-groups.
+constexpr int kMoveThreads = 1024;   // at most; one per entry of the list where that is fewer
 template <int kRows, bool kGrad>
 __global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeArgs a)
 {
-    extern __shared__ float rows[];   // [kRows][width]
-    const int tiles = a.p.tiles;
-    const int group = blockIdx.x / (tiles + 1), tile = blockIdx.x - group * (tiles + 1);
+    extern __shared__ __align__(16) float rows[];   // [kRows][width]
+    const int tiles = a.p.tiles, at_block = xcd_run(blockIdx.x, gridDim.x), threads = blockDim.x;
+    const int group = at_block / tiles, tile = at_block - group * tiles;
     const int f0 = group * kRows, nf = min(kRows, a.features - f0);
-    if (tile == tiles) {
-        if (!a.out_blocks) return;
-        const int lane = threadIdx.x & (kWave - 1);
-        for (int e = wave_in_block(); e < a.experts; e += kMoveThreads / kWave) {
-            const int n = min(max(a.p.filled[e], 0), a.capacity);
-            float *block = a.out_blocks + (static_cast<int64_t>(e) * a.features + f0) * a.ldb;
-            for (int r = 0; r < nf; ++r, block += a.ldb)
-                for (int p = n + lane; p < a.capacity; p += kWave) block[p] = 0.f;
-        }
-        return;
-    }
-    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0), width = min(kPlaceTile, a.batch);
-    const float *in = a.columns + static_cast<int64_t>(f0) * a.ldc + c0;
-    for (int r = 0; r < nf; ++r, in += a.ldc)
-        for (int c = threadIdx.x; c < here; c += kMoveThreads) rows[r * width + c] = in[c];
+    if (nf <= 0) return;
+    const int c0 = tile * a.p.tile, here = min(a.p.tile, a.batch - c0), width = pitch_of(a.batch, a.p.tile);
+    stage_rows(rows, width, a.columns + static_cast<int64_t>(f0) * a.ldc + c0, a.ldc, nf, here);
     __syncthreads();
     const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
-    const int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
-    float *partial = kGrad ? a.partial + static_cast<int64_t>(group) * a.batch * a.k + static_cast<int64_t>(tile) * kPlaceTile * a.k : nullptr;
-    for (int i = threadIdx.x; i < kept; i += kMoveThreads) {
-        const Entry t = entry_of(list[i]);
-        if (!inside(t, a, here)) continue;
-        const int64_t at = (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
-        float *out = a.out_blocks + at;
-        if constexpr (kGrad) {
-            const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
-            const float *y = a.blocks + at;
-            float dot = 0.f;
+    const int2 *list = a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k;
+    float *partial = kGrad ? a.partial + static_cast<int64_t>(group) * a.batch * a.k + static_cast<int64_t>(tile) * a.p.tile * a.k : nullptr;
+    auto move = [&](auto whole) {
+        const int n = whole.value ? kRows : nf;   // (without a bound inside, a whole group's loads are all in flight at once)
+        for (int i = threadIdx.x; i < kept; i += threads) {
+            const Entry t = entry_of(list[i]);
+            if (!inside(t, a, here)) continue;
+            const int64_t at = (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
+            float *out = a.out_blocks + at;
+            if constexpr (kGrad) {
+                const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
+                if (a.dweights) {
+                    const float *y = a.blocks + at;
+                    float dot = 0.f;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                if (r >= nf) break;
-                const float d = rows[r * width + t.column];
-                if (a.dweights) dot = fmaf(y[r * a.ldb], d, dot);
-                if (a.out_blocks) out[r * a.ldb] = w * d;
-            }
-            if (a.dweights) partial[i] = dot;
-        } else {
+                    for (int r = 0; r < n; ++r) dot = fmaf(y[r * a.ldb], rows[r * width + t.column], dot);
+                    partial[i] = dot;
+                }
+                if (!a.out_blocks) continue;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                if (r >= nf) break;
-                out[r * a.ldb] = rows[r * width + t.column];
+                for (int r = 0; r < n; ++r) out[r * a.ldb] = w * rows[r * width + t.column];
+            } else {
+#pragma unroll
+                for (int r = 0; r < n; ++r) out[r * a.ldb] = rows[r * width + t.column];
             }
+        }
+    };
+    if (nf == kRows) move(std::true_type{});
+    else move(std::false_type{});
+    if (!a.out_blocks) return;
+    const int lane = threadIdx.x & (kWave - 1), waves = threads / kWave;
+    const int share = (a.experts + tiles - 1) / tiles, end = min(a.experts, (tile + 1) * share);
+    for (int e0 = tile * share + wave_in_block(); e0 < end; e0 += waves * kWave) {
+        // lane l knows how full block e0 + l * waves is
+        const int filled = min(max(a.p.filled[min(e0 + lane * waves, a.experts - 1)], 0), a.capacity);
+        for (int l = 0; l < kWave && e0 + l * waves < end; ++l) {
+            float *block = a.out_blocks + (static_cast<int64_t>(e0 + l * waves) * a.features + f0) * a.ldb;
+            for (int p = __builtin_amdgcn_readlane(filled, l) + lane; p < a.capacity; p += kWave)
+                for (int r = 0; r < nf; ++r) block[r * a.ldb + p] = 0.f;
         }
     }
 }
 
-// gradients of the weights from the products of every group of rows, added up in the order of the rows
-__global__ __launch_bounds__(256) void weight_gradient_kernel(const ExchangeArgs a, const int groups)
+// Gradients of the weights from the products of every group of rows: a wave adds up every kGradWaves-th group for 64 entries, and
+// the waves' sums are added in their order.
+constexpr int kGradWaves = 8;
+__global__ __launch_bounds__(kGradWaves * kWave) void weight_gradient_kernel(const ExchangeArgs a, const int groups)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, total = static_cast<int64_t>(a.batch) * a.k;
-    if (i >= total) return;
-    const int tile = static_cast<int>(i / (static_cast<int64_t>(kPlaceTile) * a.k));
-    const int64_t from = static_cast<int64_t>(tile) * kPlaceTile * a.k;
-    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0);
+    __shared__ double sums[kGradWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int64_t total = static_cast<int64_t>(a.batch) * a.k, i = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    const int tile = static_cast<int>(min(i, total - 1) / (static_cast<int64_t>(a.p.tile) * a.k));
+    const int64_t from = static_cast<int64_t>(tile) * a.p.tile * a.k;
+    double sum = 0.0;   // (hundreds of sums, each read once: 64 bits cost nothing)
+    if (i < total && i - from < a.p.listed[tile]) {
+        const float *p = a.partial + i;
+        int g = wv;
+        for (; g + 3 * kGradWaves < groups; g += 4 * kGradWaves) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = p[(g + u * kGradWaves) * total];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) sum += v[u];
+        }
+        for (; g < groups; g += kGradWaves) sum += p[g * total];
+    }
+    sums[wv][lane] = sum;
+    __syncthreads();
+    if (wv > 0 || i >= total) return;
+#pragma unroll
+    for (int w = 1; w < kGradWaves; ++w) sum += sums[w][lane];
+    const int c0 = tile * a.p.tile, here = min(a.p.tile, a.batch - c0);
     const Entry t = entry_of(a.p.lists[i]);
     if (t.column >= here || t.choice >= a.k) return;
-    double sum = 0.0;   // (hundreds of sums, each read once: 64 bits cost nothing)
-    if (i - from < a.p.listed[tile])
-        for (int g = 0; g < groups; ++g) sum += a.partial[g * total + i];
     a.dweights[t.choice * a.ldk + c0 + t.column] = static_cast<float>(sum);
 }
 
-// Blocks to columns, Y = sum of the kept choices' results times their weights.  A wave keeps kRows rows of one tile's columns in
-// LDS, for itself alone, and adds the tile's list to them, entry by entry: reads of the blocks are as wide as the list's runs.
-constexpr int kCombineWaves = 4;
-template <int kRows>
-__global__ __launch_bounds__(kCombineWaves * kWave) void combine_kernel(const ExchangeArgs a)
+// Blocks to columns, Y = sum of the kept choices' results times their weights, in the order of the list.  A wave keeps the sums of
+// kCombineRows rows and one tile's columns in LDS, for itself alone, so that nothing waits for other waves, and adds 64 entries of the
+// list to them at a time: read, add, write, for the first entry of every column, then for the second ones, as the turns say.
+// (LDS additions as atomics would need no turns, but take about 176 cycles for 64 lanes: 600 us for 4096 features, 8192 columns and four
+// choices of 64 experts, where this takes 160, 5.0 TB/s, and 177 with weights.)
+constexpr size_t kCombineLds = 160 * 1024;
+constexpr int64_t kCombineWavesWanted = 1024;
+constexpr int kCombineUnroll = 4;    // list entries per lane and iteration; those of the next one are on their way
+enum Weights { kNone, kGathered, kStaged };
+template <int kRows, int kWaves, Weights kWeights>
+__global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeArgs a)
 {
-    extern __shared__ float rows[];   // [waves][kRows][width]
+    constexpr int U = kCombineUnroll;
+    extern __shared__ __align__(16) float rows[];   // [waves][kRows][width], then with kStaged the weights [k][width]
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
-    const int tiles = a.p.tiles;
-    const int group = blockIdx.x / tiles, tile = blockIdx.x - group * tiles;
-    const int f0 = (group * kCombineWaves + wv) * kRows, nf = min(kRows, a.features - f0);
-    if (nf <= 0) return;              // (no barrier below: waves share nothing)
-    const int c0 = tile * kPlaceTile, here = min(kPlaceTile, a.batch - c0), width = min(kPlaceTile, a.batch);
+    const int tiles = a.p.tiles, at_block = xcd_run(blockIdx.x, gridDim.x);
+    const int group = at_block / tiles, tile = at_block - group * tiles;
+    if (group * kWaves * kRows >= a.features) return;
+    const int f0 = (group * kWaves + wv) * kRows, nf = min(kRows, a.features - f0);
+    const int c0 = tile * a.p.tile, here = min(a.p.tile, a.batch - c0), width = pitch_of(a.batch, a.p.tile);
+    const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
+    const int2 *__restrict__ list = a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k;
+    const float *__restrict__ weights = a.weights + c0;
+    float *staged = rows + kWaves * kRows * width;
+    if constexpr (kWeights == kStaged) {
+        stage_rows(staged, width, weights, a.ldk, a.k, here);
+        __syncthreads();
+    }
+    if (nf <= 0) return;              // (no barrier from here on: waves share nothing that is written)
     float *sum = rows + wv * kRows * width;
     for (int i = lane; i < kRows * width; i += kWave) sum[i] = 0.f;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
-    const int2 *list = a.p.lists + static_cast<int64_t>(tile) * kPlaceTile * a.k;
-    for (int i = lane; i < kept; i += kWave) {
-        const Entry t = entry_of(list[i]);
-        if (!inside(t, a, here)) continue;
-        const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
-        const float *y = a.blocks + (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
-        float v[kRows];
+    const int64_t block = a.features * a.ldb, last_row = (nf - 1) * a.ldb;
+    const float *__restrict__ first = a.blocks + f0 * a.ldb;
+    // Entries are read one iteration before their values, and those one before they are added.  All reads are made, at a place of their own or
+    // a valid one, so that none waits for a branch.
+    struct Values {
+        float w[U], v[U][kRows];
+        int column[U], turn[U];   // (turn -1: no entry)
+    };
+    int2 entry[U];
+    auto fetch_entries = [&](int i) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) v[r] = r < nf ? y[r * a.ldb] : 0.f;
+        for (int u = 0; u < U; ++u) entry[u] = list[min(i + u * kWave + lane, total - 1)];
+    };
+    auto fetch_values = [&](int i) {
+        Values x;
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            __hip_atomic_fetch_add(&sum[r * width + t.column], w * v[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        for (int u = 0; u < U; ++u) {
+            const Entry t = entry_of(entry[u]);
+            const bool on = i + u * kWave + lane < kept && inside(t, a, here);
+            x.column[u] = t.column;
+            x.turn[u] = on ? t.turn : -1;
+            const float *y = first + (on ? t.expert * block + t.place : 0);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) x.v[u][r] = y[min(r * a.ldb, last_row)];
+            if constexpr (kWeights == kGathered) x.w[u] = weights[on ? t.choice * a.ldk + t.column : 0];
+            else if constexpr (kWeights == kStaged) x.w[u] = staged[on ? t.choice * width + t.column : 0];
+            else x.w[u] = 1.f;
+        }
+        return x;
+    };
+    fetch_entries(0);
+    Values now = fetch_values(0);
+    fetch_entries(U * kWave);
+    for (int i = 0; i < kept; i += U * kWave) {
+        const Values next = fetch_values(i + U * kWave);
+        fetch_entries(i + 2 * U * kWave);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            int m = 0;
+            do {
+                if (now.turn[u] == m) {
+                    float *s = sum + now.column[u];
+                    float x[kRows];
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) x[r] = s[r * width];
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) s[r * width] = x[r] + __fmul_rn(now.w[u], now.v[u][r]);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                ++m;
+            } while (__ballot(now.turn[u] >= m));
+        }
+        now = next;
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    float *out = a.out_columns + static_cast<int64_t>(f0) * a.ldc + c0;
+    float *out = a.out_columns + f0 * a.ldc + c0;
     for (int r = 0; r < nf; ++r, out += a.ldc)
         for (int c = lane; c < here; c += kWave) out[c] = sum[r * width + c];
 }
 
+uint32_t whole_eights(int64_t blocks) { return static_cast<uint32_t>((blocks + 7) / 8 * 8); }
+
 template <int kRows, bool kGrad>
 hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
 {
-    const int groups = (a.features + kRows - 1) / kRows, width = a.batch < kPlaceTile ? a.batch : kPlaceTile;
-    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(static_cast<uint32_t>(groups) * (a.p.tiles + 1)), dim3(kMoveThreads), kRows * width * sizeof(float), s, a);
+    const int groups = (a.features + kRows - 1) / kRows, width = pitch_of(a.batch, a.p.tile);
+    const int share = (a.experts + a.p.tiles - 1) / a.p.tiles;   // of the experts, cleared one per wave
+    int threads = (width * a.k > 16 * share ? width * a.k : 16 * share);
+    threads = (threads + kWave - 1) / kWave * kWave;
+    threads = threads < 512 ? 512 : threads > kMoveThreads ? kMoveThreads : threads;
+    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), dim3(threads),
+                       kRows * width * sizeof(float), s, a);
     return hipGetLastError();
 }
 
@@ -655,27 +807,49 @@ hipError_t launch_place(const PlaceArgs &a, hipStream_t s)
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL(place_kernel, dim3(a.p.subs), dim3(kPlaceThreads), kPlaceWaves * (a.experts + 1) * sizeof(int32_t), s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.p.tile == kPlaceSub) return e;
+    const int blocks = (a.p.tile * a.k + kPlaceThreads - 1) / kPlaceThreads;
+    hipLaunchKernelGGL(place_turns_kernel, dim3(static_cast<uint32_t>(a.p.tiles) * blocks), dim3(kPlaceThreads), 0, s, a, blocks);
     return hipGetLastError();
 }
 
-hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s) { return dispatch_go<16, false>(a, s); }
+hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s)
+{
+    // All that the work-groups of one XCD write at a time should stay in its L2 until the neighbouring tile has filled the lines up.
+    int most = 16;
+    while (most > 4 && most * a.p.tile * a.k > 8192) most /= 2;
+    const int rows = move_rows(a.features, a.p.tiles, most);
+    return rows == 16 ? dispatch_go<16, false>(a, s) : rows == 8 ? dispatch_go<8, false>(a, s) : dispatch_go<4, false>(a, s);
+}
+
+template <int kRows, int kWaves>
+static hipError_t combine_go(const ExchangeArgs &a, hipStream_t s)
+{
+    constexpr int per_block = kRows * kWaves;
+    const int groups = (a.features + per_block - 1) / per_block, width = pitch_of(a.batch, a.p.tile);
+    const dim3 grid(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), block(kWaves * kWave);
+    const size_t lds = per_block * width * sizeof(float), with_weights = lds + static_cast<size_t>(width) * a.k * sizeof(float);
+    if (!a.weights) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kNone>), grid, block, lds, s, a);
+    else if (with_weights <= kCombineLds) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kStaged>), grid, block, with_weights, s, a);
+    else hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kGathered>), grid, block, lds, s, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s)
 {
-    constexpr int kRows = 2;
-    const int groups = (a.features + kRows * kCombineWaves - 1) / (kRows * kCombineWaves), width = a.batch < kPlaceTile ? a.batch : kPlaceTile;
-    hipLaunchKernelGGL(combine_kernel<kRows>, dim3(static_cast<uint32_t>(groups) * a.p.tiles), dim3(kCombineWaves * kWave),
-                       kCombineWaves * kRows * width * sizeof(float), s, a);
-    return hipGetLastError();
+    auto waves = [&](int rows) { return static_cast<int64_t>((a.features + rows - 1) / rows) * a.p.tiles; };
+    if (waves(4) < kCombineWavesWanted) return waves(2) < kCombineWavesWanted ? combine_go<1, 4>(a, s) : combine_go<2, 4>(a, s);
+    return a.p.tile * a.k > 4096 ? combine_go<4, 8>(a, s) : combine_go<4, 4>(a, s);
 }
 
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s)
 {
-    static_assert(kPartialRows == 16, "rows of one work-group");
-    hipError_t e = dispatch_go<kPartialRows, true>(a, s);
+    const int rows = partial_rows(a.features, a.batch);
+    const hipError_t e = rows == 16 ? dispatch_go<16, true>(a, s) : rows == 8 ? dispatch_go<8, true>(a, s) : dispatch_go<4, true>(a, s);
     if (e != hipSuccess || !a.dweights) return e;
     const int64_t total = static_cast<int64_t>(a.batch) * a.k;
-    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + 255) / 256)), dim3(256), 0, s, a, (a.features + kPartialRows - 1) / kPartialRows);
+    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + kWave - 1) / kWave)), dim3(kGradWaves * kWave), 0, s, a, (a.features + rows - 1) / rows);
     return hipGetLastError();
 }
 
