@@ -2027,13 +2027,15 @@ static int check_list(int32_t n, const void *values, const void *velocities, con
 {
     if (n < 0) return fail(NERVA_ERR_ARGUMENT, "n is negative");
     if (n > 0 && (!grads || !counts || (update && (!values || !velocities)))) return fail(NERVA_ERR_ARGUMENT, "null list");
+    int64_t total = 0;
     for (int32_t t = 0; t < n; ++t) {
         if (counts[t] < 0) return fail(NERVA_ERR_ARGUMENT, "array %d has a negative length", t);
         if (counts[t] == 0) continue;
         if (!grads[t]) return fail(NERVA_ERR_ARGUMENT, "gradient %d is null", t);
         if (values && !static_cast<float *const *>(values)[t]) return fail(NERVA_ERR_ARGUMENT, "array %d is null", t);
         if (velocities && !static_cast<float *const *>(velocities)[t]) return fail(NERVA_ERR_ARGUMENT, "velocity %d is null", t);
-        if (counts[t] > INT64_C(1) << 40) return fail(NERVA_ERR_SHAPE, "array %d has %lld entries, more than 2^40", t, (long long)counts[t]);
+        if (counts[t] > (INT64_C(1) << 40) - total) return fail(NERVA_ERR_SHAPE, "more than 2^40 entries up to array %d of %lld", t, (long long)counts[t]);
+        total += counts[t];
     }
     if (!workspace) return fail(NERVA_ERR_ARGUMENT, "workspace is null");
     if (reinterpret_cast<uintptr_t>(workspace) % 8) return fail(NERVA_ERR_WORKSPACE, "workspace must be 8-byte aligned");

@@ -14,46 +14,52 @@
 namespace nerva {
 namespace {
 
+// The arrays are cut into short chunks, and work-groups, as many as the GPU holds, take chunk after chunk, so that all of them together
+// read one stretch of memory at a time.  (A long stretch for each work-group instead, all of the same length, keeps meeting in few
+// memory channels: the norm and step of 134 M entries took 727 us that way, 600 so.)
 constexpr int kClipThreads = 256;
 constexpr int kClipWaves = kClipThreads / kWave;
-constexpr int kNormThreads = 1024;
-constexpr int kListMax = 64;                       // arrays per launch: they travel in the kernel's arguments
-constexpr int64_t kChunkMin = 4 * kNormThreads;    // entries per work-group, at least
-constexpr int32_t kApplyBlocks = 4096;
-constexpr int64_t kApplyChunkMin = 4 * kClipThreads;
+constexpr int kNormThreads = 512;
+constexpr int kNormLoads = 4;                      // 16-byte reads in flight per thread
+constexpr int kNormChunk = 4 * kNormLoads * kNormThreads;
+constexpr int kApplyLoads = 4;
+constexpr int kApplyChunk = 4 * kApplyLoads * kClipThreads;
+constexpr int kApplyBlocks = 2048;
+constexpr int kPartialMost = 2048;                 // more partial sums are first added up by a launch of their own
+// Arrays per launch: they travel in the kernel's arguments, of which there may be 4 KiB.
+constexpr int kApplyList = 104;
 
 struct NormList {
-    const float *grads[kListMax];
-    int64_t counts[kListMax];
-    int32_t first[kListMax + 1];                   // work-group that an array starts with
+    const float *grads[kNormList];
+    int64_t counts[kNormList];
+    int32_t first[kNormList + 1];                  // chunk that an array starts with, and one past the last
     int32_t n;
-    int64_t chunk;                                 // entries per work-group, a multiple of 4
     double *partial;                               // of this launch
 };
 
 struct ApplyList {
-    float *a[kListMax];                            // weights, or scaled gradients
-    float *v[kListMax];
-    const float *grads[kListMax];
-    int64_t counts[kListMax];
-    int32_t first[kListMax + 1];
+    float *a[kApplyList];                          // weights, or scaled gradients
+    float *v[kApplyList];
+    const float *grads[kApplyList];
+    int64_t counts[kApplyList];
+    int32_t first[kApplyList + 1];
     int32_t n;
-    int64_t chunk;
     const double *partial;
     int32_t n_partial;
     float lr, momentum, max_norm;
     int32_t nesterov;
     float *norm_out;
 };
+static_assert(sizeof(NormList) <= 4096 && sizeof(ApplyList) <= 4096, "kernel arguments");
 
-// array that a work-group works on: the last whose first work-group is not behind it
+// array of a chunk: the last that does not start behind it
 template <typename List>
-__device__ __forceinline__ int array_of(const List &l, int block)
+__device__ __forceinline__ int array_of(const List &l, int chunk)
 {
     int lo = 0, hi = l.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (l.first[mid] <= block) lo = mid;
+        if (l.first[mid] <= chunk) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -82,99 +88,137 @@ __device__ __forceinline__ double add_squares(double s, float4 g)
 __global__ __launch_bounds__(kNormThreads) void norm_partial_kernel(const NormList l)
 {
     __shared__ double lds[kNormThreads / kWave];
-    const int t = array_of(l, blockIdx.x);
-    const int64_t from = (blockIdx.x - l.first[t]) * l.chunk;
-    const int64_t left = l.counts[t] - from;
-    const int64_t n = left < l.chunk ? left : l.chunk;
-    const float *g = l.grads[t] + from;
-    double s0 = 0, s1 = 0;
-    int64_t i = 4 * static_cast<int64_t>(threadIdx.x);
-    constexpr int64_t kStep = 4 * kNormThreads;
-    for (; i + 3 * kStep + 3 < n; i += 4 * kStep) {
-        const float4 a = ld4(g + i), b = ld4(g + i + kStep), c = ld4(g + i + 2 * kStep), d = ld4(g + i + 3 * kStep);
-        s0 = add_squares(s0, a);
-        s1 = add_squares(s1, b);
-        s0 = add_squares(s0, c);
-        s1 = add_squares(s1, d);
+    double s[2] = {0, 0};
+    for (int back = blockIdx.x; back < l.first[l.n]; back += gridDim.x) {
+        const int chunk = l.first[l.n] - 1 - back, t = array_of(l, chunk);   // (from the last one on: see kCacheBytes)
+        const int64_t from = static_cast<int64_t>(chunk - l.first[t]) * kNormChunk;
+        const int n = static_cast<int>(min(l.counts[t] - from, static_cast<int64_t>(kNormChunk)));
+        const float *g = l.grads[t] + from;
+        int i = 4 * threadIdx.x;
+        if (n == kNormChunk) {
+            float4 x[kNormLoads];
+#pragma unroll
+            for (int u = 0; u < kNormLoads; ++u) x[u] = ld4(g + i + u * 4 * kNormThreads);
+#pragma unroll
+            for (int u = 0; u < kNormLoads; ++u) s[u & 1] = add_squares(s[u & 1], x[u]);
+        } else {
+            for (; i + 3 < n; i += 4 * kNormThreads) s[0] = add_squares(s[0], ld4(g + i));
+            for (; i < n; ++i) s[1] = fma(static_cast<double>(g[i]), static_cast<double>(g[i]), s[1]);   // (the array's last one to three: one thread has them)
+        }
     }
-    for (; i + 3 < n; i += kStep) s0 = add_squares(s0, ld4(g + i));
-    for (; i < n; ++i) s1 = fma(static_cast<double>(g[i]), static_cast<double>(g[i]), s1);   // (the array's last one to three entries: one thread has them)
-    s0 = block_sum(s0 + s1, lds, kNormThreads / kWave);
-    if (threadIdx.x == 0) l.partial[blockIdx.x] = s0;
+    const double sum = block_sum(s[0] + s[1], lds, kNormThreads / kWave);
+    if (threadIdx.x == 0) l.partial[blockIdx.x] = sum;
 }
 
-// The norm from the partial sums, the same bits in every work-group.
-__device__ __forceinline__ double norm_of(const double *partial, int n, double *lds)
+// the partial sums' sum, the same bits in every work-group
+__device__ __forceinline__ double sum_of(const double *partial, int n, double *lds)
 {
     double s = 0;
     for (int i = threadIdx.x; i < n; i += kClipThreads) s += partial[i];
-    return sqrt(block_sum(s, lds, kClipWaves));
+    return block_sum(s, lds, kClipWaves);
 }
 
-__global__ __launch_bounds__(kClipThreads) void norm_finish_kernel(const double *partial, int n, float *norm_out)
+__global__ __launch_bounds__(kClipThreads) void norm_finish_kernel(const double *partial, int n, double *sum_out, float *norm_out)
 {
     __shared__ double lds[kClipWaves];
-    const double norm = norm_of(partial, n, lds);
-    if (threadIdx.x == 0) *norm_out = static_cast<float>(norm);
+    const double sum = sum_of(partial, n, lds);
+    if (threadIdx.x != 0) return;
+    if (sum_out) *sum_out = sum;
+    if (norm_out) *norm_out = static_cast<float>(sqrt(sum));
 }
 
-template <bool kUpdate>
+__device__ __forceinline__ void step4(float4 &w, float4 &v, float4 g, float c, const ApplyList &l)
+{
+    momentum_step(w.x, v.x, c * g.x, l.lr, l.momentum, l.nesterov);
+    momentum_step(w.y, v.y, c * g.y, l.lr, l.momentum, l.nesterov);
+    momentum_step(w.z, v.z, c * g.z, l.lr, l.momentum, l.nesterov);
+    momentum_step(w.w, v.w, c * g.w, l.lr, l.momentum, l.nesterov);
+}
+
+// Of arrays that the 256 MiB of Infinity Cache cannot hold, weights and momentum buffers go past it, and the norm is taken from the last array to
+// the first, so that the step, which goes forward, still finds the gradients there that were read last: 134 M entries 642 us -> 554
+// (forward and past the cache 579, backward alone 639).  Smaller ones may still be there from the step before, and
+// past the cache 4.4 M entries take 24.3 us instead of 22.5.
+constexpr int64_t kCacheBytes = 256ll << 20;
+template <bool kPast>
+__device__ __forceinline__ float4 load4(const float *p)
+{
+    if constexpr (!kPast) return ld4(p);
+    const v4f_any x = __builtin_nontemporal_load(reinterpret_cast<const v4f_any *>(p));
+    return make_float4(x.x, x.y, x.z, x.w);
+}
+template <bool kPast>
+__device__ __forceinline__ void store4(float *p, float4 v)
+{
+    if constexpr (!kPast) return st4(p, v);
+    const v4f_any x = {v.x, v.y, v.z, v.w};
+    __builtin_nontemporal_store(x, reinterpret_cast<v4f_any *>(p));
+}
+
+template <bool kUpdate, bool kPast>
 __global__ __launch_bounds__(kClipThreads) void clip_apply_kernel(const ApplyList l)
 {
     __shared__ double lds[kClipWaves];
-    const double norm = norm_of(l.partial, l.n_partial, lds);
+    const double norm = sqrt(sum_of(l.partial, l.n_partial, lds));
     const float norm32 = static_cast<float>(norm);
     if (blockIdx.x == 0 && threadIdx.x == 0 && l.norm_out) *l.norm_out = norm32;
     if (!(norm32 <= 3.402823466e38f)) return;   // no factor makes such gradients finite: nothing is changed
     const float c = norm > l.max_norm ? static_cast<float>(l.max_norm / norm) : 1.f;
+    auto times = [c](float4 x) { return make_float4(c * x.x, c * x.y, c * x.z, c * x.w); };
 
-    const int t = array_of(l, blockIdx.x);
-    const int64_t from = (blockIdx.x - l.first[t]) * l.chunk;
-    const int64_t left = l.counts[t] - from;
-    const int64_t n = left < l.chunk ? left : l.chunk;
-    const float *g = l.grads[t] + from;
-    float *a = l.a[t] + from;
-    constexpr int64_t kStep = 4 * kClipThreads;
-    int64_t i = 4 * static_cast<int64_t>(threadIdx.x);
-    if constexpr (kUpdate) {
-        float *v = l.v[t] + from;
+    for (int chunk = blockIdx.x; chunk < l.first[l.n]; chunk += gridDim.x) {
+        const int t = array_of(l, chunk);
+        const int64_t from = static_cast<int64_t>(chunk - l.first[t]) * kApplyChunk;
+        const int n = static_cast<int>(min(l.counts[t] - from, static_cast<int64_t>(kApplyChunk)));
+        const float *g = l.grads[t] + from;
+        float *a = l.a[t] + from;
+        float *v = kUpdate ? l.v[t] + from : nullptr;
+        if (!kUpdate && c == 1.f && a == g) continue;
+        int i = 4 * threadIdx.x;
+        constexpr int kStep = 4 * kClipThreads;
+        if (n == kApplyChunk) {
+            float4 ww[kApplyLoads], vv[kApplyLoads], gg[kApplyLoads];
+#pragma unroll
+            for (int u = 0; u < kApplyLoads; ++u) {
+                gg[u] = ld4(g + i + u * kStep);
+                if constexpr (kUpdate) {
+                    ww[u] = load4<kPast>(a + i + u * kStep);
+                    vv[u] = load4<kPast>(v + i + u * kStep);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kApplyLoads; ++u) {
+                if constexpr (kUpdate) {
+                    step4(ww[u], vv[u], gg[u], c, l);
+                    store4<kPast>(v + i + u * kStep, vv[u]);
+                    store4<kPast>(a + i + u * kStep, ww[u]);
+                } else {
+                    st4(a + i + u * kStep, times(gg[u]));
+                }
+            }
+            continue;
+        }
         for (; i + 3 < n; i += kStep) {
-            float4 ww = ld4(a + i), vv = ld4(v + i);
-            const float4 gg = ld4(g + i);
-            momentum_step(ww.x, vv.x, c * gg.x, l.lr, l.momentum, l.nesterov);
-            momentum_step(ww.y, vv.y, c * gg.y, l.lr, l.momentum, l.nesterov);
-            momentum_step(ww.z, vv.z, c * gg.z, l.lr, l.momentum, l.nesterov);
-            momentum_step(ww.w, vv.w, c * gg.w, l.lr, l.momentum, l.nesterov);
-            st4(v + i, vv);
-            st4(a + i, ww);
+            if constexpr (kUpdate) {
+                float4 ww = ld4(a + i), vv = ld4(v + i);
+                step4(ww, vv, ld4(g + i), c, l);
+                st4(v + i, vv);
+                st4(a + i, ww);
+            } else {
+                st4(a + i, times(ld4(g + i)));
+            }
         }
-        for (; i < n; ++i) {
-            float ww = a[i], vv = v[i];
-            momentum_step(ww, vv, c * g[i], l.lr, l.momentum, l.nesterov);
-            v[i] = vv;
-            a[i] = ww;
+        for (; i < n; ++i) {   // (the array's last one to three: one thread has them)
+            if constexpr (kUpdate) {
+                float ww = a[i], vv = v[i];
+                momentum_step(ww, vv, c * g[i], l.lr, l.momentum, l.nesterov);
+                v[i] = vv;
+                a[i] = ww;
+            } else {
+                a[i] = c * g[i];
+            }
         }
-    } else {
-        if (c == 1.f && a == g) return;
-        for (; i + 3 < n; i += kStep) {
-            float4 gg = ld4(g + i);
-            gg.x *= c;
-            gg.y *= c;
-            gg.z *= c;
-            gg.w *= c;
-            st4(a + i, gg);
-        }
-        for (; i < n; ++i) a[i] = c * g[i];
     }
-}
-
-// entries per work-group: at most `blocks` of them and one more for each array
-int64_t chunk_of(const ArrayList &l, int32_t blocks, int64_t least)
-{
-    int64_t total = 0;
-    for (int32_t t = 0; t < l.n; ++t) total += l.counts[t];
-    const int64_t even = (total + blocks - 1) / blocks;
-    return even <= least ? least : (even + 3) / 4 * 4;
 }
 
 // whether arrays [a, a + n) and [b, b + m) share an entry
@@ -182,30 +226,38 @@ bool overlap(const float *a, int64_t n, const float *b, int64_t m) { return a < 
 
 }  // namespace
 
-// partial sums of all arrays; returns how many there are in *n_partial
-static hipError_t launch_partial(const ArrayList &l, double *partial, int32_t *n_partial, hipStream_t s)
+// Partial sums of all arrays; *n_partial receives how many there are, at most kPartialMost, from *partial on.
+static hipError_t launch_partial(const ArrayList &l, double **partial, int32_t *n_partial, hipStream_t s)
 {
-    const int64_t chunk = chunk_of(l, kNormBlocks, kChunkMin);
     int32_t done = 0;
-    for (int32_t t = 0; t < l.n;) {
+    for (int32_t end = l.n; end > 0;) {   // stretches of the list, the last one first
+        const int32_t from = end > kNormList ? end - kNormList : 0;
         NormList a;
         a.n = 0;
-        int32_t blocks = 0;
-        for (; t < l.n && a.n < kListMax; ++t) {
+        int64_t chunks = 0;
+        for (int32_t t = from; t < end; ++t) {
             if (l.counts[t] == 0) continue;
             a.grads[a.n] = l.grads[t];
             a.counts[a.n] = l.counts[t];
-            a.first[a.n++] = blocks;
-            blocks += static_cast<int32_t>((l.counts[t] + chunk - 1) / chunk);
+            a.first[a.n++] = static_cast<int32_t>(chunks);
+            chunks += (l.counts[t] + kNormChunk - 1) / kNormChunk;
         }
-        if (blocks == 0) break;
-        a.first[a.n] = blocks;
-        a.chunk = chunk;
-        a.partial = partial + done;
+        end = from;
+        if (chunks == 0) continue;
+        a.first[a.n] = static_cast<int32_t>(chunks);
+        a.partial = *partial + done;
+        const int blocks = static_cast<int>(chunks < kNormBlocks ? chunks : kNormBlocks);
         hipLaunchKernelGGL(norm_partial_kernel, dim3(blocks), dim3(kNormThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         done += blocks;
+    }
+    if (done > kPartialMost) {
+        hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kClipThreads), 0, s, *partial, done, *partial + done, static_cast<float *>(nullptr));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        *partial += done;
+        done = 1;
     }
     *n_partial = done;
     return hipSuccess;
@@ -214,31 +266,34 @@ static hipError_t launch_partial(const ArrayList &l, double *partial, int32_t *n
 static hipError_t launch_finish(const double *partial, int32_t n, float *norm_out, hipStream_t s)
 {
     if (!norm_out) return hipSuccess;
-    hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kClipThreads), 0, s, partial, n, norm_out);
+    hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kClipThreads), 0, s, partial, n, static_cast<double *>(nullptr), norm_out);
     return hipGetLastError();
 }
 
 hipError_t launch_norm(const ArrayList &l, double *partial, float *norm_out, hipStream_t s)
 {
     int32_t n = 0;
-    const hipError_t e = launch_partial(l, partial, &n, s);
+    const hipError_t e = launch_partial(l, &partial, &n, s);
     return e != hipSuccess ? e : launch_finish(partial, n, norm_out, s);
 }
 
 hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
 {
     int32_t n_partial = 0;
-    hipError_t e = launch_partial(l, c.partial, &n_partial, s);
+    double *partial = c.partial;
+    hipError_t e = launch_partial(l, &partial, &n_partial, s);
     if (e != hipSuccess) return e;
-    if (n_partial == 0) return launch_finish(c.partial, 0, c.norm_out, s);
+    if (n_partial == 0) return launch_finish(partial, 0, c.norm_out, s);
     float *const *out = l.values ? l.values : l.clipped;
-    const int64_t chunk = chunk_of(l, kApplyBlocks, kApplyChunkMin);
     float *norm_out = c.norm_out;
+    int64_t entries = 0;
+    for (int32_t t = 0; t < l.n; ++t) entries += l.counts[t];
+    const bool past = 20 * entries > kCacheBytes;
     for (int32_t t = 0; t < l.n;) {
         ApplyList a;
         a.n = 0;
-        int32_t blocks = 0;
-        for (; t < l.n && a.n < kListMax; ++t) {
+        int64_t chunks = 0;
+        for (; t < l.n && a.n < kApplyList; ++t) {
             const int64_t m = l.counts[t];
             if (m == 0) continue;
             // an array that is in the list twice is stepped twice, one launch after the other
@@ -250,13 +305,12 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
             a.v[a.n] = l.values ? l.velocities[t] : nullptr;
             a.grads[a.n] = l.grads[t];
             a.counts[a.n] = m;
-            a.first[a.n++] = blocks;
-            blocks += static_cast<int32_t>((m + chunk - 1) / chunk);
+            a.first[a.n++] = static_cast<int32_t>(chunks);
+            chunks += (m + kApplyChunk - 1) / kApplyChunk;
         }
-        if (blocks == 0) break;
-        a.first[a.n] = blocks;
-        a.chunk = chunk;
-        a.partial = c.partial;
+        if (chunks == 0) break;
+        a.first[a.n] = static_cast<int32_t>(chunks);
+        a.partial = partial;
         a.n_partial = n_partial;
         a.lr = c.lr;
         a.momentum = c.momentum;
@@ -264,8 +318,10 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
         a.nesterov = c.nesterov;
         a.norm_out = norm_out;
         norm_out = nullptr;
-        if (l.values) hipLaunchKernelGGL((clip_apply_kernel<true>), dim3(blocks), dim3(kClipThreads), 0, s, a);
-        else hipLaunchKernelGGL((clip_apply_kernel<false>), dim3(blocks), dim3(kClipThreads), 0, s, a);
+        const dim3 grid(static_cast<uint32_t>(chunks < kApplyBlocks ? chunks : kApplyBlocks));
+        if (l.values && past) hipLaunchKernelGGL((clip_apply_kernel<true, true>), grid, dim3(kClipThreads), 0, s, a);
+        else if (l.values) hipLaunchKernelGGL((clip_apply_kernel<true, false>), grid, dim3(kClipThreads), 0, s, a);
+        else hipLaunchKernelGGL((clip_apply_kernel<false, false>), grid, dim3(kClipThreads), 0, s, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

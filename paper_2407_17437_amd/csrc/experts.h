@@ -111,8 +111,9 @@ hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s);
 
 // ---- norm over many arrays (clip.hip) -------------------------------------------------------
-constexpr int32_t kNormBlocks = 512;         // work-groups that the arrays are shared out to, and one more for each array
-inline int64_t norm_workspace_bytes(int64_t arrays) { return (8 * (kNormBlocks + arrays) + 255) / 256 * 256; }
+constexpr int32_t kNormList = 192;           // arrays per launch that adds up squares
+constexpr int32_t kNormBlocks = 1024;        // its work-groups, at most, each of which leaves a sum
+inline int64_t norm_workspace_bytes(int64_t arrays) { return (8 * (kNormBlocks * ((arrays + kNormList - 1) / kNormList + 1) + 1) + 255) / 256 * 256; }
 
 struct ArrayList {
     int32_t n;
