@@ -34,19 +34,17 @@ __device__ __forceinline__ double read_lane(double x, int lane)
     const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane);
     return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 
 // largest over the wave (no lane holds NaN), wave-uniform
 template <typename T>
 __device__ __forceinline__ T wave_max(T x)
 {
-    x = larger(x, dpp_keep<0xB1>(x));        // quad_perm [1,0,3,2]
-    x = larger(x, dpp_keep<0x4E>(x));        // quad_perm [2,3,0,1]
-    x = larger(x, dpp_keep<0x141>(x));       // row_half_mirror
-    x = larger(x, dpp_keep<0x140>(x));       // row_mirror
-    x = larger(x, dpp_keep<0x142, 0xA>(x));  // row_bcast15 into rows 1 and 3
-    x = larger(x, dpp_keep<0x143, 0xC>(x));  // row_bcast31 into rows 2 and 3
+    x = max(x, dpp_keep<0xB1>(x));        // quad_perm [1,0,3,2]
+    x = max(x, dpp_keep<0x4E>(x));        // quad_perm [2,3,0,1]
+    x = max(x, dpp_keep<0x141>(x));       // row_half_mirror
+    x = max(x, dpp_keep<0x140>(x));       // row_mirror
+    x = max(x, dpp_keep<0x142, 0xA>(x));  // row_bcast15 into rows 1 and 3
+    x = max(x, dpp_keep<0x143, 0xC>(x));  // row_bcast31 into rows 2 and 3
     return read_lane(x, 63);
 }
 // sum over the wave in one fixed order
@@ -62,14 +60,63 @@ __device__ __forceinline__ float wave_sum(float x) { return group_sum<kWave>(x);
 __device__ __forceinline__ float log_sigmoid(float z) { return fminf(z, 0.f) - log1pf(expf(-fabsf(z))); }
 
 // ---- routing -----------------------------------------------------------------------------------
-// A work-group takes `cols` columns: their logits come to LDS row by row, then a wave works on one column at a time,
-// lane l holding the experts l, l + 64, ...  The k choices are k rounds of a maximum over the wave; among equal keys
-// the lowest expert is found from ballots.
-//
 // Keys.  Softmax and sigmoid rise with the logit, so without a bias the logits themselves are the keys.  With a bias, or where
 // a group's score is a sum, the scores are, in 64 bits: two biased scores that differ by less than 32 bits
 // tell apart are common among a few hundred experts, and the choice must not depend on how a sum was rounded.
-template <int R, typename Key>
+// The low 10 bits of a key's mantissa make way for the expert, so that the largest of several numbers says at once which expert is chosen and, among
+// keys that agree in the other 42 bits (a logit has 23), that it is the lowest.
+constexpr double kNone = -__builtin_huge_val();   // no expert
+constexpr uint64_t kIndexBits = 1023;
+static_assert(kExpertsMax <= static_cast<int>(kIndexBits) + 1, "experts in a key");
+__device__ __forceinline__ double pack(double key, int index)
+{
+    if (!(key > kNone)) return kNone;             // (NaN too)
+    key = fmin(key, 1.7976931348623157e308) + 0.0;   // (+inf has no mantissa to use, and -0 is 0)
+    const uint64_t low = key < 0.0 ? index : kIndexBits - index;
+    return __builtin_bit_cast(double, (__builtin_bit_cast(uint64_t, key) & ~kIndexBits) | low);
+}
+__device__ __forceinline__ int index_of(double packed)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, packed), low = b & kIndexBits;
+    return static_cast<int>(b >> 63 ? low : kIndexBits - low);
+}
+__device__ __forceinline__ double key_of(double packed)
+{
+    return packed == kNone ? kNone : __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, packed) & ~kIndexBits);
+}
+// a group's score from its two best keys
+__device__ __forceinline__ double group_score(double best, double second, bool pair, int group)
+{
+    return pair && second > kNone ? pack(key_of(best) + key_of(second), group) : pack(key_of(best), group);
+}
+// a logit that may not be chosen: NaN, or +inf where the softmax of its column is NaN (-inf is no key anyway)
+__device__ __forceinline__ bool no_number(float z, bool sigmoid) { return !(z == z) || (!sigmoid && z == kInf); }
+
+// What keys are made of: the logits, or the scores of either kind.
+enum Keys { kLogits, kSigmoids, kSoftmaxes };
+// Key of one expert.  top: the column's largest logit, part: 1 / the sum of exp(z - top), for softmax scores.
+template <Keys kKeys>
+__device__ __forceinline__ double key_from(float z, const float *bias, int e, float top, double part)
+{
+    if constexpr (kKeys == kLogits) return pack(z, e);   // (-inf is none)
+    double q;
+    if constexpr (kKeys == kSigmoids) {
+        // the reciprocal from the hardware's first guess and three Newton steps, of a denominator that is finite
+        const double d = fmin(1.0 + exp(-static_cast<double>(z)), 1e300);
+        q = __builtin_amdgcn_rcp(d);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) q = fma(q, fma(-d, q, 1.0), q);
+    } else {
+        q = exp(static_cast<double>(z) - static_cast<double>(top)) * part;
+    }
+    if (bias) q += static_cast<double>(bias[e]);
+    const double packed = pack(q, e);
+    return z == -kInf ? kNone : packed;
+}
+
+// Few columns: a wave works on one column at a time, lane l holding the experts l, l + 64, ...; the k choices are k rounds of a maximum over the
+// wave.  A work-group takes `cols` columns, whose logits come to LDS row by row.
+template <int R, Keys kKeys>
 __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const int cols)
 {
     extern __shared__ __align__(16) char lds_raw[];
@@ -80,7 +127,7 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
     const int tile_floats = (E * pitch + 3) / 4 * 4;
     int32_t *out_e = reinterpret_cast<int32_t *>(tile + tile_floats);   // [cols][k]
     float *out_w = reinterpret_cast<float *>(out_e + cols * k);
-    Key *keys = reinterpret_cast<Key *>(lds_raw + (tile_floats + 2 * cols * k + 3) / 4 * 16) + wv * E;   // [waves][E], with groups only
+    double *keys = reinterpret_cast<double *>(lds_raw + (tile_floats + 2 * cols * k + 3) / 4 * 16) + wv * E;   // [waves][E], with groups only
 
     const int c0 = blockIdx.x * cols, here = min(cols, a.batch - c0);
     for (int i = threadIdx.x; i < E * cols; i += blockDim.x) {
@@ -91,7 +138,6 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
 
     const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, pair = a.flags & NERVA_EXPERT_GROUP_PAIR;
     const int size = E / a.groups;
-    const Key kNone = -static_cast<Key>(kInf);
     for (int c = wv; c < here; c += waves) {
         float z[R];
         float top = -kInf;
@@ -100,44 +146,27 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
         for (int i = 0; i < R; ++i) {
             const int e = lane + i * kWave;
             z[i] = e < E ? tile[e * pitch + c] : -kInf;
-            const bool off = !(z[i] == z[i]) || (!sigmoid && z[i] == kInf);
+            const bool off = no_number(z[i], sigmoid);
             bad |= off;
-            if (off) z[i] = -kInf;                                      // not to be chosen
+            if (off) z[i] = -kInf;
             top = fmaxf(top, z[i]);
         }
         bad = __ballot(bad) != 0;
-        Key key[R];
-        float sum = 0.f;
-        if constexpr (sizeof(Key) == 8) {
-            double total = 1.0;
-            if (!sigmoid) {
-                top = wave_max(top);
-                total = 0.0;
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    key[i] = z[i] == -kInf ? 0.0 : exp(static_cast<double>(z[i]) - static_cast<double>(top));
-                    total += key[i];
-                }
-                total = wave_sum(total);
-                sum = static_cast<float>(total);
-            }
+        double total = 1.0;
+        if (kKeys == kSoftmaxes || (!sigmoid && !renormalise)) {
+            top = wave_max(top);
+            double sum = 0.0;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const int e = lane + i * kWave;
-                Key q = sigmoid ? 1.0 / (1.0 + exp(-static_cast<double>(z[i]))) : key[i] / total;
-                if (a.bias && e < E) q += static_cast<double>(a.bias[e]);
-                key[i] = z[i] == -kInf || !(q == q) ? kNone : q;
+                if constexpr (kKeys == kSoftmaxes) sum += z[i] == -kInf ? 0.0 : exp(static_cast<double>(z[i]) - static_cast<double>(top));
+                else sum += z[i] == -kInf ? 0.f : expf(z[i] - top);
             }
-        } else {
-            if (!sigmoid && !renormalise) {
-                top = wave_max(top);
-#pragma unroll
-                for (int i = 0; i < R; ++i) sum += z[i] == -kInf ? 0.f : expf(z[i] - top);
-                sum = wave_sum(sum);
-            }
-#pragma unroll
-            for (int i = 0; i < R; ++i) key[i] = z[i];
+            total = wave_sum(sum);
         }
+        double key[R];
+        const double part = 1.0 / total;
+#pragma unroll
+        for (int i = 0; i < R; ++i) key[i] = key_from<kKeys>(z[i], a.bias, min(lane + i * kWave, E - 1), top, part);
 
         if (a.groups > 1) {
 #pragma unroll
@@ -145,23 +174,31 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
                 if (lane + i * kWave < E) keys[lane + i * kWave] = key[i];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            Key best = kNone, second = kNone;
-            if (lane < a.groups)
-                for (int i = 0; i < size; ++i) {
-                    const Key q = keys[lane * size + i];
-                    second = q > best ? best : larger(second, q);
-                    best = larger(best, q);
+            // 2^n lanes a group, as many as there are
+            int per_group = kWave;
+            while (per_group * a.groups > kWave) per_group >>= 1;
+            const int g = lane / per_group;
+            double best = kNone, second = kNone;
+            if (g < a.groups)
+                for (int i = lane & (per_group - 1); i < size; i += per_group) {
+                    const double q = keys[g * size + i];
+                    second = fmax(second, fmin(best, q));
+                    best = fmax(best, q);
                 }
+            for (int d = 1; d < per_group; d <<= 1) {
+                const double b = __shfl_xor(best, d, kWave), q = __shfl_xor(second, d, kWave);
+                second = fmax(fmin(best, b), fmax(second, q));
+                best = fmax(best, b);
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            Key score = pair && second > kNone ? best + second : best;
+            double score = g < a.groups ? group_score(best, second, pair, g) : kNone;
             uint64_t open = 0;
             for (int t = 0; t < a.top_groups; ++t) {
-                const Key m = wave_max(score);
+                const double m = wave_max(score);
                 if (!(m > kNone)) break;
-                const int g = __builtin_ctzll(__ballot(score == m));
-                open |= 1ull << g;
-                if (lane == g) score = kNone;
+                open |= 1ull << index_of(m);
+                if (score == m) score = kNone;
             }
 #pragma unroll
             for (int i = 0; i < R; ++i)
@@ -171,21 +208,14 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
         // lane j ends up with the j-th choice
         int mine = -1;
         for (int j = 0; j < k; ++j) {
-            Key m = key[0];
+            double m = key[0];
 #pragma unroll
-            for (int i = 1; i < R; ++i) m = larger(m, key[i]);
+            for (int i = 1; i < R; ++i) m = fmax(m, key[i]);
             m = wave_max(m);
             if (!(m > kNone)) break;
-            int e = -1;
+            if (lane == j) mine = index_of(m);
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const uint64_t at = __ballot(key[i] == m);
-                if (e < 0 && at) {
-                    e = __builtin_ctzll(at) + i * kWave;
-                    if (lane == (e & (kWave - 1))) key[i] = kNone;
-                }
-            }
-            if (lane == j) mine = e;
+            for (int i = 0; i < R; ++i) key[i] = key[i] == m ? kNone : key[i];
         }
 
         const float zm = mine >= 0 ? tile[mine * pitch + c] : -kInf;
@@ -196,7 +226,7 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
             const float u = mine < 0 ? 0.f : expf(l - high);
             w = u / wave_sum(u);
         } else {
-            w = sigmoid ? 1.f / (1.f + expf(-zm)) : expf(zm - top) / sum;
+            w = sigmoid ? 1.f / (1.f + expf(-zm)) : expf(zm - top) / static_cast<float>(total);
         }
         w = mine >= 0 ? w * a.scale : 0.f;
         if (bad) w = __builtin_nanf("");
@@ -214,99 +244,316 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
     }
 }
 
+// Many columns: a lane owns a column, nothing crosses lanes.  The experts are cut into lists, of which a group has `parts`; a wave goes through
+// the experts of a list and keeps its K best keys in order, in registers: two instructions for each key and rank, as the expert travels in
+// the key.  With the lists in LDS a group's score is read off their heads, lists of groups that are not taken are emptied, and pairs of lists are
+// merged until one is left.
+// Bound by the arithmetic on 64-bit keys: 256 experts in 8 groups, 8 choices, 16384 columns 20 us, where one column per wave takes 54; the same
+// for 8192 columns 19 and 26, for 4096 18 and 14 (without a bias or groups 11 and 10).
+template <int K, Keys kKeys>
+__global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, const int lists, const int parts, const int size)
+{
+    static_assert((K & (K - 1)) == 0 && K >= 2, "lists are merged by halving");
+    extern __shared__ double kept[];                                     // [lists][K][64]
+    const int E = a.experts, k = a.k, waves = blockDim.x / kWave;
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    double *red = kept + lists * K * kWave;                              // [waves][64]
+    float *logs = reinterpret_cast<float *>(red + waves * kWave);        // [K][64]
+    int *bads = reinterpret_cast<int *>(logs + K * kWave);               // [waves][64]
+    const int own = blockIdx.x * kWave + lane, c = min(own, a.batch - 1);
+    const float *__restrict__ Z = a.Z + c;
+    const int64_t ldz = a.ldz;
+    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, pair = a.flags & NERVA_EXPERT_GROUP_PAIR;
+    constexpr int U = 8;   // logits in flight
+
+    float top = -kInf;
+    double total = 1.0;
+    if (kKeys == kSoftmaxes || (!sigmoid && !renormalise)) {
+        float z[U];
+        for (int e = wv; e < E; e += U * waves) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * waves, E - 1) * ldz];
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, no_number(z[u], false) ? -kInf : z[u]);
+        }
+        red[wv * kWave + lane] = top;
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, static_cast<float>(red[w * kWave + lane]));
+        __syncthreads();
+        double sum = 0.0;
+        for (int e = wv; e < E; e += U * waves) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * waves, E - 1) * ldz];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (z[u] == -kInf || no_number(z[u], false) || e + u * waves >= E) continue;
+                if constexpr (kKeys == kSoftmaxes) sum += exp(static_cast<double>(z[u]) - static_cast<double>(top));
+                else sum += expf(z[u] - top);
+            }
+        }
+        red[wv * kWave + lane] = sum;
+        __syncthreads();
+        total = 0.0;
+        for (int w = 0; w < waves; ++w) total += red[w * kWave + lane];
+    }
+
+    const int group_size = E / a.groups;
+    const double part = 1.0 / total;
+    bool bad = false;
+    for (int l = wv; l < lists; l += waves) {
+        const int group = l / parts, start = group * group_size + (l - group * parts) * size, end = min(start + size, (group + 1) * group_size);
+        double x[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) x[j] = kNone;
+        float z[U], next[U];
+        auto fetch = [&](int e0) {
+            const float *p = Z + e0 * ldz;
+            if (e0 + U <= end) {
+#pragma unroll
+                for (int u = 0; u < U; ++u, p += ldz) next[u] = *p;
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u, p += ldz) next[u] = e0 + u < end ? *p : -kInf;
+            }
+        };
+        fetch(start);
+        for (int e0 = start; e0 < end; e0 += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) z[u] = next[u];
+            fetch(e0 + U);
+            double q[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool off = no_number(z[u], sigmoid);
+                bad |= off;
+                q[u] = key_from<kKeys>(off ? -kInf : z[u], a.bias, min(e0 + u, end - 1), top, part);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    const double high = fmax(x[j], q[u]);
+                    q[u] = fmin(x[j], q[u]);
+                    x[j] = high;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) kept[(l * K + j) * kWave + lane] = x[j];
+    }
+    bads[wv * kWave + lane] = bad;
+    __syncthreads();
+
+    if (a.groups > 1) {
+        // scores to LDS, in the place of the sums that are done with
+        for (int g = wv; g < a.groups; g += waves) {
+            double best = kNone, second = kNone;
+            for (int l = g * parts; l < (g + 1) * parts; ++l) {
+                const double b = kept[l * K * kWave + lane], q = kept[(l * K + 1) * kWave + lane];
+                second = fmax(fmin(best, b), fmax(second, q));
+                best = fmax(best, b);
+            }
+            red[g * kWave + lane] = group_score(best, second, pair, g);
+        }
+        __syncthreads();
+        for (int l = wv; l < lists; l += waves) {
+            const double mine = red[l / parts * kWave + lane];
+            int better = 0;
+            for (int g = 0; g < a.groups; ++g) better += red[g * kWave + lane] > mine;
+            if (better >= a.top_groups)
+#pragma unroll
+                for (int j = 0; j < K; ++j) kept[(l * K + j) * kWave + lane] = kNone;
+        }
+        __syncthreads();
+    }
+    for (int n = lists; n > 1;) {
+        const int half = (n + 1) / 2;
+        for (int l = wv; l < n - half; l += waves) {
+            double *p = kept + l * K * kWave + lane, x[K];
+            const double *q = p + half * K * kWave;
+#pragma unroll
+            for (int j = 0; j < K; ++j) x[j] = fmax(p[j * kWave], q[(K - 1 - j) * kWave]);   // the K largest, up and then down or the reverse
+#pragma unroll
+            for (int d = K / 2; d > 0; d /= 2)
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (!(j & d)) {
+                        const double high = fmax(x[j], x[j + d]);
+                        x[j + d] = fmin(x[j], x[j + d]);
+                        x[j] = high;
+                    }
+#pragma unroll
+            for (int j = 0; j < K; ++j) p[j * kWave] = x[j];
+        }
+        __syncthreads();
+        n = half;
+    }
+
+    for (int j = wv; j < k; j += waves) {
+        const double x = kept[j * kWave + lane];
+        const float z = x > kNone ? Z[index_of(x) * ldz] : -kInf;
+        logs[j * kWave + lane] = renormalise && sigmoid && z > -kInf ? log_sigmoid(z) : z;
+    }
+    __syncthreads();
+    bad = false;
+    for (int w = 0; w < waves; ++w) bad |= bads[w * kWave + lane];
+    if (own >= a.batch) return;
+    float high = -kInf, sum = 0.f;
+    if (renormalise) {
+        for (int j = 0; j < k; ++j) high = fmaxf(high, logs[j * kWave + lane]);
+        for (int j = 0; j < k; ++j) {
+            const float l = logs[j * kWave + lane];
+            sum += l == -kInf ? 0.f : expf(l - high);
+        }
+    }
+    for (int j = wv; j < k; j += waves) {
+        const double x = kept[j * kWave + lane];
+        const int e = x > kNone ? index_of(x) : -1;
+        const float l = logs[j * kWave + lane];
+        float w = renormalise ? expf(l - high) / sum : sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top) / static_cast<float>(total);
+        w = e >= 0 ? w * a.scale : 0.f;
+        a.chosen[j * a.ldk + own] = e;
+        a.weights[j * a.ldk + own] = bad ? __builtin_nanf("") : w;
+    }
+}
+
 // Gradient of the logits.  With u = weight / scale, d the gradients of the column's weights:
 //     renormalised    dL_j = scale u_j (d_j - sum_i u_i d_i),  dz = dL for softmax, dL (1 - s) for sigmoid
 //     softmax         dz_e = scale p_e ([e chosen] d_e - sum_i p_i d_i), over all experts
 //     sigmoid         dz_e = scale s_e (1 - s_e) d_e
-// A lane owns a column and keeps its k choices in registers; the waves of a work-group share the experts, whose rows are
+// A lane owns a column; the waves of a work-group share its choices, then, each with all of them in registers, the experts, whose rows are
 // written whole, zeros included.
-constexpr int kBackWaves = 8;
+constexpr int kBackWaves = 16;   // at most
+constexpr int kBackRows = 8;     // of dZ for a wave, where there may be fewer waves
 template <int K>
 __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(const RouteBackwardArgs a)
 {
     __shared__ float red[2][kBackWaves][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    __shared__ float logs[K][kWave], grads[K][kWave];   // of the scores (of the logits for a softmax), and the gradients of the weights
+    __shared__ int chosen[K][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block(), waves = blockDim.x / kWave;
     const int own = blockIdx.x * kWave + lane, c = min(own, a.batch - 1);
     const int E = a.experts;
-    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE;
-    int e[K];
-    float g[K], z[K];
+    const float *__restrict__ Z = a.Z + c;
+    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, full = !sigmoid && !renormalise;
+    constexpr int U = 8;   // logits in flight
+    float z[U];
+    auto fetch = [&](int i) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-        e[j] = j < a.k ? a.chosen[j * a.ldk + c] : -1;
-        if (e[j] < 0 || e[j] >= E) e[j] = -1;
-        g[j] = e[j] >= 0 ? a.dweights[j * a.ldk + c] : 0.f;
-        z[j] = e[j] >= 0 ? a.Z[static_cast<int64_t>(e[j]) * a.ldz + c] : -kInf;
+        for (int u = 0; u < U; ++u) z[u] = Z[min(i + u * waves, E - 1) * a.ldz];
+    };
+    const bool once = E <= U * waves;   // a wave's rows stay in registers
+    if (full) fetch(wv);
+    for (int j = wv; j < K; j += waves) {
+        int e = j < a.k ? a.chosen[j * a.ldk + c] : -1;
+        if (e < 0 || e >= E) e = -1;
+        const float x = e >= 0 ? Z[e * a.ldz] : -kInf;
+        chosen[j][lane] = e;
+        grads[j][lane] = e >= 0 ? a.dweights[j * a.ldk + c] : 0.f;
+        // (without renormalisation a sigmoid's own gradient is all: it takes the place of its logarithm)
+        logs[j][lane] = e < 0 || !sigmoid ? x : renormalise ? log_sigmoid(x) : (1.f / (1.f + expf(-x))) * (1.f / (1.f + expf(x)));
     }
-    const bool full = !sigmoid && !renormalise;
     float top = -kInf, inv = 0.f, all = 0.f;
     if (full) {
-        float m = -kInf;
-        for (int i = wv; i < E; i += kBackWaves) m = fmaxf(m, a.Z[static_cast<int64_t>(i) * a.ldz + c]);
-        red[0][wv][lane] = m;
-        __syncthreads();
+        for (int i = wv; i < E; i += U * waves) {
+            if (i > wv) fetch(i);
 #pragma unroll
-        for (int w = 0; w < kBackWaves; ++w) top = fmaxf(top, red[0][w][lane]);
+            for (int u = 0; u < U; ++u) top = fmaxf(top, z[u]);
+        }
+        red[0][wv][lane] = top;
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, red[0][w][lane]);
         float s = 0.f;
-        for (int i = wv; i < E; i += kBackWaves) {
-            const float x = a.Z[static_cast<int64_t>(i) * a.ldz + c];
-            s += x == -kInf ? 0.f : expf(x - top);
+        for (int i = wv; i < E; i += U * waves) {
+            if (!once) fetch(i);
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += z[u] == -kInf || i + u * waves >= E ? 0.f : expf(z[u] - top);
         }
         red[1][wv][lane] = s;
         __syncthreads();
         s = 0.f;
-#pragma unroll
-        for (int w = 0; w < kBackWaves; ++w) s += red[1][w][lane];
+        for (int w = 0; w < waves; ++w) s += red[1][w][lane];
         inv = 1.f / s;
+    } else {
+        __syncthreads();
+    }
+    int e[K];
+    float g[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        e[j] = chosen[j][lane];
+        g[j] = grads[j][lane];
+    }
+    if (renormalise) {
+        float u[K], high = -kInf, s = 0.f, mean = 0.f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) high = fmaxf(high, logs[j][lane]);
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            g[j] = e[j] >= 0 ? a.scale * g[j] * (expf(z[j] - top) * inv) : 0.f;
-            all += g[j];
+            u[j] = e[j] >= 0 ? expf(logs[j][lane] - high) : 0.f;
+            s += u[j];
         }
-    } else if (renormalise) {
-        float l[K], high = -kInf, s = 0.f, mean = 0.f;
+        const float part = 1.f / s;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            l[j] = e[j] < 0 ? -kInf : sigmoid ? log_sigmoid(z[j]) : z[j];
-            high = fmaxf(high, l[j]);
+            u[j] = e[j] >= 0 ? u[j] * part : 0.f;
+            mean = fmaf(u[j], g[j], mean);
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            l[j] = e[j] >= 0 ? expf(l[j] - high) : 0.f;
-            s += l[j];
-        }
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            l[j] = e[j] >= 0 ? l[j] / s : 0.f;
-            mean = fmaf(l[j], g[j], mean);
-        }
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            g[j] = e[j] >= 0 ? a.scale * l[j] * (g[j] - mean) : 0.f;
-            if (sigmoid && e[j] >= 0) g[j] *= 1.f / (1.f + expf(z[j]));
+            g[j] = e[j] >= 0 ? a.scale * u[j] * (g[j] - mean) : 0.f;
+            if (sigmoid && e[j] >= 0) g[j] *= -expm1f(logs[j][lane]);   // 1 - s
         }
     } else {
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (e[j] >= 0) g[j] *= a.scale * (1.f / (1.f + expf(-z[j]))) * (1.f / (1.f + expf(z[j])));
+            if (e[j] >= 0) {
+                g[j] *= a.scale * (full ? expf(logs[j][lane] - top) * inv : logs[j][lane]);
+                all += full ? g[j] : 0.f;
+            }
     }
     if (own >= a.batch) return;
-    for (int i = wv; i < E; i += kBackWaves) {
-        float d = 0.f;
+    float *dZ = a.dZ + own;
+    for (int i = wv; i < E; i += U * waves) {
+        if (full && !once) fetch(i);
 #pragma unroll
-        for (int j = 0; j < K; ++j) d += e[j] == i ? g[j] : 0.f;
-        if (full) {
-            const float x = a.Z[static_cast<int64_t>(i) * a.ldz + c];
-            if (!(x == -kInf)) d -= expf(x - top) * inv * all;
+        for (int u = 0; u < U; ++u) {
+            const int x = i + u * waves;
+            if (x >= E) break;
+            float d = 0.f;
+#pragma unroll
+            for (int j = 0; j < K; ++j) d += e[j] == x ? g[j] : 0.f;
+            if (full && !(z[u] == -kInf)) d -= expf(z[u] - top) * inv * all;
+            dZ[x * a.lddz] = d;
         }
-        a.dZ[static_cast<int64_t>(i) * a.lddz + c] = d;
     }
 }
 
-template <int R, typename Key>
-hipError_t route_go(const RouteArgs &a, int cols, int waves, size_t lds, hipStream_t s)
+template <int R>
+hipError_t route_go(const RouteArgs &a, Keys keys, int cols, int waves, size_t lds, hipStream_t s)
 {
-    hipLaunchKernelGGL((route_kernel<R, Key>), dim3((a.batch + cols - 1) / cols), dim3(waves * kWave), lds, s, a, cols);
+    const dim3 grid((a.batch + cols - 1) / cols), block(waves * kWave);
+    if (keys == kLogits) hipLaunchKernelGGL((route_kernel<R, kLogits>), grid, block, lds, s, a, cols);
+    else if (keys == kSigmoids) hipLaunchKernelGGL((route_kernel<R, kSigmoids>), grid, block, lds, s, a, cols);
+    else hipLaunchKernelGGL((route_kernel<R, kSoftmaxes>), grid, block, lds, s, a, cols);
+    return hipGetLastError();
+}
+
+constexpr int kRouteLists = 16;    // of route_columns_kernel, at most
+constexpr int kRouteListSize = 8;  // experts in one, at least, where there may be fewer lists
+constexpr int kRouteColumnsFrom = 6144;
+template <int K>
+hipError_t route_columns_go(const RouteArgs &a, Keys keys, hipStream_t s)
+{
+    const int group_size = a.experts / a.groups;
+    int parts = kRouteLists / a.groups;
+    if (parts > group_size / kRouteListSize) parts = group_size / kRouteListSize;
+    if (parts < 1) parts = 1;
+    const int size = (group_size + parts - 1) / parts, lists = a.groups * parts, waves = lists < 4 ? 4 : lists;
+    const size_t lds = (static_cast<size_t>(lists) * K + waves) * kWave * 8 + (K + waves) * kWave * 4;
+    const dim3 grid((a.batch + kWave - 1) / kWave), block(waves * kWave);
+    if (keys == kLogits) hipLaunchKernelGGL((route_columns_kernel<K, kLogits>), grid, block, lds, s, a, lists, parts, size);
+    else if (keys == kSigmoids) hipLaunchKernelGGL((route_columns_kernel<K, kSigmoids>), grid, block, lds, s, a, lists, parts, size);
+    else hipLaunchKernelGGL((route_columns_kernel<K, kSoftmaxes>), grid, block, lds, s, a, lists, parts, size);
     return hipGetLastError();
 }
 
@@ -661,7 +908,7 @@ __global__ __launch_bounds__(kGradWaves * kWave) void weight_gradient_kernel(con
 constexpr size_t kCombineLds = 160 * 1024;
 constexpr int64_t kCombineWavesWanted = 1024;
 constexpr int kCombineUnroll = 4;    // list entries per lane and iteration; those of the next one are on their way
-enum Weights { kNone, kGathered, kStaged };
+enum Weights { kAllOne, kGathered, kStaged };
 template <int kRows, int kWaves, Weights kWeights>
 __global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeArgs a)
 {
@@ -765,27 +1012,31 @@ hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s)
 {
-    const bool wide = a.bias || (a.flags & NERVA_EXPERT_GROUP_PAIR);
+    const Keys keys = !a.bias && !(a.flags & NERVA_EXPERT_GROUP_PAIR) ? kLogits : a.flags & NERVA_EXPERT_SIGMOID ? kSigmoids : kSoftmaxes;
+    if (a.batch >= kRouteColumnsFrom && a.k <= 8 && a.groups <= kRouteLists)
+        return a.k <= 2 ? route_columns_go<2>(a, keys, s) : a.k <= 4 ? route_columns_go<4>(a, keys, s) : route_columns_go<8>(a, keys, s);
     int cols = a.batch >= 8192 ? 32 : a.batch >= 2048 ? 16 : a.batch >= 512 ? 8 : 4;
     auto bytes = [&](int c) {
         const int waves = c < 16 ? c : 16;
         const size_t tile = static_cast<size_t>((a.experts * (c + 1) + 3) / 4 * 4 + 2 * c * a.k + 3) / 4 * 16;
-        return tile + (a.groups > 1 ? static_cast<size_t>(waves) * a.experts * (wide ? 8 : 4) : 0);
+        return tile + (a.groups > 1 ? static_cast<size_t>(waves) * a.experts * 8 : 0);
     };
     while (cols > 4 && bytes(cols) > 64 * 1024) cols /= 2;
     const int waves = cols < 16 ? cols : 16;
     const size_t lds = bytes(cols);
-    if (a.experts <= 64) return wide ? route_go<1, double>(a, cols, waves, lds, s) : route_go<1, float>(a, cols, waves, lds, s);
-    if (a.experts <= 128) return wide ? route_go<2, double>(a, cols, waves, lds, s) : route_go<2, float>(a, cols, waves, lds, s);
-    if (a.experts <= 256) return wide ? route_go<4, double>(a, cols, waves, lds, s) : route_go<4, float>(a, cols, waves, lds, s);
-    if (a.experts <= 512) return wide ? route_go<8, double>(a, cols, waves, lds, s) : route_go<8, float>(a, cols, waves, lds, s);
-    return wide ? route_go<16, double>(a, cols, waves, lds, s) : route_go<16, float>(a, cols, waves, lds, s);
+    if (a.experts <= 64) return route_go<1>(a, keys, cols, waves, lds, s);
+    if (a.experts <= 128) return route_go<2>(a, keys, cols, waves, lds, s);
+    if (a.experts <= 256) return route_go<4>(a, keys, cols, waves, lds, s);
+    if (a.experts <= 512) return route_go<8>(a, keys, cols, waves, lds, s);
+    return route_go<16>(a, keys, cols, waves, lds, s);
 }
 
 template <int K>
 static void route_backward_go(const RouteBackwardArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(route_backward_kernel<K>, dim3((a.batch + kWave - 1) / kWave), dim3(kBackWaves * kWave), 0, s, a);
+    int waves = a.experts / kBackRows;
+    waves = waves < 4 ? 4 : waves > kBackWaves ? kBackWaves : waves;
+    hipLaunchKernelGGL(route_backward_kernel<K>, dim3((a.batch + kWave - 1) / kWave), dim3(waves * kWave), 0, s, a);
 }
 
 hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s)
@@ -830,7 +1081,7 @@ static hipError_t combine_go(const ExchangeArgs &a, hipStream_t s)
     const int groups = (a.features + per_block - 1) / per_block, width = pitch_of(a.batch, a.p.tile);
     const dim3 grid(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), block(kWaves * kWave);
     const size_t lds = per_block * width * sizeof(float), with_weights = lds + static_cast<size_t>(width) * a.k * sizeof(float);
-    if (!a.weights) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kNone>), grid, block, lds, s, a);
+    if (!a.weights) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kAllOne>), grid, block, lds, s, a);
     else if (with_weights <= kCombineLds) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kStaged>), grid, block, with_weights, s, a);
     else hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kGathered>), grid, block, lds, s, a);
     return hipGetLastError();

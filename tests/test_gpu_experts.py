@@ -87,6 +87,31 @@ def test_route(nb, E, B, k, groups, top, sigmoid, renorm, bias, pair):
         assert padding_untouched(chosen) and padding_untouched(w)
 
 
+@pytest.mark.parametrize("E,B,k,groups,top,sigmoid,renorm,bias,pair", [
+    (16, 6200, 2, 1, 1, 0, 0, 0, 0), (1, 6150, 1, 1, 1, 1, 1, 1, 0), (130, 6500, 7, 1, 1, 0, 1, 1, 0), (256, 6144, 8, 8, 4, 1, 1, 1, 1), (7, 6145, 1, 7, 3, 0, 0, 0, 1),
+    (1000, 6144, 4, 8, 5, 0, 0, 1, 1), (45, 6201, 8, 3, 2, 1, 0, 0, 1), (60, 6150, 5, 15, 9, 0, 1, 0, 0), (40, 6144, 3, 1, 1, 0, 1, 0, 0), (96, 6144, 9, 1, 1, 1, 1, 1, 0),
+    (34, 6160, 4, 17, 6, 0, 0, 1, 1)])
+def test_route_of_many_columns(nb, E, B, k, groups, top, sigmoid, renorm, bias, pair):
+    import torch
+    rng = np.random.default_rng(E + B + k)
+    Z = logits(rng, E, B, "masked")
+    Z[:, 3000:] = np.round(Z[:, 3000:] * (1 if not (bias or pair) else 4096)) / (1 if not (bias or pair) else 4096)
+    Z[rng.integers(0, E, 5), rng.integers(0, B, 5)] = np.nan
+    Z[rng.integers(0, E, 5), rng.integers(0, B, 5)] = np.inf
+    Z[:, 17] = np.finfo(np.float32).min
+    b = (0.3 * rng.standard_normal(E)).astype(np.float32) if bias else None
+    if bias and E > 8:
+        b[3], b[5], b[6] = -np.inf, np.nan, np.inf
+    want, weights, bound = ref.route(Z, b, k, groups, top, sigmoid, renorm, pair, 1.5)
+    flags = nb.NERVA_EXPERT_SIGMOID * sigmoid | nb.NERVA_EXPERT_RENORMALISE * renorm | nb.NERVA_EXPERT_GROUP_PAIR * pair
+    chosen, w = device_matrix(np.zeros((k, B), np.int32), B + 3), device_matrix(np.zeros((k, B), np.float32), B + 3)
+    nb.expert_route(device_matrix(Z, B + 1), None if b is None else torch.as_tensor(b).cuda(), E, B, k, groups, top, flags, 1.5, chosen, w)
+    got, gw = chosen.cpu().numpy(), w.cpu().numpy().astype(np.float64)
+    assert np.array_equal(got, want), np.argwhere(got != want)[:4]
+    assert np.array_equal(np.isnan(gw), np.isnan(weights)) and np.all(np.isnan(weights) | (np.abs(gw - weights) <= bound))
+    assert padding_untouched(chosen) and padding_untouched(w)
+
+
 def test_route_of_logits_that_are_no_numbers(nb):
     """NaN is not chosen and shows in the column's weights; +inf likewise under a softmax and the best score under a sigmoid."""
     import torch
