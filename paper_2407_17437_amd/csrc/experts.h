@@ -103,8 +103,8 @@ inline int32_t move_rows(int32_t features, int64_t tiles, int32_t most)
     while (rows > 4 && (features + rows - 1) / rows * tiles < 512) rows /= 2;
     return rows;
 }
-// ... of the combine's backward pass, whose products over so many rows make one entry of `partial` (without the placement's tiles: the
-// workspace is asked for without the experts)
+// The fewest that the combine's backward pass takes, whose products over so many rows make one entry of `partial`: the workspace is asked for without
+// the experts, and with them there may be more tiles.
 inline int32_t partial_rows(int32_t features, int32_t batch) { return move_rows(features, (batch + kPlaceTileMax - 1) / kPlaceTileMax, 16); }
 hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s);
