@@ -101,11 +101,11 @@ __device__ __forceinline__ double key_from(float z, const float *bias, int e, fl
     if constexpr (kKeys == kLogits) return pack(z, e);   // (-inf is none)
     double q;
     if constexpr (kKeys == kSigmoids) {
-        // the reciprocal from the hardware's first guess and three Newton steps, of a denominator that is finite
+        // the reciprocal from the hardware's first guess, good to 23 bits, and two Newton steps, of a denominator that is finite
         const double d = fmin(1.0 + exp(-static_cast<double>(z)), 1e300);
         q = __builtin_amdgcn_rcp(d);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) q = fma(q, fma(-d, q, 1.0), q);
+        for (int i = 0; i < 2; ++i) q = fma(q, fma(-d, q, 1.0), q);
     } else {
         q = exp(static_cast<double>(z) - static_cast<double>(top)) * part;
     }
@@ -420,21 +420,22 @@ __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, 
 //     renormalised    dL_j = scale u_j (d_j - sum_i u_i d_i),  dz = dL for softmax, dL (1 - s) for sigmoid
 //     softmax         dz_e = scale p_e ([e chosen] d_e - sum_i p_i d_i), over all experts
 //     sigmoid         dz_e = scale s_e (1 - s_e) d_e
-// A lane owns a column; the waves of a work-group share its choices, then, each with all of them in registers, the experts, whose rows are
-// written whole, zeros included.
+// A lane owns a column, the waves of a work-group share its choices and the experts, whose rows are written whole.  Where only the chosen
+// experts have a gradient the zeros are under way before the choices are read, and the gradients follow one by one.
 constexpr int kBackWaves = 16;   // at most
 constexpr int kBackRows = 8;     // of dZ for a wave, where there may be fewer waves
-template <int K>
+template <int K, bool kFull>
 __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(const RouteBackwardArgs a)
 {
-    __shared__ float red[2][kBackWaves][kWave];
+    __shared__ float red[kFull ? 2 : 1][kBackWaves][kWave];
     __shared__ float logs[K][kWave], grads[K][kWave];   // of the scores (of the logits for a softmax), and the gradients of the weights
     __shared__ int chosen[K][kWave];
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block(), waves = blockDim.x / kWave;
     const int own = blockIdx.x * kWave + lane, c = min(own, a.batch - 1);
     const int E = a.experts;
     const float *__restrict__ Z = a.Z + c;
-    const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, full = !sigmoid && !renormalise;
+    float *dZ = a.dZ + c;
+    const bool on = own < a.batch, sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE;
     constexpr int U = 8;   // logits in flight
     float z[U];
     auto fetch = [&](int i) {
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
         for (int u = 0; u < U; ++u) z[u] = Z[min(i + u * waves, E - 1) * a.ldz];
     };
     const bool once = E <= U * waves;   // a wave's rows stay in registers
-    if (full) fetch(wv);
+    if constexpr (kFull) fetch(wv);
     for (int j = wv; j < K; j += waves) {
         int e = j < a.k ? a.chosen[j * a.ldk + c] : -1;
         if (e < 0 || e >= E) e = -1;
@@ -452,8 +453,8 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
         // (without renormalisation a sigmoid's own gradient is all: it takes the place of its logarithm)
         logs[j][lane] = e < 0 || !sigmoid ? x : renormalise ? log_sigmoid(x) : (1.f / (1.f + expf(-x))) * (1.f / (1.f + expf(x)));
     }
-    float top = -kInf, inv = 0.f, all = 0.f;
-    if (full) {
+    if constexpr (kFull) {
+        float top = -kInf, s = 0.f;
         for (int i = wv; i < E; i += U * waves) {
             if (i > wv) fetch(i);
 #pragma unroll
@@ -462,7 +463,6 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
         red[0][wv][lane] = top;
         __syncthreads();
         for (int w = 0; w < waves; ++w) top = fmaxf(top, red[0][w][lane]);
-        float s = 0.f;
         for (int i = wv; i < E; i += U * waves) {
             if (!once) fetch(i);
 #pragma unroll
@@ -472,58 +472,67 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
         __syncthreads();
         s = 0.f;
         for (int w = 0; w < waves; ++w) s += red[1][w][lane];
-        inv = 1.f / s;
-    } else {
-        __syncthreads();
-    }
-    int e[K];
-    float g[K];
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-        e[j] = chosen[j][lane];
-        g[j] = grads[j][lane];
-    }
-    if (renormalise) {
-        float u[K], high = -kInf, s = 0.f, mean = 0.f;
-#pragma unroll
-        for (int j = 0; j < K; ++j) high = fmaxf(high, logs[j][lane]);
+        const float inv = 1.f / s;
+        int e[K];
+        float g[K], all = 0.f;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            u[j] = e[j] >= 0 ? expf(logs[j][lane] - high) : 0.f;
-            s += u[j];
+            e[j] = chosen[j][lane];
+            g[j] = e[j] >= 0 ? a.scale * grads[j][lane] * (expf(logs[j][lane] - top) * inv) : 0.f;
+            all += g[j];
         }
-        const float part = 1.f / s;
+        if (!on) return;
+        for (int i = wv; i < E; i += U * waves) {
+            if (!once) fetch(i);
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            u[j] = e[j] >= 0 ? u[j] * part : 0.f;
-            mean = fmaf(u[j], g[j], mean);
-        }
+            for (int u = 0; u < U; ++u) {
+                const int x = i + u * waves;
+                if (x >= E) break;
+                float d = 0.f;
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            g[j] = e[j] >= 0 ? a.scale * u[j] * (g[j] - mean) : 0.f;
-            if (sigmoid && e[j] >= 0) g[j] *= -expm1f(logs[j][lane]);   // 1 - s
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (e[j] >= 0) {
-                g[j] *= a.scale * (full ? expf(logs[j][lane] - top) * inv : logs[j][lane]);
-                all += full ? g[j] : 0.f;
+                for (int j = 0; j < K; ++j) d += e[j] == x ? g[j] : 0.f;
+                if (!(z[u] == -kInf)) d -= expf(z[u] - top) * inv * all;
+                dZ[x * a.lddz] = d;
             }
-    }
-    if (own >= a.batch) return;
-    float *dZ = a.dZ + own;
-    for (int i = wv; i < E; i += U * waves) {
-        if (full && !once) fetch(i);
+        }
+    } else {
+        if (on)
+            for (int i = wv; i < E; i += waves) dZ[i * a.lddz] = 0.f;
+        // the zeros come before what another wave writes in their places: they are waited for (vmcnt 0), and the barrier orders the work-group's
+        // writes.  (A fence for the whole device would write the L2 back: 96 us where this takes 6.6, for 256 experts, 16384 columns and 8 choices.)
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+        if (!on || wv >= a.k) return;
+        float high = -kInf, s = 0.f, mean = 0.f;
+        if (renormalise) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int x = i + u * waves;
-            if (x >= E) break;
+            for (int j = 0; j < K; ++j) high = fmaxf(high, logs[j][lane]);
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const float u = chosen[j][lane] >= 0 ? expf(logs[j][lane] - high) : 0.f;
+                s += u;
+                mean = fmaf(u, grads[j][lane], mean);
+            }
+            s = 1.f / s;
+            mean *= s;
+        }
+        auto gradient = [&](int j) {
+            const float l = logs[j][lane], d = grads[j][lane];
+            if (!renormalise) return a.scale * d * l;
+            const float g = a.scale * (expf(l - high) * s) * (d - mean);
+            return sigmoid ? g * -expm1f(l) : g;   // (times 1 - score)
+        };
+        for (int j = wv; j < a.k; j += waves) {
+            const int e = chosen[j][lane];
+            bool first = e >= 0;
             float d = 0.f;
-#pragma unroll
-            for (int j = 0; j < K; ++j) d += e[j] == x ? g[j] : 0.f;
-            if (full && !(z[u] == -kInf)) d -= expf(z[u] - top) * inv * all;
-            dZ[x * a.lddz] = d;
+            if (first) d = gradient(j);
+            for (int i = 0; i < a.k; ++i) {   // an expert that a column has several times gets their sum, from the first of them
+                if (i == j || chosen[i][lane] != e || e < 0) continue;
+                if (i < j) first = false;
+                else d += gradient(i);
+            }
+            if (first) dZ[e * a.lddz] = d;
         }
     }
 }
@@ -1012,6 +1021,9 @@ hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
     const int groups = (a.features + kRows - 1) / kRows, width = pitch_of(a.batch, a.p.tile);
     const int share = (a.experts + a.p.tiles - 1) / a.p.tiles;   // of the experts, cleared one per wave
     int threads = (width * a.k > 16 * share ? width * a.k : 16 * share);
+    // (with few work-groups rather twice as many at a time on a compute unit: 1501 rows of 777 columns 15.0 us -> 12.8, 512 of 4096 12.6 -> 10.6;
+    // with many it is the other way round: 4096 rows of 8192 columns, one choice, 77 us -> 91)
+    if (static_cast<int64_t>(groups) * a.p.tiles < 2048) threads /= 2;
     threads = (threads + kWave - 1) / kWave * kWave;
     threads = threads < 512 ? 512 : threads > kMoveThreads ? kMoveThreads : threads;
     hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), dim3(threads),
@@ -1047,7 +1059,9 @@ static void route_backward_go(const RouteBackwardArgs &a, hipStream_t s)
 {
     int waves = a.experts / kBackRows;
     waves = waves < 4 ? 4 : waves > kBackWaves ? kBackWaves : waves;
-    hipLaunchKernelGGL(route_backward_kernel<K>, dim3((a.batch + kWave - 1) / kWave), dim3(waves * kWave), 0, s, a);
+    const dim3 grid((a.batch + kWave - 1) / kWave), block(waves * kWave);
+    if (a.flags & (NERVA_EXPERT_SIGMOID | NERVA_EXPERT_RENORMALISE)) hipLaunchKernelGGL((route_backward_kernel<K, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((route_backward_kernel<K, true>), grid, block, 0, s, a);
 }
 
 hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s)
