@@ -343,7 +343,8 @@ enum {
  * logit itself is the key, which orders alike), the experts of a column are, best first, the k of largest key; among equal
  * keys the lower expert comes first.  With groups > 1 the experts are cut into so many groups of consecutive ones (at most 64,
  * of equal size) and only those of the top_groups groups of largest score may be chosen (ties as above).  Keys are formed
- * in 64 bits; those that agree in the leading 42 bits of their mantissas count as equal, and groups' scores likewise.  Weights come from the scores, without the bias:
+ * in 64 bits and cut to the leading 42 bits of their mantissas before they are compared or added up to a group's score, which is cut likewise.
+ * Weights come from the scores, without the bias:
  *     weights[j,c] = scale * s_e, or scale * s_e / (sum of s over the column's choices).
  * An expert whose logit is -inf (or whose key is -inf or NaN) is never chosen; a column with fewer than k experts left
  * gets chosen = -1 and weight 0 for the rest.  A NaN logit (or +inf under the softmax) is not chosen either and makes all weights of its

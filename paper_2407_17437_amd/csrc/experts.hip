@@ -101,11 +101,13 @@ __device__ __forceinline__ double key_from(float z, const float *bias, int e, fl
     if constexpr (kKeys == kLogits) return pack(z, e);   // (-inf is none)
     double q;
     if constexpr (kKeys == kSigmoids) {
-        // the reciprocal from the hardware's first guess, good to 23 bits, and two Newton steps, of a denominator that is finite
-        const double d = fmin(1.0 + exp(-static_cast<double>(z)), 1e300);
+        // 1 / (1 + exp(-z)), or exp(z) / (1 + exp(z)): nothing overflows.  The reciprocal from the hardware's first guess, good to 23 bits, and
+        // two Newton steps.
+        const double t = exp(-fabs(static_cast<double>(z))), d = 1.0 + t;
         q = __builtin_amdgcn_rcp(d);
 #pragma unroll
         for (int i = 0; i < 2; ++i) q = fma(q, fma(-d, q, 1.0), q);
+        if (z < 0.f) q *= t;
     } else {
         q = exp(static_cast<double>(z) - static_cast<double>(top)) * part;
     }

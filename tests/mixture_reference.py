@@ -29,7 +29,7 @@ def route(Z, bias, k, groups, top_groups, sigmoid, renorm, pair, scale):
         top = z[open_].max() if open_.any() else 0.0
         with np.errstate(over="ignore", invalid="ignore"):
             total = np.exp(z[open_] - top).sum()
-            score = np.where(open_, 1 / (1 + np.exp(-z)) if sigmoid else np.exp(z - top) / max(total, 1), 0)
+            score = np.where(open_, np.where(z >= 0, 1 / (1 + np.exp(-z)), np.exp(z) / (1 + np.exp(z))) if sigmoid else np.exp(z - top) / max(total, 1), 0)
         key = z.copy()
         if bias is not None or (pair and groups > 1):
             key = np.where(open_, score + (0 if bias is None else np.asarray(bias, np.float64)), -np.inf)

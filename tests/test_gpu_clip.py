@@ -101,6 +101,29 @@ def test_step_without_clipping_is_the_plain_step(nb):
         assert all(torch.equal(a, b) for a, b in zip(w + v, w2 + v2))
 
 
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_step_on_more_than_the_cache_holds(nb, nesterov):
+    """Lists beyond 256 MiB of arrays, in several launches: without clipping the bits of the plain step, with it the step of scaled gradients."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(3)
+    counts = [65537, 12, 150001] * 74 + [4097]
+    assert 20 * sum(counts) > 256 << 20 and len(counts) > 192
+    new = lambda scale: [scale * torch.randn(n, generator=g, device="cuda") for n in counts]
+    grads, w, v = new(1.0), new(1.0), new(0.1)
+    total = sum(float(x.double().square().sum()) for x in grads) ** 0.5
+    ws, norm = workspace(nb, len(counts)), torch.zeros(1, device="cuda")
+    plain = nb.sgd_update_values_nesterov if nesterov else nb.sgd_update_values
+    for max_norm in (float("inf"), 2.5):
+        w2, v2 = [t.clone() for t in w], [t.clone() for t in v]
+        nb.sgd_update_clipped(w, v, grads, 0.05, 0.9, max_norm, nesterov, ws, norm)
+        assert abs(float(norm) - total) <= total * U * 1.001
+        # the kernel's factor is the fp32 nearest to max_norm / norm, whose last step the sum's order in 64 bits does not reach
+        c = float(np.float32(min(1.0, max_norm / total)))
+        for a, b, x in zip(w2, v2, grads):
+            plain(a, b, c * x, x.numel(), 0.05, 0.9)
+        assert all(torch.equal(a, b) for a, b in zip(w + v, w2 + v2))
+
+
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 3.0e38])
 def test_a_norm_that_is_not_finite_changes_nothing(nb, value):
     import torch

@@ -112,6 +112,31 @@ def test_route_of_many_columns(nb, E, B, k, groups, top, sigmoid, renorm, bias, 
     assert padding_untouched(chosen) and padding_untouched(w)
 
 
+@pytest.mark.parametrize("B", [3, 6200])
+def test_route_by_scores_far_out(nb, B):
+    """Sums of two scores whose logits lie where a sigmoid of 32 bits, or the exponential in it, has left its range."""
+    import torch
+    E = 16
+    z = np.array([-720, -700, -690.5, -650, -100, -89, -20, -1, 0, 1, 17, 36, -708, np.finfo(np.float32).min, -np.inf, -30], np.float32)
+    rng = np.random.default_rng(1)
+    Z = np.stack([rng.permutation(z) for _ in range(B)], 1)
+    for groups, top, k in ((8, 3, 6), (4, 2, 8)):
+        want, weights, bound = ref.route(Z, None, k, groups, top, 1, 0, 1, 1.0)
+        chosen, w = device_matrix(np.zeros((k, B), np.int32)), device_matrix(np.zeros((k, B), np.float32))
+        nb.expert_route(device_matrix(Z), None, E, B, k, groups, top, nb.NERVA_EXPERT_SIGMOID | nb.NERVA_EXPERT_GROUP_PAIR, 1.0, chosen, w)
+        # Scores are compared in 42 bits, and some sums here are nearly equal: 1/(1+e) + e/(1+e) = 1 and 1/(1+exp(-36)) = 1 - 2.3e-16.  A key is cut
+        # by less than 2^-42 of it, so is the sum of two cut keys, and two such sums are compared: nearer than 2^-40, and not equal, either may win.
+        with np.errstate(over="ignore"):
+            z = Z.astype(np.float64)
+            key = np.sort(np.where(z >= 0, 1 / (1 + np.exp(-z)), np.exp(z) / (1 + np.exp(z))).reshape(groups, E // groups, B), axis=1)
+        score = np.sort(key[:, -1] + key[:, -2], axis=0)
+        gap = np.diff(score, axis=0)
+        clear = ~((gap > 0) & (gap < 2.0 ** -40 * score[1:])).any(0)
+        assert clear.mean() > 0.5
+        assert np.array_equal(chosen.cpu().numpy()[:, clear], want[:, clear])
+        assert np.all(np.abs(w.cpu().numpy() - weights)[:, clear] <= bound[:, clear])
+
+
 def test_route_of_logits_that_are_no_numbers(nb):
     """NaN is not chosen and shows in the column's weights; +inf likewise under a softmax and the best score under a sigmoid."""
     import torch
@@ -282,6 +307,32 @@ def test_large_exchange_is_the_same_on_every_run(nb):
             want = ref.combine(Ye.cpu().numpy(), chosen.cpu().numpy(), slots.cpu().numpy(), w.cpu().numpy())
             assert np.array_equal(Y.cpu().numpy(), want)
         assert all(torch.equal(a, b) for a, b in zip(first, [Y, dYe, dw]))
+
+
+def test_blocks_beyond_32_bits(nb):
+    """2.3 G entries: offsets that 32 bits do not hold, in entries; the same bits as the columns that went in."""
+    import torch
+    E, F, B, k, C = 8, 4096, 9, 2, 70000
+    Xe = torch.empty(E, F, C, device="cuda")
+    assert Xe.numel() > 2 ** 31
+    chosen = torch.tensor([[7, 0, 7, 3, 7, 6, 7, 5, 7], [0, 7, 6, 7, 5, 7, 4, 7, 3]], dtype=torch.int32, device="cuda")
+    slots, w = torch.empty_like(chosen), torch.rand(k, B, device="cuda")
+    X, dY = torch.randn(F, B, device="cuda"), torch.randn(F, B, device="cuda")
+    placement = torch.empty(nb.expert_placement_bytes(E, B, k) // 4, dtype=torch.int32, device="cuda")
+    nb.expert_place(chosen, E, B, k, C, slots, None, placement)
+    nb.expert_dispatch(X, placement, F, E, B, k, C, Xe)
+    for j in range(k):
+        for c in range(B):
+            assert torch.equal(Xe[int(chosen[j, c]), :, int(slots[j, c])], X[:, c])
+    assert int(torch.count_nonzero(Xe[7, -1])) == 9 and int(torch.count_nonzero(Xe[7])) == int(torch.count_nonzero(X))
+    Y, dw = torch.empty(F, B, device="cuda"), torch.empty(k, B, device="cuda")
+    nb.expert_combine(Xe, placement, None, F, E, B, k, C, Y)
+    assert torch.equal(Y, X + X)
+    room = torch.empty(nb.expert_combine_workspace_bytes(F, B, k) // 4, device="cuda")
+    nb.expert_combine_backward(Xe, dY, placement, w, F, E, B, k, C, None, dw, room)
+    want = (X.double() * dY.double()).sum(0)
+    bound = (X.double() * dY.double()).abs().sum(0) * (18 + F // 4) * ref.U
+    assert ((dw - want).abs() <= bound).all()
 
 
 def test_placement_of_other_sizes_stays_inside_the_operands(nb):
