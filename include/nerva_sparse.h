@@ -333,7 +333,8 @@ int sgd_update_clipped(int32_t n, float *const *values, float *const *velocities
  * Block e of an operand (experts, features, lde) starts at e * features * lde; it is an operand (features, lde) of the calls
  * above with `capacity` columns, lde >= capacity.  Sizes are known before the router has run: nothing waits for the device, and the whole
  * sequence may be captured.  1 <= experts <= 1024, 1 <= k <= 32; batch * k < 2^30.
- * Inputs and outputs of one call must not overlap. */
+ * Inputs and outputs of one call must not overlap; nor may, in time, calls that write a placement or a workspace and others that use it
+ * (two captured graphs, say, that hold the same one). */
 enum {
     NERVA_EXPERT_SIGMOID = 1,       /* scores are sigmoids of the logits, else their softmax over all experts       */
     NERVA_EXPERT_RENORMALISE = 2,   /* weights are divided by their sum over the column's choices                   */

@@ -285,28 +285,41 @@ def test_exchange(nb, E, F, B, k, C, kind):
             assert (got[slots < 0] == 0).all() and padding_untouched(dw)
 
 
-def test_large_exchange_is_the_same_on_every_run(nb):
-    """Several tiles, several hundred work-groups: the sums' order must not depend on which of them come first."""
+@pytest.mark.parametrize("E,F,B,k,C,variant", [
+    (128, 600, 5000, 6, 260, "a row per wave"), (8, 700, 2048, 2, 600, "two rows, short tiles"), (8, 1600, 4096, 2, 1100, "four rows, short tiles"),
+    (64, 1200, 6000, 4, 400, "four rows, long tiles"), (96, 1001, 8192, 8, 760, "work-groups of eight waves"), (128, 803, 8191, 10, 700, "weights not staged"),
+    (300, 301, 2500, 3, 30, "short runs")])
+def test_large_exchange_is_the_same_on_every_run(nb, E, F, B, k, C, variant):
+    """Many tiles and work-groups, in every way that the sizes choose: against the plain forms, and the sums' order must not depend on which work-groups
+    come first."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(4)
-    E, F, B, k, C = 128, 600, 5000, 6, 260
-    chosen = torch.rand(E, B, generator=g, device="cuda").topk(k, dim=0).indices.to(torch.int32)
-    Ye, dY = torch.randn(E, F, C, generator=g, device="cuda"), torch.randn(F, B, generator=g, device="cuda")
+    chosen = (torch.rand(E, B, generator=g, device="cuda") + 0.1 * torch.rand(E, 1, generator=g, device="cuda")).topk(k, dim=0).indices.to(torch.int32)
+    Ye, dY, X = torch.randn(E, F, C, generator=g, device="cuda"), torch.randn(F, B, generator=g, device="cuda"), torch.randn(F, B, generator=g, device="cuda")
     w = torch.rand(k, B, generator=g, device="cuda")
     placement = torch.empty(nb.expert_placement_bytes(E, B, k) // 4, dtype=torch.int32, device="cuda")
     room = torch.empty(nb.expert_combine_workspace_bytes(F, B, k) // 4, device="cuda")
-    slots = torch.empty_like(chosen)
+    slots, counts = torch.empty_like(chosen), torch.empty(E, dtype=torch.int32, device="cuda")
     first = None
-    for _ in range(4):
-        Y, dYe, dw = torch.empty(F, B, device="cuda"), torch.empty_like(Ye), torch.empty_like(w)
-        nb.expert_place(chosen, E, B, k, C, slots, None, placement)
+    for _ in range(3):
+        Y, dYe, dw, Xe, dX = torch.empty(F, B, device="cuda"), torch.empty_like(Ye), torch.empty_like(w), torch.empty_like(Ye), torch.empty(F, B, device="cuda")
+        nb.expert_place(chosen, E, B, k, C, slots, counts, placement)
+        nb.expert_dispatch(X, placement, F, E, B, k, C, Xe)
         nb.expert_combine(Ye, placement, w, F, E, B, k, C, Y)
         nb.expert_combine_backward(Ye, dY, placement, w, F, E, B, k, C, dYe, dw, room)
+        nb.expert_combine(Ye, placement, None, F, E, B, k, C, dX)
         if first is None:
-            first = [Y, dYe, dw]
-            want = ref.combine(Ye.cpu().numpy(), chosen.cpu().numpy(), slots.cpu().numpy(), w.cpu().numpy())
-            assert np.array_equal(Y.cpu().numpy(), want)
-        assert all(torch.equal(a, b) for a, b in zip(first, [Y, dYe, dw]))
+            first = [Y, dYe, dw, Xe, dX]
+            h = [t.cpu().numpy() for t in (chosen, Ye, dY, X, w)]
+            want, n = ref.place(h[0], E, C)
+            assert np.array_equal(slots.cpu().numpy(), want) and np.array_equal(counts.cpu().numpy(), n)
+            assert np.array_equal(Y.cpu().numpy(), ref.combine(h[1], h[0], want, h[4]))
+            assert np.array_equal(dX.cpu().numpy(), ref.combine(h[1], h[0], want))
+            assert np.array_equal(Xe.cpu().numpy(), ref.dispatch(h[3], h[0], want, E, C))
+            assert np.array_equal(dYe.cpu().numpy(), ref.dispatch(h[2], h[0], want, E, C, h[4]))
+            gw, bound = ref.weight_gradient(h[1], h[2], h[0], want)
+            assert np.all(np.abs(dw.cpu().numpy() - gw) <= bound)
+        assert all(torch.equal(a, b) for a, b in zip(first, [Y, dYe, dw, Xe, dX]))
 
 
 def test_blocks_beyond_32_bits(nb):
