@@ -8,6 +8,8 @@
 // Squares are added up in 64 bits: the square of any fp32 number is exact there and in range (1e-90 ... 1e77), so the
 // norm neither overflows nor loses small entries beside large ones.  At 4 bytes read per entry the memory leaves some 80
 // cycles per wave and entry, which the conversion and the 64-bit multiply-add do not fill.
+#include <type_traits>
+
 #include "device.h"
 #include "experts.h"
 
@@ -16,15 +18,16 @@ namespace {
 
 // The arrays are cut into short chunks, and work-groups, as many as the GPU holds, take chunk after chunk, so that all of them together
 // read one stretch of memory at a time.  (A long stretch for each work-group instead, all of the same length, keeps meeting in few
-// memory channels: the norm and step of 134 M entries took 727 us that way, 600 so.)
+// memory channels: the norm and step of 135 M entries took 727 us that way, 600 so.)
 constexpr int kClipThreads = 256;
 constexpr int kClipWaves = kClipThreads / kWave;
 constexpr int kNormThreads = 512;
 constexpr int kNormLoads = 4;                      // 16-byte reads in flight per thread
 constexpr int kNormChunk = 4 * kNormLoads * kNormThreads;
 constexpr int kApplyLoads = 4;
-constexpr int kApplyChunk = 4 * kApplyLoads * kClipThreads;
+constexpr int kPastLoads = 2;                      // of lists past the cache: four take more than 64 registers, and a wave of eight with them (535 us -> 566)
 constexpr int kApplyBlocks = 2048;
+constexpr int kFewEntries = 1 << 20;               // lists of so many and fewer are cut into chunks of a quarter
 constexpr int kPartialMost = 2048;                 // more partial sums are first added up by a launch of their own
 // Arrays per launch: they travel in the kernel's arguments, of which there may be 4 KiB.
 constexpr int kApplyList = 104;
@@ -110,9 +113,16 @@ __global__ __launch_bounds__(kNormThreads) void norm_partial_kernel(const NormLi
     if (threadIdx.x == 0) l.partial[blockIdx.x] = sum;
 }
 
-// the partial sums' sum, the same bits in every work-group
+// the partial sums' sum, the same bits in every work-group (few of them: every wave adds up all, and none waits for another)
 __device__ __forceinline__ double sum_of(const double *partial, int n, double *lds)
 {
+    if (n <= kWave) {
+        const int lane = threadIdx.x & (kWave - 1);
+        double s = lane < n ? partial[lane] : 0.0;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
+        return s;
+    }
     double s = 0;
     for (int i = threadIdx.x; i < n; i += kClipThreads) s += partial[i];
     return block_sum(s, lds, kClipWaves);
@@ -136,9 +146,9 @@ __device__ __forceinline__ void step4(float4 &w, float4 &v, float4 g, float c, c
 }
 
 // Of arrays that the 256 MiB of Infinity Cache cannot hold, weights and momentum buffers go past it, and the norm is taken from the last array to
-// the first, so that the step, which goes forward, still finds the gradients there that were read last: 134 M entries 642 us -> 554
-// (forward and past the cache 579, backward alone 639).  Smaller ones may still be there from the step before, and
-// past the cache 4.4 M entries take 24.3 us instead of 22.5.
+// the first, so that the step, which goes forward, still finds the gradients there that were read last: 135 M entries 642 us -> 554
+// (forward and past the cache 579, backward alone 639; now 535).  Smaller ones may still be there from the step before, and
+// past the cache 4.6 M entries took 24.3 us instead of 22.5 (now 20.7).
 constexpr int64_t kCacheBytes = 256ll << 20;
 template <bool kPast>
 __device__ __forceinline__ float4 load4(const float *p)
@@ -155,69 +165,77 @@ __device__ __forceinline__ void store4(float *p, float4 v)
     __builtin_nontemporal_store(x, reinterpret_cast<v4f_any *>(p));
 }
 
-template <bool kUpdate, bool kPast>
+template <bool kUpdate, bool kPast, int kLoads>
 __global__ __launch_bounds__(kClipThreads) void clip_apply_kernel(const ApplyList l)
 {
     __shared__ double lds[kClipWaves];
+    constexpr int kStep = 4 * kClipThreads, kChunk = kLoads * kStep;
+    const int i = 4 * threadIdx.x;
+    const float *g = nullptr;
+    float *a = nullptr, *v = nullptr;
+    int n = 0;   // entries of the chunk
+    float4 ww[kLoads], vv[kLoads], gg[kLoads];
+    auto load = [&](int chunk) {
+        const int t = array_of(l, chunk);
+        const int64_t from = static_cast<int64_t>(chunk - l.first[t]) * kChunk;
+        n = static_cast<int>(min(l.counts[t] - from, static_cast<int64_t>(kChunk)));
+        g = l.grads[t] + from;
+        a = l.a[t] + from;
+        if constexpr (kUpdate) v = l.v[t] + from;
+        auto all = [&](auto whole) {   // (a whole chunk without a look at its end)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u)
+                if (whole.value || i + u * kStep + 3 < n) {
+                    gg[u] = ld4(g + i + u * kStep);
+                    if constexpr (kUpdate) {
+                        ww[u] = load4<kPast>(a + i + u * kStep);
+                        vv[u] = load4<kPast>(v + i + u * kStep);
+                    }
+                }
+        };
+        if (n == kChunk) all(std::true_type{});
+        else all(std::false_type{});
+    };
+    load(blockIdx.x);   // (on its way while the norm is added up)
+
     const double norm = sqrt(sum_of(l.partial, l.n_partial, lds));
     const float norm32 = static_cast<float>(norm);
     if (blockIdx.x == 0 && threadIdx.x == 0 && l.norm_out) *l.norm_out = norm32;
     if (!(norm32 <= 3.402823466e38f)) return;   // no factor makes such gradients finite: nothing is changed
     const float c = norm > l.max_norm ? static_cast<float>(l.max_norm / norm) : 1.f;
-    auto times = [c](float4 x) { return make_float4(c * x.x, c * x.y, c * x.z, c * x.w); };
 
-    for (int chunk = blockIdx.x; chunk < l.first[l.n]; chunk += gridDim.x) {
-        const int t = array_of(l, chunk);
-        const int64_t from = static_cast<int64_t>(chunk - l.first[t]) * kApplyChunk;
-        const int n = static_cast<int>(min(l.counts[t] - from, static_cast<int64_t>(kApplyChunk)));
-        const float *g = l.grads[t] + from;
-        float *a = l.a[t] + from;
-        float *v = kUpdate ? l.v[t] + from : nullptr;
-        if (!kUpdate && c == 1.f && a == g) continue;
-        int i = 4 * threadIdx.x;
-        constexpr int kStep = 4 * kClipThreads;
-        if (n == kApplyChunk) {
-            float4 ww[kApplyLoads], vv[kApplyLoads], gg[kApplyLoads];
+    for (int chunk = blockIdx.x;;) {
+        if (kUpdate || c != 1.f || a != g) {
+            auto all = [&](auto whole) {
 #pragma unroll
-            for (int u = 0; u < kApplyLoads; ++u) {
-                gg[u] = ld4(g + i + u * kStep);
+                for (int u = 0; u < kLoads; ++u)
+                    if (whole.value || i + u * kStep + 3 < n) {
+                        if constexpr (kUpdate) {
+                            step4(ww[u], vv[u], gg[u], c, l);
+                            store4<kPast>(v + i + u * kStep, vv[u]);
+                            store4<kPast>(a + i + u * kStep, ww[u]);
+                        } else {
+                            st4(a + i + u * kStep, make_float4(c * gg[u].x, c * gg[u].y, c * gg[u].z, c * gg[u].w));
+                        }
+                    }
+            };
+            if (n == kChunk) all(std::true_type{});
+            else all(std::false_type{});
+            const int last = (n & ~3) + threadIdx.x;   // an array's last one to three
+            if (last < n) {
                 if constexpr (kUpdate) {
-                    ww[u] = load4<kPast>(a + i + u * kStep);
-                    vv[u] = load4<kPast>(v + i + u * kStep);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kApplyLoads; ++u) {
-                if constexpr (kUpdate) {
-                    step4(ww[u], vv[u], gg[u], c, l);
-                    store4<kPast>(v + i + u * kStep, vv[u]);
-                    store4<kPast>(a + i + u * kStep, ww[u]);
+                    float w1 = a[last], v1 = v[last];
+                    momentum_step(w1, v1, c * g[last], l.lr, l.momentum, l.nesterov);
+                    v[last] = v1;
+                    a[last] = w1;
                 } else {
-                    st4(a + i + u * kStep, times(gg[u]));
+                    a[last] = c * g[last];
                 }
             }
-            continue;
         }
-        for (; i + 3 < n; i += kStep) {
-            if constexpr (kUpdate) {
-                float4 ww = ld4(a + i), vv = ld4(v + i);
-                step4(ww, vv, ld4(g + i), c, l);
-                st4(v + i, vv);
-                st4(a + i, ww);
-            } else {
-                st4(a + i, times(ld4(g + i)));
-            }
-        }
-        for (; i < n; ++i) {   // (the array's last one to three: one thread has them)
-            if constexpr (kUpdate) {
-                float ww = a[i], vv = v[i];
-                momentum_step(ww, vv, c * g[i], l.lr, l.momentum, l.nesterov);
-                v[i] = vv;
-                a[i] = ww;
-            } else {
-                a[i] = c * g[i];
-            }
-        }
+        chunk += gridDim.x;
+        if (chunk >= l.first[l.n]) break;
+        load(chunk);
     }
 }
 
@@ -288,7 +306,8 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
     float *norm_out = c.norm_out;
     int64_t entries = 0;
     for (int32_t t = 0; t < l.n; ++t) entries += l.counts[t];
-    const bool past = 20 * entries > kCacheBytes;
+    const bool past = 20 * entries > kCacheBytes, few = entries <= kFewEntries;
+    const int64_t chunk = 4 * kClipThreads * (few ? 1 : l.values && past ? kPastLoads : kApplyLoads);
     for (int32_t t = 0; t < l.n;) {
         ApplyList a;
         a.n = 0;
@@ -306,7 +325,7 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
             a.grads[a.n] = l.grads[t];
             a.counts[a.n] = m;
             a.first[a.n++] = static_cast<int32_t>(chunks);
-            chunks += (m + kApplyChunk - 1) / kApplyChunk;
+            chunks += (m + chunk - 1) / chunk;
         }
         if (chunks == 0) break;
         a.first[a.n] = static_cast<int32_t>(chunks);
@@ -319,9 +338,11 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
         a.norm_out = norm_out;
         norm_out = nullptr;
         const dim3 grid(static_cast<uint32_t>(chunks < kApplyBlocks ? chunks : kApplyBlocks));
-        if (l.values && past) hipLaunchKernelGGL((clip_apply_kernel<true, true>), grid, dim3(kClipThreads), 0, s, a);
-        else if (l.values) hipLaunchKernelGGL((clip_apply_kernel<true, false>), grid, dim3(kClipThreads), 0, s, a);
-        else hipLaunchKernelGGL((clip_apply_kernel<false, false>), grid, dim3(kClipThreads), 0, s, a);
+        if (l.values && past) hipLaunchKernelGGL((clip_apply_kernel<true, true, kPastLoads>), grid, dim3(kClipThreads), 0, s, a);
+        else if (l.values && !few) hipLaunchKernelGGL((clip_apply_kernel<true, false, kApplyLoads>), grid, dim3(kClipThreads), 0, s, a);
+        else if (l.values) hipLaunchKernelGGL((clip_apply_kernel<true, false, 1>), grid, dim3(kClipThreads), 0, s, a);
+        else if (!few) hipLaunchKernelGGL((clip_apply_kernel<false, false, kApplyLoads>), grid, dim3(kClipThreads), 0, s, a);
+        else hipLaunchKernelGGL((clip_apply_kernel<false, false, 1>), grid, dim3(kClipThreads), 0, s, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
