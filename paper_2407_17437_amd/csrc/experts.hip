@@ -578,9 +578,10 @@ __device__ __forceinline__ int expert_at(const PlaceArgs &a, int c, int j)
     return e >= 0 && e < a.experts ? e : a.experts;   // (one more for "no expert")
 }
 
+constexpr int kPlaceCounts = 4096;
 // Whether every work-group counts the choices of the whole batch for itself, in the place of a launch before: 777 columns with 4 choices
-// 8.1 us against 4.1 + 6.6, 1024 with 8 choices 15.1 against 4.9 + 10.0.
-__host__ __device__ inline bool counts_itself(const PlaceArgs &a) { return a.p.subs <= kPlaceWaves && a.batch * a.k <= 4096; }
+// 8.4 us against 2.4 + 6.4 and the gap between two launches, 1024 with 8 choices 15.8 against 4.7 + 10.3.
+__host__ __device__ inline bool counts_itself(const PlaceArgs &a) { return a.batch * a.k <= kPlaceCounts; }
 
 // choices of every expert in one run of kPlaceSub columns
 __global__ __launch_bounds__(kPlaceThreads) void place_count_kernel(const PlaceArgs a)
@@ -653,26 +654,40 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
     __shared__ int32_t kept_at[kExpertsMax + 1];  // list position of a place: kept_at + place, or ...
     __shared__ int32_t lost_at[kExpertsMax + 1];  // ... lost_at + place, of places beyond the capacity
     __shared__ int scan[kPlaceWaves][3];
-    extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in this round; at first those of every run, where nobody has counted them
+    extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in this round; at first before | inside | mine, [E + 1] each
     const int E = a.experts, E1 = E + 1;
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
     const int subs_per_tile = a.p.tile / kPlaceSub, sub = blockIdx.x, tile = sub / subs_per_tile;
     const int tile_sub = tile * subs_per_tile, tile_end = min(tile_sub + subs_per_tile, a.p.subs);
     const int c0 = sub * kPlaceSub, here = min(kPlaceSub, a.batch - c0);
 
-    // choices per expert: before the tile, before this run, in the tile
-    const bool count = counts_itself(a);
-    if (count) {
-        for (int i = threadIdx.x; i < a.p.subs * E1; i += kPlaceThreads) by_wave[i] = 0;
-        __syncthreads();
+    // choices per expert: before the tile, in the tile, and in its runs before this one
+    int32_t *before = by_wave, *inside = by_wave + E1, *mine = by_wave + 2 * E1;
+    static_assert(kPlaceWaves >= 3, "room for them");
+    for (int i = threadIdx.x; i < 3 * E1; i += kPlaceThreads) by_wave[i] = 0;
+    __syncthreads();
+    auto add = [&](int q, int e, int n) {   // n choices of expert e in run q
+        if (q < tile_sub) {
+            atomicAdd(&before[e], n);
+        } else if (q < tile_end) {
+            atomicAdd(&inside[e], n);
+            if (q < sub) atomicAdd(&mine[e], n);
+        }
+    };
+    if (counts_itself(a)) {
         for (int i = threadIdx.x; i < a.batch * a.k; i += kPlaceThreads) {
             const int j = i / a.batch, c = i - j * a.batch;
-            atomicAdd(&by_wave[c / kPlaceSub * E1 + expert_at(a, c, j)], 1);
+            add(c / kPlaceSub, expert_at(a, c, j), 1);
         }
-        __syncthreads();
+    } else {
+        const int64_t n = static_cast<int64_t>(tile_end) * E;
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < n; i += kPlaceThreads) {
+            const int q = static_cast<int>(i / E);
+            add(q, static_cast<int>(i - static_cast<int64_t>(q) * E), a.p.before[i]);
+        }
     }
-    const int32_t *counted = count ? by_wave : a.p.before;
-    const int64_t step = count ? E1 : E;
+    __syncthreads();
     int sums[3] = {0, 0, 0};   // choices with a place in this tile, without one, and of any expert in its runs before this one
     const int per = (E1 + kPlaceThreads - 1) / kPlaceThreads;   // consecutive experts per thread
     int kept[(kExpertsMax + 1 + kPlaceThreads - 1) / kPlaceThreads], lost[sizeof kept / sizeof *kept], at[sizeof kept / sizeof *kept], now[sizeof kept / sizeof *kept];
@@ -682,24 +697,16 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
         kept[i] = lost[i] = at[i] = now[i] = 0;
         const int e = first + i;
         if (i >= per || e >= E) continue;
-        int before = 0, inside = 0, mine = 0;
-        const int32_t *n = counted + e;
-        for (int q = 0; q < tile_sub; ++q) before += n[q * step];
-        for (int q = tile_sub; q < tile_end; ++q) {
-            const int x = n[q * step];
-            inside += x;
-            mine += q < sub ? x : 0;
-        }
-        at[i] = before;
-        now[i] = before + mine;
-        kept[i] = min(a.capacity, before + inside) - min(a.capacity, before);
-        lost[i] = inside - kept[i];
+        at[i] = before[e];
+        now[i] = at[i] + mine[e];
+        kept[i] = min(a.capacity, at[i] + inside[e]) - min(a.capacity, at[i]);
+        lost[i] = inside[e] - kept[i];
         sums[0] += kept[i];
         sums[1] += lost[i];
-        sums[2] += mine;
+        sums[2] += mine[e];
         if (tile == a.p.tiles - 1 && sub == tile_sub) {   // one work-group knows the whole batch
-            if (a.counts) a.counts[e] = before + inside;
-            a.p.filled[e] = min(a.capacity, before + inside);
+            if (a.counts) a.counts[e] = at[i] + inside[e];
+            a.p.filled[e] = min(a.capacity, at[i] + inside[e]);
         }
     }
     int totals[3];
@@ -834,15 +841,16 @@ __device__ __host__ __forceinline__ int pitch_of(int batch, int tile) { return (
 // neighbours lie next to each other in a block.  The empty places are cleared on the way, a share of the experts by each tile's work-groups.
 constexpr int kMoveThreads = 1024;   // at most; one per entry of the list where that is fewer
 template <int kRows, bool kGrad>
-__global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeArgs a)
+__global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeArgs a, const int staged)
 {
-    extern __shared__ __align__(16) float rows[];   // [kRows][width]
+    extern __shared__ __align__(16) float rows[];   // [kRows][width], then with `staged` the weights [k][width]
     const int tiles = a.p.tiles, at_block = xcd_run(blockIdx.x, gridDim.x), threads = blockDim.x;
     const int group = at_block / tiles, tile = at_block - group * tiles;
     const int f0 = group * kRows, nf = min(kRows, a.features - f0);
     if (nf <= 0) return;
     const int c0 = tile * a.p.tile, here = min(a.p.tile, a.batch - c0), width = pitch_of(a.batch, a.p.tile);
     stage_rows(rows, width, a.columns + static_cast<int64_t>(f0) * a.ldc + c0, a.ldc, nf, here);
+    if (kGrad && staged) stage_rows(rows + kRows * width, width, a.weights + c0, a.ldk, a.k, here);
     __syncthreads();
     const int total = here * a.k, kept = min(max(a.p.listed[tile], 0), total);
     const int2 *list = a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k;
@@ -855,7 +863,7 @@ __global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeAr
             const int64_t at = (static_cast<int64_t>(t.expert) * a.features + f0) * a.ldb + t.place;
             float *out = a.out_blocks + at;
             if constexpr (kGrad) {
-                const float w = a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
+                const float w = staged ? rows[(kRows + t.choice) * width + t.column] : a.weights ? a.weights[t.choice * a.ldk + c0 + t.column] : 1.f;
                 if (a.dweights) {
                     const float *y = a.blocks + at;
                     float dot = 0.f;
@@ -1017,6 +1025,7 @@ __global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeA
 
 uint32_t whole_eights(int64_t blocks) { return static_cast<uint32_t>((blocks + 7) / 8 * 8); }
 
+constexpr size_t kMoveLds = 160 * 1024;
 template <int kRows, bool kGrad>
 hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
 {
@@ -1028,8 +1037,12 @@ hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
     if (static_cast<int64_t>(groups) * a.p.tiles < 2048) threads /= 2;
     threads = (threads + kWave - 1) / kWave * kWave;
     threads = threads < 512 ? 512 : threads > kMoveThreads ? kMoveThreads : threads;
-    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), dim3(threads),
-                       kRows * width * sizeof(float), s, a);
+    // Weights from LDS, if only one work-group fits a compute unit with them: 64 experts and 4 choices 337 us -> 315, 256 and 8 (96 KiB) 413 -> 371; from the
+    // caches 64 lanes read 64 lines.
+    const size_t lds = kRows * width * sizeof(float), with_weights = lds + static_cast<size_t>(width) * a.k * sizeof(float);
+    const bool staged = kGrad && a.weights && a.out_blocks && with_weights <= kMoveLds;
+    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), dim3(threads), staged ? with_weights : lds, s, a,
+                       staged ? 1 : 0);
     return hipGetLastError();
 }
 
