@@ -934,7 +934,7 @@ __global__ __launch_bounds__(kGradWaves * kWave) void weight_gradient_kernel(con
 // kCombineRows rows and one tile's columns in LDS, for itself alone, so that nothing waits for other waves, and adds 64 entries of the
 // list to them at a time: read, add, write, for the first entry of every column, then for the second ones, as the turns say.
 // (LDS additions as atomics would need no turns, but take about 176 cycles for 64 lanes: 600 us for 4096 features, 8192 columns and four
-// choices of 64 experts, where this takes 160, 5.0 TB/s, and 177 with weights.)
+// choices of 64 experts, where this takes 158, 5.1 TB/s, and 171 with weights.)
 constexpr size_t kCombineLds = 160 * 1024;
 constexpr int64_t kCombineWavesWanted = 1536;
 constexpr int kCombineUnroll = 4;    // list entries per lane and iteration; those of the next one are on their way
@@ -954,22 +954,18 @@ __global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeA
     const int2 *__restrict__ list = a.p.lists + static_cast<int64_t>(tile) * a.p.tile * a.k;
     const float *__restrict__ weights = a.weights + c0;
     float *staged = rows + kWaves * kRows * width;
-    if constexpr (kWeights == kStaged) {
-        stage_rows(staged, width, weights, a.ldk, a.k, here);
-        __syncthreads();
-    }
-    if (nf <= 0) return;              // (no barrier from here on: waves share nothing that is written)
     float *sum = rows + wv * kRows * width;
     for (int i = lane; i < kRows * width; i += kWave) sum[i] = 0.f;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int64_t block = a.features * a.ldb, last_row = (nf - 1) * a.ldb;
-    const float *__restrict__ first = a.blocks + f0 * a.ldb;
+    const int64_t block = a.features * a.ldb, last_row = (max(nf, 1) - 1) * a.ldb;
+    const float *__restrict__ first = a.blocks + min(f0, a.features - 1) * a.ldb;
     // Entries are read one iteration before their values, and those one before they are added.  All reads are made, at a place of their own or
-    // a valid one, so that none waits for a branch.
+    // a valid one, so that none waits for a branch.  Weights are staged between the first of these reads, and taken from LDS where they are
+    // used: 1501 rows of 777 columns 13.4 us -> 12.1, 512 of 1024 with 16 experts 12.2 -> 11.4, 4096 of 8192 174 -> 171.
     struct Values {
         float w[U], v[U][kRows];
-        int column[U], turn[U];   // (turn -1: no entry)
+        int column[U], turn[U], weight[U];   // (turn -1: no entry; weight: where it is in `staged`)
     };
     int2 entry[U];
     auto fetch_entries = [&](int i) {
@@ -988,17 +984,24 @@ __global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeA
 #pragma unroll
             for (int r = 0; r < kRows; ++r) x.v[u][r] = y[min(r * a.ldb, last_row)];
             if constexpr (kWeights == kGathered) x.w[u] = weights[on ? t.choice * a.ldk + t.column : 0];
-            else if constexpr (kWeights == kStaged) x.w[u] = staged[on ? t.choice * width + t.column : 0];
+            else if constexpr (kWeights == kStaged) x.weight[u] = on ? t.choice * width + t.column : 0;
             else x.w[u] = 1.f;
         }
         return x;
     };
     fetch_entries(0);
+    if constexpr (kWeights == kStaged) stage_rows(staged, width, weights, a.ldk, a.k, here);
     Values now = fetch_values(0);
     fetch_entries(U * kWave);
+    if constexpr (kWeights == kStaged) __syncthreads();
+    if (nf <= 0) return;              // (no barrier from here on: waves share nothing that is written)
     for (int i = 0; i < kept; i += U * kWave) {
         const Values next = fetch_values(i + U * kWave);
         fetch_entries(i + 2 * U * kWave);
+        if constexpr (kWeights == kStaged) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) now.w[u] = staged[now.weight[u]];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             int m = 0;
@@ -1140,7 +1143,8 @@ hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s)
     const hipError_t e = rows == 16 ? dispatch_go<16, true>(a, s) : rows == 8 ? dispatch_go<8, true>(a, s) : dispatch_go<4, true>(a, s);
     if (e != hipSuccess || !a.dweights) return e;
     const int64_t total = static_cast<int64_t>(a.batch) * a.k;
-    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + kWave - 1) / kWave)), dim3(kGradWaves * kWave), 0, s, a, (a.features + rows - 1) / rows);
+    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + kWave - 1) / kWave)), dim3(kGradWaves * kWave), 0, s, a,
+                       (a.features + rows - 1) / rows);
     return hipGetLastError();
 }
 
