@@ -962,7 +962,7 @@ __global__ __launch_bounds__(kWaves * kWave) void combine_kernel(const ExchangeA
     const float *__restrict__ first = a.blocks + min(f0, a.features - 1) * a.ldb;
     // Entries are read one iteration before their values, and those one before they are added.  All reads are made, at a place of their own or
     // a valid one, so that none waits for a branch.  Weights are staged between the first of these reads, and taken from LDS where they are
-    // used: 1501 rows of 777 columns 13.4 us -> 12.1, 512 of 1024 with 16 experts 12.2 -> 11.4, 4096 of 8192 174 -> 171.
+    // used: 1501 rows of 777 columns 13.4 us -> 12.1, 512 of 4096 with 16 experts 12.2 -> 11.4, 4096 of 8192 174 -> 171.
     struct Values {
         float w[U], v[U][kRows];
         int column[U], turn[U], weight[U];   // (turn -1: no entry; weight: where it is in `staged`)
