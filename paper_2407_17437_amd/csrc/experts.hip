@@ -246,12 +246,46 @@ __global__ __launch_bounds__(1024) void route_kernel(const RouteArgs a, const in
     }
 }
 
+// the larger one to a
+__device__ __forceinline__ void order(double &a, double &b)
+{
+    const double high = fmax(a, b);
+    b = fmin(a, b);
+    a = high;
+}
+// eight keys in falling order: pairs, then two sorted halves merged, twice
+__device__ __forceinline__ void sort_down(double (&q)[8])
+{
+#pragma unroll
+    for (int n = 1; n < 8; n *= 2)        // runs of n are sorted
+#pragma unroll
+        for (int d = n; d > 0; d /= 2)
+#pragma unroll
+            for (int j = d % n; j + d < 8; j += 2 * d)
+#pragma unroll
+                for (int i = 0; i < d; ++i)
+                    if (j + i + d < 8 && (j + i) / (2 * n) == (j + i + d) / (2 * n)) order(q[j + i], q[j + i + d]);
+}
+// the K largest of two lists in falling order, x and y, in the same order
+template <int K, typename Y>
+__device__ __forceinline__ void keep_largest(double (&x)[K], Y y)
+{
+#pragma unroll
+    for (int j = 0; j < K; ++j) x[j] = fmax(x[j], y(K - 1 - j));   // up and then down or the reverse
+#pragma unroll
+    for (int d = K / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (!(j & d)) order(x[j], x[j + d]);
+}
+
 // Many columns: a lane owns a column, nothing crosses lanes.  The experts are cut into lists, of which a group has `parts`; a wave goes through
 // the experts of a list and keeps its K best keys in order, in registers: two instructions for each key and rank, as the expert travels in
-// the key.  With the lists in LDS a group's score is read off their heads, lists of groups that are not taken are emptied, and pairs of lists are
+// the key, or, where K is as many as the keys at a time, a sort of those and one merge (128 instructions for eight keys -> 70; 256
+// experts in 8 groups, 16384 columns 20.1 us -> 19.3, 1024 experts 81.7 -> 79.4).  With the lists in LDS a group's score is read off their heads, lists of groups that are not taken are emptied, and pairs of lists are
 // merged until one is left.
-// Bound by the arithmetic on 64-bit keys: 256 experts in 8 groups, 8 choices, 16384 columns 20 us, where one column per wave takes 54; the same
-// for 8192 columns 19 and 26, for 4096 18 and 14 (without a bias or groups 11 and 10).
+// Bound by the arithmetic on 64-bit keys: 256 experts in 8 groups, 8 choices, 16384 columns 19 us, where one column per wave takes 54; the same
+// for 8192 columns 18 and 26, for 4096 18 and 14 (without a bias or groups 11 and 10).
 template <int K, Keys kKeys>
 __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, const int lists, const int parts, const int size)
 {
@@ -330,6 +364,16 @@ __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, 
                 bad |= off;
                 q[u] = key_from<kKeys>(off ? -kInf : z[u], a.bias, min(e0 + u, end - 1), top, part);
             }
+            if constexpr (K == U) {
+                sort_down(q);
+                if (e0 == start) {
+#pragma unroll
+                    for (int j = 0; j < K; ++j) x[j] = q[j];
+                } else {
+                    keep_largest(x, [&](int j) { return q[j]; });
+                }
+                continue;
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -373,16 +417,8 @@ __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, 
             double *p = kept + l * K * kWave + lane, x[K];
             const double *q = p + half * K * kWave;
 #pragma unroll
-            for (int j = 0; j < K; ++j) x[j] = fmax(p[j * kWave], q[(K - 1 - j) * kWave]);   // the K largest, up and then down or the reverse
-#pragma unroll
-            for (int d = K / 2; d > 0; d /= 2)
-#pragma unroll
-                for (int j = 0; j < K; ++j)
-                    if (!(j & d)) {
-                        const double high = fmax(x[j], x[j + d]);
-                        x[j + d] = fmin(x[j], x[j + d]);
-                        x[j] = high;
-                    }
+            for (int j = 0; j < K; ++j) x[j] = p[j * kWave];
+            keep_largest(x, [&](int j) { return q[j * kWave]; });
 #pragma unroll
             for (int j = 0; j < K; ++j) p[j * kWave] = x[j];
         }
