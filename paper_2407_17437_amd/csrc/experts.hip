@@ -279,24 +279,26 @@ __device__ __forceinline__ void keep_largest(double (&x)[K], Y y)
             if (!(j & d)) order(x[j], x[j + d]);
 }
 
-// Many columns: a lane owns a column, nothing crosses lanes.  The experts are cut into lists, of which a group has `parts`; a wave goes through
-// the experts of a list and keeps its K best keys in order, in registers: two instructions for each key and rank, as the expert travels in
-// the key, or, where K is as many as the keys at a time, a sort of those and one merge (128 instructions for eight keys -> 70; 256
-// experts in 8 groups, 16384 columns 20.1 us -> 19.3, 1024 experts 81.7 -> 79.4).  With the lists in LDS a group's score is read off their heads, lists of groups that are not taken are emptied, and pairs of lists are
-// merged until one is left.
-// Bound by the arithmetic on 64-bit keys: 256 experts in 8 groups, 8 choices, 16384 columns 19 us, where one column per wave takes 54; the same
-// for 8192 columns 18 and 26, for 4096 18 and 14 (without a bias or groups 11 and 10).
-template <int K, Keys kKeys>
-__global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, const int lists, const int parts, const int size)
+// Many columns: a lane owns a column, nothing crosses lanes.  The experts are cut into lists, of which a group has `parts`; a taker, which is kCols
+// lanes, one for each of the work-group's columns, goes through the experts of a list and keeps its K best keys in order, in registers: two
+// instructions for each key and rank, as the expert travels in the key, or, where K is as many as the keys at a time, a sort of
+// those and one merge (128 instructions for eight keys -> 70; 256 experts in 8 groups, 16384 columns 20.1 us -> 19.3, 1024 experts 81.7 ->
+// 79.4).  With the lists in LDS a group's score is read off their heads, lists of groups that are not taken are emptied, and pairs of
+// lists are merged until one is left.
+// Bound by the arithmetic on 64-bit keys, some 100 instructions each from the logit to its rank: the vector units are busy for 64 % of the 70 us of 65536
+// columns of that kind in work-groups of 64, 78 % of the 65 in those of 32.  16384 columns take 19 us, where one column per wave takes 54.
+constexpr int kRouteLists = 16;    // at most
+template <int K, int kCols, Keys kKeys>
+__global__ __launch_bounds__(kRouteLists * kCols) void route_columns_kernel(const RouteArgs a, const int lists, const int parts, const int size)
 {
     static_assert((K & (K - 1)) == 0 && K >= 2, "lists are merged by halving");
-    extern __shared__ double kept[];                                     // [lists][K][64]
-    const int E = a.experts, k = a.k, waves = blockDim.x / kWave;
-    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
-    double *red = kept + lists * K * kWave;                              // [waves][64]
-    float *logs = reinterpret_cast<float *>(red + waves * kWave);        // [K][64]
-    int *bads = reinterpret_cast<int *>(logs + K * kWave);               // [waves][64]
-    const int own = blockIdx.x * kWave + lane, c = min(own, a.batch - 1);
+    extern __shared__ double kept[];                                     // [lists][K][kCols]
+    const int E = a.experts, k = a.k, takers = blockDim.x / kCols;
+    const int lane = threadIdx.x & (kCols - 1), taker = kCols == kWave ? wave_in_block() : static_cast<int>(threadIdx.x / kCols);
+    double *red = kept + lists * K * kCols;                              // [takers][kCols]
+    float *logs = reinterpret_cast<float *>(red + takers * kCols);       // [K][kCols]
+    int *bads = reinterpret_cast<int *>(logs + K * kCols);               // [takers][kCols]
+    const int own = blockIdx.x * kCols + lane, c = min(own, a.batch - 1);
     const float *__restrict__ Z = a.Z + c;
     const int64_t ldz = a.ldz;
     const bool sigmoid = a.flags & NERVA_EXPERT_SIGMOID, renormalise = a.flags & NERVA_EXPERT_RENORMALISE, pair = a.flags & NERVA_EXPERT_GROUP_PAIR;
@@ -306,37 +308,37 @@ __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, 
     double total = 1.0;
     if (kKeys == kSoftmaxes || (!sigmoid && !renormalise)) {
         float z[U];
-        for (int e = wv; e < E; e += U * waves) {
+        for (int e = taker; e < E; e += U * takers) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * waves, E - 1) * ldz];
+            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * takers, E - 1) * ldz];
 #pragma unroll
             for (int u = 0; u < U; ++u) top = fmaxf(top, no_number(z[u], false) ? -kInf : z[u]);
         }
-        red[wv * kWave + lane] = top;
+        red[taker * kCols + lane] = top;
         __syncthreads();
-        for (int w = 0; w < waves; ++w) top = fmaxf(top, static_cast<float>(red[w * kWave + lane]));
+        for (int w = 0; w < takers; ++w) top = fmaxf(top, static_cast<float>(red[w * kCols + lane]));
         __syncthreads();
         double sum = 0.0;
-        for (int e = wv; e < E; e += U * waves) {
+        for (int e = taker; e < E; e += U * takers) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * waves, E - 1) * ldz];
+            for (int u = 0; u < U; ++u) z[u] = Z[min(e + u * takers, E - 1) * ldz];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (z[u] == -kInf || no_number(z[u], false) || e + u * waves >= E) continue;
+                if (z[u] == -kInf || no_number(z[u], false) || e + u * takers >= E) continue;
                 if constexpr (kKeys == kSoftmaxes) sum += exp(static_cast<double>(z[u]) - static_cast<double>(top));
                 else sum += expf(z[u] - top);
             }
         }
-        red[wv * kWave + lane] = sum;
+        red[taker * kCols + lane] = sum;
         __syncthreads();
         total = 0.0;
-        for (int w = 0; w < waves; ++w) total += red[w * kWave + lane];
+        for (int w = 0; w < takers; ++w) total += red[w * kCols + lane];
     }
 
     const int group_size = E / a.groups;
     const double part = 1.0 / total;
     bool bad = false;
-    for (int l = wv; l < lists; l += waves) {
+    for (int l = taker; l < lists; l += takers) {
         const int group = l / parts, start = group * group_size + (l - group * parts) * size, end = min(start + size, (group + 1) * group_size);
         double x[K];
 #pragma unroll
@@ -384,69 +386,69 @@ __global__ __launch_bounds__(1024) void route_columns_kernel(const RouteArgs a, 
                 }
         }
 #pragma unroll
-        for (int j = 0; j < K; ++j) kept[(l * K + j) * kWave + lane] = x[j];
+        for (int j = 0; j < K; ++j) kept[(l * K + j) * kCols + lane] = x[j];
     }
-    bads[wv * kWave + lane] = bad;
+    bads[taker * kCols + lane] = bad;
     __syncthreads();
 
     if (a.groups > 1) {
         // scores to LDS, in the place of the sums that are done with
-        for (int g = wv; g < a.groups; g += waves) {
+        for (int g = taker; g < a.groups; g += takers) {
             double best = kNone, second = kNone;
             for (int l = g * parts; l < (g + 1) * parts; ++l) {
-                const double b = kept[l * K * kWave + lane], q = kept[(l * K + 1) * kWave + lane];
+                const double b = kept[l * K * kCols + lane], q = kept[(l * K + 1) * kCols + lane];
                 second = fmax(fmin(best, b), fmax(second, q));
                 best = fmax(best, b);
             }
-            red[g * kWave + lane] = group_score(best, second, pair, g);
+            red[g * kCols + lane] = group_score(best, second, pair, g);
         }
         __syncthreads();
-        for (int l = wv; l < lists; l += waves) {
-            const double mine = red[l / parts * kWave + lane];
+        for (int l = taker; l < lists; l += takers) {
+            const double mine = red[l / parts * kCols + lane];
             int better = 0;
-            for (int g = 0; g < a.groups; ++g) better += red[g * kWave + lane] > mine;
+            for (int g = 0; g < a.groups; ++g) better += red[g * kCols + lane] > mine;
             if (better >= a.top_groups)
 #pragma unroll
-                for (int j = 0; j < K; ++j) kept[(l * K + j) * kWave + lane] = kNone;
+                for (int j = 0; j < K; ++j) kept[(l * K + j) * kCols + lane] = kNone;
         }
         __syncthreads();
     }
     for (int n = lists; n > 1;) {
         const int half = (n + 1) / 2;
-        for (int l = wv; l < n - half; l += waves) {
-            double *p = kept + l * K * kWave + lane, x[K];
-            const double *q = p + half * K * kWave;
+        for (int l = taker; l < n - half; l += takers) {
+            double *p = kept + l * K * kCols + lane, x[K];
+            const double *q = p + half * K * kCols;
 #pragma unroll
-            for (int j = 0; j < K; ++j) x[j] = p[j * kWave];
-            keep_largest(x, [&](int j) { return q[j * kWave]; });
+            for (int j = 0; j < K; ++j) x[j] = p[j * kCols];
+            keep_largest(x, [&](int j) { return q[j * kCols]; });
 #pragma unroll
-            for (int j = 0; j < K; ++j) p[j * kWave] = x[j];
+            for (int j = 0; j < K; ++j) p[j * kCols] = x[j];
         }
         __syncthreads();
         n = half;
     }
 
-    for (int j = wv; j < k; j += waves) {
-        const double x = kept[j * kWave + lane];
+    for (int j = taker; j < k; j += takers) {
+        const double x = kept[j * kCols + lane];
         const float z = x > kNone ? Z[index_of(x) * ldz] : -kInf;
-        logs[j * kWave + lane] = renormalise && sigmoid && z > -kInf ? log_sigmoid(z) : z;
+        logs[j * kCols + lane] = renormalise && sigmoid && z > -kInf ? log_sigmoid(z) : z;
     }
     __syncthreads();
     bad = false;
-    for (int w = 0; w < waves; ++w) bad |= bads[w * kWave + lane];
+    for (int w = 0; w < takers; ++w) bad |= bads[w * kCols + lane];
     if (own >= a.batch) return;
     float high = -kInf, sum = 0.f;
     if (renormalise) {
-        for (int j = 0; j < k; ++j) high = fmaxf(high, logs[j * kWave + lane]);
+        for (int j = 0; j < k; ++j) high = fmaxf(high, logs[j * kCols + lane]);
         for (int j = 0; j < k; ++j) {
-            const float l = logs[j * kWave + lane];
+            const float l = logs[j * kCols + lane];
             sum += l == -kInf ? 0.f : expf(l - high);
         }
     }
-    for (int j = wv; j < k; j += waves) {
-        const double x = kept[j * kWave + lane];
+    for (int j = taker; j < k; j += takers) {
+        const double x = kept[j * kCols + lane];
         const int e = x > kNone ? index_of(x) : -1;
-        const float l = logs[j * kWave + lane];
+        const float l = logs[j * kCols + lane];
         float w = renormalise ? expf(l - high) / sum : sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top) / static_cast<float>(total);
         w = e >= 0 ? w * a.scale : 0.f;
         a.chosen[j * a.ldk + own] = e;
@@ -585,23 +587,32 @@ hipError_t route_go(const RouteArgs &a, Keys keys, int cols, int waves, size_t l
     return hipGetLastError();
 }
 
-constexpr int kRouteLists = 16;    // of route_columns_kernel, at most
 constexpr int kRouteListSize = 8;  // experts in one, at least, where there may be fewer lists
-constexpr int kRouteColumnsFrom = 6144;
-template <int K>
-hipError_t route_columns_go(const RouteArgs &a, Keys keys, hipStream_t s)
+template <int K, int kCols>
+hipError_t route_columns_of(const RouteArgs &a, Keys keys, hipStream_t s)
 {
     const int group_size = a.experts / a.groups;
     int parts = kRouteLists / a.groups;
     if (parts > group_size / kRouteListSize) parts = group_size / kRouteListSize;
     if (parts < 1) parts = 1;
-    const int size = (group_size + parts - 1) / parts, lists = a.groups * parts, waves = lists < 4 ? 4 : lists;
-    const size_t lds = (static_cast<size_t>(lists) * K + waves) * kWave * 8 + (K + waves) * kWave * 4;
-    const dim3 grid((a.batch + kWave - 1) / kWave), block(waves * kWave);
-    if (keys == kLogits) hipLaunchKernelGGL((route_columns_kernel<K, kLogits>), grid, block, lds, s, a, lists, parts, size);
-    else if (keys == kSigmoids) hipLaunchKernelGGL((route_columns_kernel<K, kSigmoids>), grid, block, lds, s, a, lists, parts, size);
-    else hipLaunchKernelGGL((route_columns_kernel<K, kSoftmaxes>), grid, block, lds, s, a, lists, parts, size);
+    const int size = (group_size + parts - 1) / parts, lists = a.groups * parts, takers = lists < 4 ? 4 : lists;
+    const size_t lds = (static_cast<size_t>(lists) * K + takers) * kCols * 8 + (K + takers) * kCols * 4;
+    const dim3 grid((a.batch + kCols - 1) / kCols), block(takers * kCols);
+    if (keys == kLogits) hipLaunchKernelGGL((route_columns_kernel<K, kCols, kLogits>), grid, block, lds, s, a, lists, parts, size);
+    else if (keys == kSigmoids) hipLaunchKernelGGL((route_columns_kernel<K, kCols, kSigmoids>), grid, block, lds, s, a, lists, parts, size);
+    else hipLaunchKernelGGL((route_columns_kernel<K, kCols, kSoftmaxes>), grid, block, lds, s, a, lists, parts, size);
     return hipGetLastError();
+}
+
+// Work-groups of 64 columns where each of them finds a compute unit of its own and those of 32 would not; else of 32, which share one by two: 8192
+// columns, 256 experts in 8 groups 18.3 us -> 14.0, 20000 columns 34.2 -> 27.7, 65536 70.5 -> 65; 16384 19.1 against 19.9, without groups
+// 11.1 against 12.8.  Logits as keys and few choices leave registers for two of 64 at a time: 65536 columns of 96 experts 16.8, in 32s 19.8.
+constexpr int kComputeUnits = 256;
+template <int K>
+hipError_t route_columns_go(const RouteArgs &a, Keys keys, hipStream_t s)
+{
+    const bool wide = a.batch > 32 * kComputeUnits && (a.batch <= 64 * kComputeUnits || (keys == kLogits && K <= 4));
+    return wide ? route_columns_of<K, 64>(a, keys, s) : route_columns_of<K, 32>(a, keys, s);
 }
 
 // ---- places --------------------------------------------------------------------------------------
@@ -1090,8 +1101,16 @@ hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
 hipError_t launch_route(const RouteArgs &a, hipStream_t s)
 {
     const Keys keys = !a.bias && !(a.flags & NERVA_EXPERT_GROUP_PAIR) ? kLogits : a.flags & NERVA_EXPERT_SIGMOID ? kSigmoids : kSoftmaxes;
-    if (a.batch >= kRouteColumnsFrom && a.k <= 8 && a.groups <= kRouteLists)
-        return a.k <= 2 ? route_columns_go<2>(a, keys, s) : a.k <= 4 ? route_columns_go<4>(a, keys, s) : route_columns_go<8>(a, keys, s);
+    // A lane per column from where work-groups of a wave per column, which take 16, no longer find a compute unit each (5000 columns, 256 experts, 8
+    // choices 25.0 us -> 13.9, 96 experts and 4 choices 9.8 -> 6.3), a little later for one or two choices, which a wave finds in as many
+    // rounds (4100 columns, 60 experts, one choice 4.3 against 6.0; 5000 5.8 and 6.0, 128 experts in groups 15 and 9), and with half of
+    // that already for many choices from many experts (4096 columns 14.4 -> 11.5 with 256 experts, 11.9 -> 8.9 with 128, 30 -> 14 with
+    // 1024; 64 experts and four choices 5.8 against 6.3).
+    if (a.k <= 8 && a.groups <= kRouteLists) {
+        if (a.batch > (a.k > 2 ? 16 : 18) * kComputeUnits)
+            return a.k <= 2 ? route_columns_go<2>(a, keys, s) : a.k <= 4 ? route_columns_go<4>(a, keys, s) : route_columns_go<8>(a, keys, s);
+        if (a.batch >= 8 * kComputeUnits && a.experts >= 128 && a.k > 4) return route_columns_of<8, 16>(a, keys, s);
+    }
     int cols = a.batch >= 8192 ? 32 : a.batch >= 2048 ? 16 : a.batch >= 512 ? 8 : 4;
     auto bytes = [&](int c) {
         const int waves = c < 16 ? c : 16;

@@ -112,6 +112,15 @@ def test_route_of_many_columns(nb, E, B, k, groups, top, sigmoid, renorm, bias, 
     assert padding_untouched(chosen) and padding_untouched(w)
 
 
+@pytest.mark.parametrize("E,B,k,groups,top,sigmoid,renorm,bias,pair", [
+    (128, 2048, 5, 1, 1, 0, 1, 0, 0), (256, 4096, 8, 16, 5, 0, 1, 1, 1), (1000, 2049, 8, 8, 5, 0, 0, 1, 1), (129, 3001, 6, 3, 2, 1, 0, 0, 1), (200, 2500, 7, 1, 1, 1, 1, 1, 0),
+    (128, 2047, 5, 1, 1, 1, 1, 1, 0), (127, 2048, 5, 1, 1, 0, 1, 0, 0), (15, 4608, 2, 5, 2, 1, 0, 0, 1), (15, 4609, 2, 5, 2, 1, 0, 0, 1), (64, 4097, 6, 8, 2, 1, 1, 0, 0), (256, 8192, 8, 8, 4, 1, 1, 1, 1),
+    (300, 4133, 1, 1, 1, 0, 0, 0, 0), (16, 8193, 2, 1, 1, 0, 1, 0, 0), (1, 8200, 1, 1, 1, 1, 1, 1, 0), (130, 9000, 7, 1, 1, 0, 1, 1, 0), (256, 16384, 8, 8, 4, 1, 1, 1, 1),
+    (45, 12001, 4, 3, 2, 1, 0, 0, 1), (40, 16385, 3, 1, 1, 0, 1, 0, 0), (40, 16385, 3, 1, 1, 0, 1, 1, 0), (77, 20001, 8, 7, 4, 0, 0, 1, 1)])
+def test_route_of_many_columns_in_work_groups_of_every_size(nb, E, B, k, groups, top, sigmoid, renorm, bias, pair):
+    test_route_of_many_columns(nb, E, B, k, groups, top, sigmoid, renorm, bias, pair)
+
+
 @pytest.mark.parametrize("B", [3, 6200])
 def test_route_by_scores_far_out(nb, B):
     """Sums of two scores whose logits lie where a sigmoid of 32 bits, or the exponential in it, has left its range."""
