@@ -701,7 +701,7 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
     __shared__ int32_t kept_at[kExpertsMax + 1];  // list position of a place: kept_at + place, or ...
     __shared__ int32_t lost_at[kExpertsMax + 1];  // ... lost_at + place, of places beyond the capacity
     __shared__ int scan[kPlaceWaves][3];
-    extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in this round; at first before | inside | mine, [E + 1] each
+    extern __shared__ int32_t by_wave[];          // [kPlaceWaves][E + 1] choices in one turn of the loop; at first before | inside | mine, [E + 1] each
     const int E = a.experts, E1 = E + 1;
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
     const int subs_per_tile = a.p.tile / kPlaceSub, sub = blockIdx.x, tile = sub / subs_per_tile;
@@ -1105,7 +1105,7 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s)
     // choices 25.0 us -> 13.9, 96 experts and 4 choices 9.8 -> 6.3), a little later for one or two choices, which a wave finds in as many
     // rounds (4100 columns, 60 experts, one choice 4.3 against 6.0; 5000 5.8 and 6.0, 128 experts in groups 15 and 9), and with half of
     // that already for many choices from many experts (4096 columns 14.4 -> 11.5 with 256 experts, 11.9 -> 8.9 with 128, 30 -> 14 with
-    // 1024; 64 experts and four choices 5.8 against 6.3).
+    // 1024; 512 experts and 2048 columns 15.0 against 15.8, 64 and four choices 5.8 against 6.3).
     if (a.k <= 8 && a.groups <= kRouteLists) {
         if (a.batch > (a.k > 2 ? 16 : 18) * kComputeUnits)
             return a.k <= 2 ? route_columns_go<2>(a, keys, s) : a.k <= 4 ? route_columns_go<4>(a, keys, s) : route_columns_go<8>(a, keys, s);
