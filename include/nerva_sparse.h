@@ -302,7 +302,8 @@ int softmax_cross_entropy(const float *Z, int32_t ldz, const int32_t *labels,
  *     norm = sqrt( sum over all arrays and entries of grad^2 )      (added up in 64 bits)
  *     c    = min(1, max_norm / norm),                               max_norm > 0 (infinite: no clipping, only the norm)
  * gradient_norm leaves the norm in *norm_out.
- * gradient_clip writes clipped[t][k] = c * grads[t][k]; clipped[t] may be grads[t] itself.
+ * gradient_clip writes clipped[t][k] = c * grads[t][k]; clipped[t] may be grads[t] itself, which is multiplied by c once however
+ * often it is in the list (and counts as often in the norm).
  * sgd_update_clipped makes the step of sgd_update_values (nesterov == 0) or sgd_update_values_nesterov with c * grad in the
  * place of grad, on all arrays; an array that is in the list more than once is stepped as often, in the order of the list.
  * Where the norm is infinite or NaN (a gradient is, or the norm lies beyond fp32) no factor makes a usable step: the last two

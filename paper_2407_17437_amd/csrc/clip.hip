@@ -8,6 +8,8 @@
 // Squares are added up in 64 bits: the square of any fp32 number is exact there and in range (1e-90 ... 1e77), so the
 // norm neither overflows nor loses small entries beside large ones.  At 4 bytes read per entry the memory leaves some 80
 // cycles per wave and entry, which the conversion and the 64-bit multiply-add do not fill.
+#include <stdlib.h>
+#include <string.h>
 #include <type_traits>
 
 #include "device.h"
@@ -242,6 +244,31 @@ __global__ __launch_bounds__(kClipThreads) void clip_apply_kernel(const ApplyLis
 // whether arrays [a, a + n) and [b, b + m) share an entry
 bool overlap(const float *a, int64_t n, const float *b, int64_t m) { return a < b + m && b < a + n; }
 
+// Arrays met so far, by their addresses: a table with room for twice as many as may come, searched from where an address's hash says.
+struct Met {
+    static constexpr int64_t kInline = 512;   // (lists of up to 256 arrays: no heap memory)
+    const float *inline_[kInline], **table = inline_;
+    int64_t size = kInline;
+    Met() = default;
+    Met(const Met &) = delete;
+    ~Met() { if (table != inline_) free(table); }
+    bool reserve(int64_t most)
+    {
+        while (size < 2 * most) size *= 2;
+        if (size > kInline) table = static_cast<const float **>(malloc(static_cast<size_t>(size) * sizeof *table));
+        if (table) memset(table, 0, static_cast<size_t>(size) * sizeof *table);
+        else table = inline_;
+        return size == kInline || table != inline_;
+    }
+    // p's place, which holds p if it came before, else null until p is put there
+    const float **find(const float *p) const
+    {
+        int64_t i = static_cast<int64_t>(reinterpret_cast<uint64_t>(p) * UINT64_C(0x9E3779B97F4A7C15) >> 32) & (size - 1);
+        while (table[i] && table[i] != p) i = (i + 1) & (size - 1);
+        return table + i;
+    }
+};
+
 }  // namespace
 
 // Partial sums of all arrays; *n_partial receives how many there are, at most kPartialMost, from *partial on.
@@ -299,6 +326,12 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
 {
     int32_t n_partial = 0;
     double *partial = c.partial;
+    // Gradients that are clipped in place: where one comes again it is clipped already.
+    int64_t in_place = 0;
+    if (l.clipped)
+        for (int32_t t = 0; t < l.n; ++t) in_place += l.clipped[t] == l.grads[t];
+    Met met;
+    if (in_place > 0 && !met.reserve(in_place)) return hipErrorOutOfMemory;
     hipError_t e = launch_partial(l, &partial, &n_partial, s);
     if (e != hipSuccess) return e;
     if (n_partial == 0) return launch_finish(partial, 0, c.norm_out, s);
@@ -315,11 +348,14 @@ hipError_t launch_clipped(const ArrayList &l, const ClipArgs &c, hipStream_t s)
         for (; t < l.n && a.n < kApplyList; ++t) {
             const int64_t m = l.counts[t];
             if (m == 0) continue;
+            const float **first_time = in_place > 0 && out[t] == l.grads[t] ? met.find(out[t]) : nullptr;
+            if (first_time && *first_time) continue;
             // an array that is in the list twice is stepped twice, one launch after the other
             bool again = false;
             for (int32_t i = 0; i < a.n && !again; ++i)
                 again = overlap(a.a[i], a.counts[i], out[t], m) || (l.values && overlap(a.v[i], a.counts[i], l.velocities[t], m));
             if (again) break;
+            if (first_time) *first_time = out[t];
             a.a[a.n] = out[t];
             a.v[a.n] = l.values ? l.velocities[t] : nullptr;
             a.grads[a.n] = l.grads[t];
