@@ -48,7 +48,7 @@ constexpr int32_t kGroupsMax = 64;           // one per lane
 struct Placement {
     int32_t *filled;       // [experts] places that hold a column
     int32_t *listed;       // [tiles] entries with a place
-    int32_t *before;       // [subs * experts] choices of an expert per run of kPlaceSub columns
+    int32_t *before;       // [(subs + 1) * experts] choices of an expert in a run of kPlaceSub columns, then in all runs before it
     int2 *lists;           // [batch * k]: tile t's from t * tile * k on
     int32_t tile, tiles, subs;
     int64_t bytes;
@@ -67,7 +67,7 @@ inline Placement placement_of(void *memory, int32_t experts, int32_t batch, int3
     p.filled = reinterpret_cast<int32_t *>(p.lists + lists);
     p.listed = p.filled + experts;
     p.before = p.listed + p.tiles;
-    p.bytes = (8 * lists + 4 * (experts + p.tiles + static_cast<int64_t>(p.subs) * experts) + 15) / 16 * 16;
+    p.bytes = (8 * lists + 4 * (experts + p.tiles + (static_cast<int64_t>(p.subs) + 1) * experts) + 15) / 16 * 16;
     return p;
 }
 

@@ -630,6 +630,13 @@ constexpr int kPlaceCounts = 4096;
 // 8.4 us against 2.4 + 6.4 and the gap between two launches, 1024 with 8 choices 15.8 against 4.7 + 10.3.
 __host__ __device__ inline bool counts_itself(const PlaceArgs &a) { return a.batch * a.k <= kPlaceCounts; }
 
+constexpr int kPlaceSums = 8192;
+// Whether the counts of all runs are added up once, by a launch of its own, and not by every work-group for those before its own. That launch takes 2
+// to 3 us (8192 columns and 2 choices of 8 experts 10.2 us against 7.0, 4 of 64 13.8 against 11.6), and adding up in every work-group takes time
+// by the square of the columns: 8192 columns and 8 choices of 256 experts 19.8 us -> 18.8, 32768 and 4 of 64 15.1 -> 14.4, 65536 and 8 of 256 55 -> 23,
+// 2^20 and one of 256 1300 -> 75.
+__host__ __device__ inline bool sums_ahead(const PlaceArgs &a) { return !counts_itself(a) && static_cast<int64_t>(a.p.subs) * a.experts >= kPlaceSums; }
+
 // choices of every expert in one run of kPlaceSub columns
 __global__ __launch_bounds__(kPlaceThreads) void place_count_kernel(const PlaceArgs a)
 {
@@ -643,6 +650,46 @@ __global__ __launch_bounds__(kPlaceThreads) void place_count_kernel(const PlaceA
     }
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += kPlaceThreads) a.p.before[static_cast<int64_t>(blockIdx.x) * a.experts + e] = n[e];
+}
+
+// Those counts to the numbers of choices in the runs before, with the totals behind the last run: a work-group has 64 experts, its waves one
+// stretch of runs each, which they read for its sum and again for the numbers themselves.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kSumWaves * kWave) void place_sum_kernel(const PlaceArgs a)
+{
+    __shared__ int32_t sums[kSumWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
+    const int e = blockIdx.x * kWave + lane, own = min(e, a.experts - 1);
+    const int per = (a.p.subs + kSumWaves - 1) / kSumWaves;
+    const int from = min(wv * per, a.p.subs), to = min(from + per, a.p.subs);
+    int32_t *n = a.p.before + own;
+    const int64_t E = a.experts;
+    constexpr int U = 16;   // counts in flight
+    int sum = 0;
+    for (int q = from; q < to; q += U) {
+        int32_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = n[min(q + u, to - 1) * E];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += q + u < to ? x[u] : 0;
+    }
+    sums[wv][lane] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int w = 0; w < wv; ++w) sum += sums[w][lane];
+    if (e >= a.experts) return;
+    for (int q = from; q < to; q += U) {
+        int32_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = n[min(q + u, to - 1) * E];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (q + u >= to) break;
+            n[(q + u) * E] = sum;
+            sum += x[u];
+        }
+    }
+    if (wv == kSumWaves - 1) n[a.p.subs * E] = sum;   // (a stretch may be empty: the last wave's sum is that of all)
 }
 
 // exclusive scans of N numbers over the work-group's threads; total: their sums
@@ -692,7 +739,7 @@ __device__ __forceinline__ void set_turns(int2 *list, int i, int kept)
 }
 
 // Places of one run of kPlaceSub columns.  A choice's place is the number of choices of its expert before it, in the order of columns
-// and, in a column, of choices: those of the runs before (added up here from their counts), of the run's earlier rounds of one choice per
+// and, in a column, of choices: those of the runs before (added up before this launch or here), of the run's earlier rounds of one choice per
 // thread, of the waves before in the round, and of the lanes before in the wave (the lanes that hold the same expert, from one
 // ballot per bit of its number).
 __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
@@ -711,27 +758,37 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(const PlaceArgs a)
     // choices per expert: before the tile, in the tile, and in its runs before this one
     int32_t *before = by_wave, *inside = by_wave + E1, *mine = by_wave + 2 * E1;
     static_assert(kPlaceWaves >= 3, "room for them");
-    for (int i = threadIdx.x; i < 3 * E1; i += kPlaceThreads) by_wave[i] = 0;
-    __syncthreads();
-    auto add = [&](int q, int e, int n) {   // n choices of expert e in run q
-        if (q < tile_sub) {
-            atomicAdd(&before[e], n);
-        } else if (q < tile_end) {
-            atomicAdd(&inside[e], n);
-            if (q < sub) atomicAdd(&mine[e], n);
-        }
-    };
-    if (counts_itself(a)) {
-        for (int i = threadIdx.x; i < a.batch * a.k; i += kPlaceThreads) {
-            const int j = i / a.batch, c = i - j * a.batch;
-            add(c / kPlaceSub, expert_at(a, c, j), 1);
+    if (!sums_ahead(a)) {
+        for (int i = threadIdx.x; i < 3 * E1; i += kPlaceThreads) by_wave[i] = 0;
+        __syncthreads();
+        auto add = [&](int q, int e, int n) {   // n choices of expert e in run q
+            if (q < tile_sub) {
+                atomicAdd(&before[e], n);
+            } else if (q < tile_end) {
+                atomicAdd(&inside[e], n);
+                if (q < sub) atomicAdd(&mine[e], n);
+            }
+        };
+        if (counts_itself(a)) {
+            for (int i = threadIdx.x; i < a.batch * a.k; i += kPlaceThreads) {
+                const int j = i / a.batch, c = i - j * a.batch;
+                add(c / kPlaceSub, expert_at(a, c, j), 1);
+            }
+        } else {
+            const int n = tile_end * E;   // (at most kPlaceSums)
+#pragma unroll 4
+            for (int i = threadIdx.x; i < n; i += kPlaceThreads) {
+                const int q = i / E;
+                add(q, i - q * E, a.p.before[i]);
+            }
         }
     } else {
-        const int64_t n = static_cast<int64_t>(tile_end) * E;
-#pragma unroll 4
-        for (int64_t i = threadIdx.x; i < n; i += kPlaceThreads) {
-            const int q = static_cast<int>(i / E);
-            add(q, static_cast<int>(i - static_cast<int64_t>(q) * E), a.p.before[i]);
+        for (int e = threadIdx.x; e < E; e += kPlaceThreads) {
+            const int32_t *n = a.p.before + e;
+            const int at_tile = n[static_cast<int64_t>(tile_sub) * E];
+            before[e] = at_tile;
+            inside[e] = n[static_cast<int64_t>(tile_end) * E] - at_tile;
+            mine[e] = n[static_cast<int64_t>(sub) * E] - at_tile;
         }
     }
     __syncthreads();
@@ -1152,6 +1209,11 @@ hipError_t launch_place(const PlaceArgs &a, hipStream_t s)
 {
     if (!counts_itself(a)) {
         hipLaunchKernelGGL(place_count_kernel, dim3(a.p.subs), dim3(kPlaceThreads), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (sums_ahead(a)) {
+        hipLaunchKernelGGL(place_sum_kernel, dim3((a.experts + kWave - 1) / kWave), dim3(kSumWaves * kWave), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

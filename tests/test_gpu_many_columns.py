@@ -1,0 +1,84 @@
+"""Places of many columns in the experts' blocks."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nb():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2407_17437_amd import binding
+    return binding
+
+
+def places(chosen, experts, capacity):
+    """slots and counts: choices sorted by expert, stably, in the order of columns and then of choices."""
+    k, batch = chosen.shape
+    flat = chosen.T.reshape(-1).astype(np.int64)
+    flat = np.where((flat >= 0) & (flat < experts), flat, experts)
+    order = np.argsort(flat, kind="stable")
+    counts = np.bincount(flat, minlength=experts + 1)
+    first = np.cumsum(counts) - counts
+    place = np.empty_like(flat)
+    place[order] = np.arange(flat.size) - first[flat[order]]
+    place[(place >= capacity) | (flat == experts)] = -1
+    return place.reshape(batch, k).T.astype(np.int32), counts[:experts].astype(np.int32)
+
+
+@pytest.mark.parametrize("E,B,k,C", [(64, 200_001, 1, 3000), (1000, 70_000, 3, 211), (3, 100_000, 2, 90_000), (256, 1 << 18, 2, 2048), (7, 4097, 1, 400), (65, 1400, 3, 50),
+                                     (1, 300_000, 1, 250_000), (1024, 33_000, 32, 1000),
+                                     (256, 8192, 3, 90), (255, 8192, 3, 90), (256, 7936, 1, 40)])
+@pytest.mark.parametrize("kind", ["any", "one expert", "by turns"])
+def test_places_of_many_columns(nb, E, B, k, C, kind):
+    import torch
+    rng = np.random.default_rng(E + B)
+    if kind == "any":
+        chosen = rng.integers(-1, E + 1, (k, B)).astype(np.int32)      # twice the same, and none (-1 and E)
+    elif kind == "one expert":
+        chosen = np.full((k, B), E - 1, np.int32)
+    else:                                                              # experts that fill up one after the other, along the batch
+        chosen = np.minimum(np.arange(B) * E // B, E - 1)[None].repeat(k, 0).astype(np.int32)
+    slots, counts = places(chosen, E, C)
+    sd, nd = torch.full((k, B), 7, dtype=torch.int32, device="cuda"), torch.zeros(E, dtype=torch.int32, device="cuda")
+    room = nb.expert_placement_bytes(E, B, k) // 4
+    placement = torch.full((room + 64,), -77, dtype=torch.int32, device="cuda")
+    nb.expert_place(torch.as_tensor(chosen).cuda(), E, B, k, C, sd, nd, placement[:room])
+    assert np.array_equal(nd.cpu().numpy(), counts) and np.array_equal(sd.cpu().numpy(), slots)
+    assert (placement[room:] == -77).all()
+    # the lists, through the calls that read them: every place holds its column, every column finds its places
+    F = 2
+    X = torch.as_tensor(rng.integers(-1000, 1000, (F, B)).astype(np.float32)).cuda()
+    Xe, Y = torch.full((E, F, C), float("nan"), device="cuda"), torch.empty(F, B, device="cuda")
+    nb.expert_dispatch(X, placement, F, E, B, k, C, Xe)
+    nb.expert_combine(Xe, placement, None, F, E, B, k, C, Y)
+    kept = torch.as_tensor(slots >= 0).cuda()
+    j, c = torch.nonzero(kept, as_tuple=True)
+    e, s = torch.as_tensor(chosen).cuda()[j, c].long(), sd[j, c].long()
+    want = torch.zeros(E, F, C, device="cuda")
+    want[e, :, s] = X[:, c].t()
+    assert torch.equal(Xe, want)
+    assert torch.equal(Y, X * kept.sum(0))                             # (small whole numbers: exact)
+
+
+def test_time_of_places_grows_with_the_columns(nb):
+    """Four times as many columns take about four times as long, and would take sixteen times as long if each run of columns went
+    through all runs before it; between them is twice four."""
+    import torch
+    E, k, C = 256, 1, 1 << 22
+    times = []
+    for B in (1 << 20, 1 << 22):
+        chosen = torch.randint(0, E, (k, B), device="cuda", dtype=torch.int32)
+        placement = torch.empty(nb.expert_placement_bytes(E, B, k) // 4, dtype=torch.int32, device="cuda")
+        one = []
+        for _ in range(7):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            nb.expert_place(chosen, E, B, k, C, None, None, placement)
+            b.record()
+            b.synchronize()
+            one.append(a.elapsed_time(b))
+        times.append(sorted(one)[3])
+    print("ms:", times, flush=True)
+    assert times[1] < 8 * times[0], times
