@@ -2110,6 +2110,16 @@ int mlp_train_step_clipped(nerva_mlp *mlp, const float *X, int32_t ldx, const in
 
 // ---- mixtures -----------------------------------------------------------------------------------
 
+// result of a launch: one of too many threads is refused for its sizes
+static int launched(hipError_t e, const char *what, int32_t batch)
+{
+    if (e == hipErrorInvalidConfiguration) {
+        (void)hipGetLastError();
+        return fail(NERVA_ERR_SHAPE, "%s: %d columns of these sizes take more threads than a launch holds", what, batch);
+    }
+    return e == hipSuccess ? static_cast<int>(NERVA_OK) : hip_fail(e, what);
+}
+
 static int check_experts(int32_t experts, int32_t batch, int32_t k, int32_t ldk)
 {
     if (experts < 1 || experts > kExpertsMax) return fail(NERVA_ERR_ARGUMENT, "experts = %d is not in 1 .. %d", experts, kExpertsMax);
@@ -2141,8 +2151,7 @@ int expert_route(const float *Z, int32_t ldz, const float *bias, int32_t experts
     if (k > experts / groups * top_groups) return fail(NERVA_ERR_ARGUMENT, "%d choices among %d experts", k, experts / groups * top_groups);
     if (groups == 1) flags &= ~NERVA_EXPERT_GROUP_PAIR;   // (all experts are one group: no score to form)
     const RouteArgs a{Z, ldz, bias, experts, batch, k, groups, top_groups, flags, scale, chosen, weights, ldk};
-    HIP_TRY(launch_route(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_route(a, as_stream(stream)), "expert_route", batch);
 }
 
 int expert_route_backward(const float *Z, int32_t ldz, const int32_t *chosen, const float *dweights, int32_t ldk, int32_t experts,
@@ -2154,8 +2163,7 @@ int expert_route_backward(const float *Z, int32_t ldz, const int32_t *chosen, co
     if (rc == NERVA_OK) rc = check_batch(batch, lddz, "lddz");
     if (rc != NERVA_OK) return rc;
     const RouteBackwardArgs a{Z, ldz, chosen, dweights, ldk, experts, batch, k, flags, scale, dZ, lddz};
-    HIP_TRY(launch_route_backward(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_route_backward(a, as_stream(stream)), "expert_route_backward", batch);
 }
 
 size_t expert_placement_bytes(int32_t experts, int32_t batch, int32_t k)
@@ -2183,8 +2191,7 @@ int expert_place(const int32_t *chosen, int32_t ldk, int32_t experts, int32_t ba
     int rc = check_experts(experts, batch, k, ldk);
     if (rc == NERVA_OK) rc = check_placement(placement, placement_bytes, experts, batch, k, capacity, a.p);
     if (rc != NERVA_OK) return rc;
-    HIP_TRY(launch_place(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_place(a, as_stream(stream)), "expert_place", batch);
 }
 
 static int check_exchange(ExchangeArgs &a, const void *placement, size_t placement_bytes, int32_t ldc, const char *ldc_name, int32_t ldb)
@@ -2211,8 +2218,7 @@ int expert_dispatch(const float *X, int32_t ldx, const void *placement, size_t p
     a.features = features; a.experts = experts; a.batch = batch; a.k = k; a.capacity = capacity;
     const int rc = check_exchange(a, placement, placement_bytes, ldx, "ldx", lde);
     if (rc != NERVA_OK) return rc;
-    HIP_TRY(launch_dispatch(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_dispatch(a, as_stream(stream)), "expert_dispatch", batch);
 }
 
 int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t placement_bytes, const float *weights, int32_t ldk,
@@ -2225,8 +2231,7 @@ int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t p
     int rc = check_exchange(a, placement, placement_bytes, ldy, "ldy", lde);
     if (rc == NERVA_OK && weights) rc = check_batch(batch, ldk, "ldk");
     if (rc != NERVA_OK) return rc;
-    HIP_TRY(launch_combine(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_combine(a, as_stream(stream)), "expert_combine", batch);
 }
 
 size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k)
@@ -2255,8 +2260,7 @@ int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32
         if (workspace_bytes < need) return fail(NERVA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
         a.partial = static_cast<float *>(workspace);
     }
-    HIP_TRY(launch_combine_backward(a, as_stream(stream)));
-    return NERVA_OK;
+    return launched(launch_combine_backward(a, as_stream(stream)), "expert_combine_backward", batch);
 }
 
 int nerva_copy_f32(float *dst, const float *src, int64_t n, void *stream)

@@ -7,6 +7,7 @@
 namespace nerva {
 
 // ---- routing (experts.hip) ----------------------------------------------------------------
+// The launches of mixtures return hipErrorInvalidConfiguration, with nothing launched, where one of them would take 2^32 threads or more.
 struct RouteArgs {
     const float *Z;
     int64_t ldz;

@@ -577,10 +577,14 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
     }
 }
 
+// A launch holds fewer than 2^32 threads.  What needs more is refused before the first launch of a call.
+bool fits_launch(int64_t blocks, int64_t threads) { return blocks * threads < (INT64_C(1) << 32); }
+
 template <int R>
 hipError_t route_go(const RouteArgs &a, Keys keys, int cols, int waves, size_t lds, hipStream_t s)
 {
     const dim3 grid((a.batch + cols - 1) / cols), block(waves * kWave);
+    if (!fits_launch(grid.x, block.x)) return hipErrorInvalidConfiguration;
     if (keys == kLogits) hipLaunchKernelGGL((route_kernel<R, kLogits>), grid, block, lds, s, a, cols);
     else if (keys == kSigmoids) hipLaunchKernelGGL((route_kernel<R, kSigmoids>), grid, block, lds, s, a, cols);
     else hipLaunchKernelGGL((route_kernel<R, kSoftmaxes>), grid, block, lds, s, a, cols);
@@ -598,6 +602,7 @@ hipError_t route_columns_of(const RouteArgs &a, Keys keys, hipStream_t s)
     const int size = (group_size + parts - 1) / parts, lists = a.groups * parts, takers = lists < 4 ? 4 : lists;
     const size_t lds = (static_cast<size_t>(lists) * K + takers) * kCols * 8 + (K + takers) * kCols * 4;
     const dim3 grid((a.batch + kCols - 1) / kCols), block(takers * kCols);
+    if (!fits_launch(grid.x, block.x)) return hipErrorInvalidConfiguration;
     if (keys == kLogits) hipLaunchKernelGGL((route_columns_kernel<K, kCols, kLogits>), grid, block, lds, s, a, lists, parts, size);
     else if (keys == kSigmoids) hipLaunchKernelGGL((route_columns_kernel<K, kCols, kSigmoids>), grid, block, lds, s, a, lists, parts, size);
     else hipLaunchKernelGGL((route_columns_kernel<K, kCols, kSoftmaxes>), grid, block, lds, s, a, lists, parts, size);
@@ -1148,8 +1153,9 @@ hipError_t dispatch_go(const ExchangeArgs &a, hipStream_t s)
     // caches 64 lanes read 64 lines.
     const size_t lds = kRows * width * sizeof(float), with_weights = lds + static_cast<size_t>(width) * a.k * sizeof(float);
     const bool staged = kGrad && a.weights && a.out_blocks && with_weights <= kMoveLds;
-    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), dim3(threads), staged ? with_weights : lds, s, a,
-                       staged ? 1 : 0);
+    const uint32_t blocks = whole_eights(static_cast<int64_t>(groups) * a.p.tiles);
+    if (!fits_launch(blocks, threads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((dispatch_kernel<kRows, kGrad>), dim3(blocks), dim3(threads), staged ? with_weights : lds, s, a, staged ? 1 : 0);
     return hipGetLastError();
 }
 
@@ -1185,24 +1191,25 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s)
 }
 
 template <int K>
-static void route_backward_go(const RouteBackwardArgs &a, hipStream_t s)
+static hipError_t route_backward_go(const RouteBackwardArgs &a, hipStream_t s)
 {
     int waves = a.experts / kBackRows;
     waves = waves < 4 ? 4 : waves > kBackWaves ? kBackWaves : waves;
     const dim3 grid((a.batch + kWave - 1) / kWave), block(waves * kWave);
+    if (!fits_launch(grid.x, block.x)) return hipErrorInvalidConfiguration;
     if (a.flags & (NERVA_EXPERT_SIGMOID | NERVA_EXPERT_RENORMALISE)) hipLaunchKernelGGL((route_backward_kernel<K, false>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((route_backward_kernel<K, true>), grid, block, 0, s, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_route_backward(const RouteBackwardArgs &a, hipStream_t s)
 {
-    if (a.k <= 1) route_backward_go<1>(a, s);
-    else if (a.k <= 2) route_backward_go<2>(a, s);
-    else if (a.k <= 4) route_backward_go<4>(a, s);
-    else if (a.k <= 8) route_backward_go<8>(a, s);
-    else if (a.k <= 16) route_backward_go<16>(a, s);
-    else route_backward_go<32>(a, s);
-    return hipGetLastError();
+    if (a.k <= 1) return route_backward_go<1>(a, s);
+    if (a.k <= 2) return route_backward_go<2>(a, s);
+    if (a.k <= 4) return route_backward_go<4>(a, s);
+    if (a.k <= 8) return route_backward_go<8>(a, s);
+    if (a.k <= 16) return route_backward_go<16>(a, s);
+    return route_backward_go<32>(a, s);
 }
 
 hipError_t launch_place(const PlaceArgs &a, hipStream_t s)
@@ -1230,7 +1237,8 @@ hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s)
     // All that the work-groups of one XCD write at a time should stay in its L2 until the neighbouring tile has filled the lines up.
     int most = 16;
     while (most > 4 && most * a.p.tile * a.k > 8192) most /= 2;
-    const int rows = move_rows(a.features, a.p.tiles, most);
+    int rows = move_rows(a.features, a.p.tiles, most);
+    while (rows < 16 && !fits_launch(static_cast<int64_t>((a.features + rows - 1) / rows) * a.p.tiles + 7, kMoveThreads)) rows *= 2;   // (2^32 entries and more)
     return rows == 16 ? dispatch_go<16, false>(a, s) : rows == 8 ? dispatch_go<8, false>(a, s) : dispatch_go<4, false>(a, s);
 }
 
@@ -1241,6 +1249,7 @@ static hipError_t combine_go(const ExchangeArgs &a, hipStream_t s)
     const int groups = (a.features + per_block - 1) / per_block, width = pitch_of(a.batch, a.p.tile);
     const dim3 grid(whole_eights(static_cast<int64_t>(groups) * a.p.tiles)), block(kWaves * kWave);
     const size_t lds = per_block * width * sizeof(float), with_weights = lds + static_cast<size_t>(width) * a.k * sizeof(float);
+    if (!fits_launch(grid.x, block.x)) return hipErrorInvalidConfiguration;
     if (!a.weights) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kAllOne>), grid, block, lds, s, a);
     else if (with_weights <= kCombineLds) hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kStaged>), grid, block, with_weights, s, a);
     else hipLaunchKernelGGL((combine_kernel<kRows, kWaves, kGathered>), grid, block, lds, s, a);
@@ -1257,11 +1266,11 @@ hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s)
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s)
 {
     const int rows = move_rows(a.features, a.p.tiles, 16);   // (at least partial_rows, which the workspace has room for)
+    const int64_t sums = (static_cast<int64_t>(a.batch) * a.k + kWave - 1) / kWave;   // work-groups of the second launch
+    if (a.dweights && !fits_launch(sums, kGradWaves * kWave)) return hipErrorInvalidConfiguration;
     const hipError_t e = rows == 16 ? dispatch_go<16, true>(a, s) : rows == 8 ? dispatch_go<8, true>(a, s) : dispatch_go<4, true>(a, s);
     if (e != hipSuccess || !a.dweights) return e;
-    const int64_t total = static_cast<int64_t>(a.batch) * a.k;
-    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>((total + kWave - 1) / kWave)), dim3(kGradWaves * kWave), 0, s, a,
-                       (a.features + rows - 1) / rows);
+    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>(sums)), dim3(kGradWaves * kWave), 0, s, a, (a.features + rows - 1) / rows);
     return hipGetLastError();
 }
 

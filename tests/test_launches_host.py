@@ -1,0 +1,124 @@
+"""The launches of mixtures and of the clipped training step, from the host's side: the library runs on a HIP runtime without a GPU
+(fake_launches.cpp), each test in a process of its own."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+sys.path.insert(0, HERE)
+
+from test_host_memory import Library  # noqa: E402
+
+OK, ARGUMENT, SHAPE, WORKSPACE, HIP = 0, -1, -2, -3, -5
+P = 1 << 20   # an address that is aligned and never read
+
+
+def library(fake):
+    L = Library(fake)
+    for name in ("expert_placement_bytes", "expert_combine_workspace_bytes", "mlp_clipped_workspace_bytes"):
+        getattr(L.lib, name).restype = ctypes.c_size_t
+    return L
+
+
+def refused_or_launched(L, call, refused):
+    before = L.hip.fake_launches()
+    rc = call()
+    launched = L.hip.fake_launches() - before
+    assert L.hip.fake_too_large() == 0, "a launch of more threads than there may be"
+    if refused:
+        assert rc == SHAPE and launched == 0, (rc, launched, L.lib.nerva_last_error())
+        assert b"columns" in L.lib.nerva_last_error()
+    else:
+        assert rc == OK and launched > 0, (rc, L.lib.nerva_last_error())
+
+
+def a_call_that_no_launch_holds_is_refused_before_the_first(L):
+    """Columns and choices that the documented ranges allow, to both sides of 2^32 threads."""
+    p = ctypes.c_void_p(P)
+    f = ctypes.c_float
+
+    def route(batch, experts, k, groups, top, flags=0, bias=False):
+        return lambda: L.lib.expert_route(p, batch, p if bias else None, experts, batch, k, groups, top, flags, f(1), p, p, batch, None)
+
+    def route_backward(batch, experts, k, flags):
+        return lambda: L.lib.expert_route_backward(p, batch, p, p, batch, experts, batch, k, flags, f(1), p, batch, None)
+
+    # a wave per column, 32 threads a column; a few experts more, 64
+    refused_or_launched(L, route(1 << 27, 32, 1, 32, 1), True)
+    refused_or_launched(L, route((1 << 27) - 32, 32, 1, 32, 1), False)
+    refused_or_launched(L, route((1 << 27) - 31, 32, 1, 32, 1), True)
+    refused_or_launched(L, route(1 << 26, 64 * 9, 1, 64, 1, bias=True), True)
+    refused_or_launched(L, route((1 << 26) - 16, 64 * 9, 1, 64, 1, bias=True), False)
+    # a lane per column, 16 threads a column
+    for flags in (0, 1, 2):
+        refused_or_launched(L, route(1 << 28, 128, 2, 1, 1, flags), True)
+        refused_or_launched(L, route((1 << 28) - 64, 128, 2, 1, 1, flags), False)
+    refused_or_launched(L, route((1 << 29) - 1, 8, 1, 1, 1), False)      # (few lists)
+    for flags in (0, 1, 2):
+        refused_or_launched(L, route_backward(1 << 28, 128, 1, flags), True)
+        refused_or_launched(L, route_backward((1 << 28) - 64, 128, 1, flags), False)
+        refused_or_launched(L, route_backward((1 << 30) - 64, 8, 1, flags), False)      # (four threads a column)
+
+    def place(batch, experts, k, capacity):
+        n = L.lib.expert_placement_bytes(experts, batch, k)
+        assert n > 0
+        return lambda: L.lib.expert_place(p, batch, experts, batch, k, capacity, p, p, p, ctypes.c_size_t(n), None)
+
+    for batch, experts, k in (((1 << 30) - 1, 1, 1), ((1 << 30) - 1, 1024, 1), ((1 << 25) - 1, 1024, 32), ((1 << 25) - 1, 2, 32), ((1 << 30) // 3 - 1, 4, 3)):
+        refused_or_launched(L, place(batch, experts, k, 1000), False)
+
+    def exchange(which, batch, experts, k, features, capacity=1000, weights=True, dye=True, dw=True):
+        n = L.lib.expert_placement_bytes(experts, batch, k)
+        room = L.lib.expert_combine_workspace_bytes(features, batch, k)
+        w = p if weights else None
+        n, room = ctypes.c_size_t(n), ctypes.c_size_t(room)
+        if which == "dispatch":
+            return lambda: L.lib.expert_dispatch(p, batch, p, n, features, experts, batch, k, capacity, p, capacity, None)
+        if which == "combine":
+            return lambda: L.lib.expert_combine(p, capacity, p, n, w, batch, features, experts, batch, k, capacity, p, batch, None)
+        return lambda: L.lib.expert_combine_backward(p, capacity, p, batch, p, n, w, batch, features, experts, batch, k, capacity, p if dye else None, p if dw else None,
+                                                     p, room, None)
+
+    # gradients of the weights: 8 threads a choice, behind a launch that writes the blocks
+    for dye in (True, False):
+        refused_or_launched(L, exchange("backward", 1 << 29, 2, 1, 1, dye=dye), True)
+        refused_or_launched(L, exchange("backward", (1 << 29) - 64, 2, 1, 1, dye=dye), False)
+    refused_or_launched(L, exchange("backward", 1 << 29, 2, 1, 1, dw=False), False)
+    refused_or_launched(L, exchange("backward", (1 << 24) - 2, 8, 32, 4, dye=False), False)
+    # rows of columns to blocks and back: 4 entries a thread at least, where tiles and groups of rows are full
+    for batch, experts, k, features in ((1 << 20, 8, 8, 4096), (1 << 20, 64, 8, 8191), (1 << 21, 8, 8, 4095), (1 << 19, 8, 32, 16383), (257, 8, 32, (1 << 24) - 1),
+                                        (511, 64, 8, (1 << 24) - 1), ((1 << 25) + 1, 8, 1, 255), ((1 << 26) - 1, 8, 7, 127)):
+        assert features * batch < 1 << 33 and batch * k < 1 << 29
+        for which in ("dispatch", "combine", "backward"):
+            refused_or_launched(L, exchange(which, batch, experts, k, features), False)
+    refused_or_launched(L, exchange("dispatch", 1 << 22, 8, 4, 4096), True)
+    refused_or_launched(L, exchange("dispatch", (1 << 22) - 2048, 8, 4, 4096), False)
+    refused_or_launched(L, exchange("backward", 1 << 22, 8, 4, 4096), True)
+    refused_or_launched(L, exchange("combine", 1 << 22, 8, 4, 4096), False)
+    for weights in (True, False):
+        refused_or_launched(L, exchange("combine", 1 << 22, 8, 4, 1 << 14, weights=weights), True)
+        refused_or_launched(L, exchange("combine", (1 << 22) - 256, 8, 4, 1 << 14, weights=weights), False)
+
+
+CASES = [a_call_that_no_launch_holds_is_refused_before_the_first]
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("hip") / "fake_launches.so")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-isystem", "/opt/rocm/include",
+                    os.path.join(HERE, "fake_launches.cpp"), "-o", out], check=True)
+    return out
+
+
+@pytest.mark.parametrize("case", [c.__name__ for c in CASES])
+def test_launches(fake, case):
+    run = subprocess.run([sys.executable, os.path.abspath(__file__), fake, case], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0, run.stdout + run.stderr
+
+
+if __name__ == "__main__":
+    globals()[sys.argv[2]](library(sys.argv[1]))
