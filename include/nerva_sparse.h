@@ -387,7 +387,8 @@ int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t p
  *     dYe[e, f, place] = weights[j, c] * dY[f, c], 0 in places that hold no column      (skipped if NULL)
  *     dweights[j, c]   = sum_f Ye[e, f, place] * dY[f, c], 0 for choices without a place (skipped if NULL)
  * Ye and dYe have the same lde; dweights has the ldk of weights.  workspace: device scratch, 16-byte aligned, of
- * expert_combine_workspace_bytes(), for dweights (may be NULL without). */
+ * expert_combine_workspace_bytes(), for dweights (may be NULL without).  (expert_combine_workspace_bytes is 0 for a batch, k or features that are
+ * refused.) */
 size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k);
 int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32_t lddy, const void *placement,
                             size_t placement_bytes, const float *weights, int32_t ldk, int32_t features, int32_t experts,

@@ -2110,12 +2110,17 @@ int mlp_train_step_clipped(nerva_mlp *mlp, const float *X, int32_t ldx, const in
 
 // ---- mixtures -----------------------------------------------------------------------------------
 
+static int too_many_threads(const char *what, int32_t batch)
+{
+    return fail(NERVA_ERR_SHAPE, "%s: %d columns of these sizes take more threads than a launch holds", what, batch);
+}
+
 // result of a launch: one of too many threads is refused for its sizes
 static int launched(hipError_t e, const char *what, int32_t batch)
 {
     if (e == hipErrorInvalidConfiguration) {
         (void)hipGetLastError();
-        return fail(NERVA_ERR_SHAPE, "%s: %d columns of these sizes take more threads than a launch holds", what, batch);
+        return too_many_threads(what, batch);
     }
     return e == hipSuccess ? static_cast<int>(NERVA_OK) : hip_fail(e, what);
 }
@@ -2194,6 +2199,14 @@ int expert_place(const int32_t *chosen, int32_t ldk, int32_t experts, int32_t ba
     return launched(launch_place(a, as_stream(stream)), "expert_place", batch);
 }
 
+// one work-group per tile of columns and few rows
+static int check_features(int32_t features, int32_t batch, int32_t tiles)
+{
+    if (features <= 0) return fail(NERVA_ERR_ARGUMENT, "features must be positive (got %d)", features);
+    if (static_cast<int64_t>(features) * (static_cast<int64_t>(tiles) + 1) > INT32_MAX) return fail(NERVA_ERR_SHAPE, "%d features of %d columns are not supported", features, batch);
+    return NERVA_OK;
+}
+
 static int check_exchange(ExchangeArgs &a, const void *placement, size_t placement_bytes, int32_t ldc, const char *ldc_name, int32_t ldb)
 {
     if (a.features <= 0) return fail(NERVA_ERR_ARGUMENT, "features must be positive (got %d)", a.features);
@@ -2202,8 +2215,7 @@ static int check_exchange(ExchangeArgs &a, const void *placement, size_t placeme
     if (rc == NERVA_OK) rc = check_batch(a.batch, ldc, ldc_name);
     if (rc != NERVA_OK) return rc;
     if (ldb < a.capacity || ldb >= (1 << 30)) return fail(NERVA_ERR_SHAPE, "lde = %d does not hold a capacity of %d", ldb, a.capacity);
-    // one work-group per tile of columns and few rows
-    if (static_cast<int64_t>(a.features) * (a.p.tiles + 1) > INT32_MAX) return fail(NERVA_ERR_SHAPE, "%d features of %d columns are not supported", a.features, a.batch);
+    if ((rc = check_features(a.features, a.batch, a.p.tiles)) != NERVA_OK) return rc;
     a.ldc = ldc;
     a.ldb = ldb;
     return NERVA_OK;
@@ -2236,7 +2248,12 @@ int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t p
 
 size_t expert_combine_workspace_bytes(int32_t features, int32_t batch, int32_t k)
 {
-    if (features <= 0 || batch <= 0 || k < 1 || k > kChoicesMax) return 0;
+    if (check_experts(1, batch, k, batch) != NERVA_OK) return 0;
+    if (!fits_launch(weight_gradient_blocks(batch, k), kGradThreads)) {
+        (void)too_many_threads("expert_combine_backward", batch);
+        return 0;
+    }
+    if (check_features(features, batch, (batch + kPlaceTileMax - 1) / kPlaceTileMax) != NERVA_OK) return 0;
     const int32_t rows = partial_rows(features, batch);
     return static_cast<size_t>((features + rows - 1) / rows) * static_cast<size_t>(batch) * static_cast<size_t>(k) * 4;
 }

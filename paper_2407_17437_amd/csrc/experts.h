@@ -7,7 +7,10 @@
 namespace nerva {
 
 // ---- routing (experts.hip) ----------------------------------------------------------------
-// The launches of mixtures return hipErrorInvalidConfiguration, with nothing launched, where one of them would take 2^32 threads or more.
+// A launch holds fewer than 2^32 threads.  Those of mixtures return hipErrorInvalidConfiguration, with nothing launched, where one of them would
+// take more.
+inline bool fits_launch(int64_t blocks, int64_t threads) { return blocks * threads < (INT64_C(1) << 32); }
+
 struct RouteArgs {
     const float *Z;
     int64_t ldz;
@@ -107,6 +110,9 @@ inline int32_t move_rows(int32_t features, int64_t tiles, int32_t most)
 // The fewest that the combine's backward pass takes, whose products over so many rows make one entry of `partial`: the workspace is asked for without
 // the experts, and with them there may be more tiles.
 inline int32_t partial_rows(int32_t features, int32_t batch) { return move_rows(features, (batch + kPlaceTileMax - 1) / kPlaceTileMax, 16); }
+// work-groups that form the gradients of the weights, one for 64 choices
+constexpr int32_t kGradThreads = 512;
+inline int64_t weight_gradient_blocks(int32_t batch, int32_t k) { return (static_cast<int64_t>(batch) * k + 63) / 64; }
 hipError_t launch_dispatch(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s);
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s);

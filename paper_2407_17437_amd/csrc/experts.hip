@@ -577,9 +577,6 @@ __global__ __launch_bounds__(kBackWaves * kWave) void route_backward_kernel(cons
     }
 }
 
-// A launch holds fewer than 2^32 threads.  What needs more is refused before the first launch of a call.
-bool fits_launch(int64_t blocks, int64_t threads) { return blocks * threads < (INT64_C(1) << 32); }
-
 template <int R>
 hipError_t route_go(const RouteArgs &a, Keys keys, int cols, int waves, size_t lds, hipStream_t s)
 {
@@ -1005,11 +1002,11 @@ __global__ __launch_bounds__(kMoveThreads) void dispatch_kernel(const ExchangeAr
     }
 }
 
-// Gradients of the weights from the products of every group of rows: a wave adds up every kGradWaves-th group for 64 entries, and
+// Gradients of the weights from the products of every group of rows: a wave adds up every eighth group for 64 entries, and
 // the waves' sums are added in their order.
-constexpr int kGradWaves = 8;
-__global__ __launch_bounds__(kGradWaves * kWave) void weight_gradient_kernel(const ExchangeArgs a, const int groups)
+__global__ __launch_bounds__(kGradThreads) void weight_gradient_kernel(const ExchangeArgs a, const int groups)
 {
+    constexpr int kGradWaves = kGradThreads / kWave;
     __shared__ double sums[kGradWaves][kWave];
     const int lane = threadIdx.x & (kWave - 1), wv = wave_in_block();
     const int64_t total = static_cast<int64_t>(a.batch) * a.k, i = static_cast<int64_t>(blockIdx.x) * kWave + lane;
@@ -1266,11 +1263,11 @@ hipError_t launch_combine(const ExchangeArgs &a, hipStream_t s)
 hipError_t launch_combine_backward(const ExchangeArgs &a, hipStream_t s)
 {
     const int rows = move_rows(a.features, a.p.tiles, 16);   // (at least partial_rows, which the workspace has room for)
-    const int64_t sums = (static_cast<int64_t>(a.batch) * a.k + kWave - 1) / kWave;   // work-groups of the second launch
-    if (a.dweights && !fits_launch(sums, kGradWaves * kWave)) return hipErrorInvalidConfiguration;
+    const int64_t sums = weight_gradient_blocks(a.batch, a.k);
+    if (a.dweights && !fits_launch(sums, kGradThreads)) return hipErrorInvalidConfiguration;
     const hipError_t e = rows == 16 ? dispatch_go<16, true>(a, s) : rows == 8 ? dispatch_go<8, true>(a, s) : dispatch_go<4, true>(a, s);
     if (e != hipSuccess || !a.dweights) return e;
-    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>(sums)), dim3(kGradWaves * kWave), 0, s, a, (a.features + rows - 1) / rows);
+    hipLaunchKernelGGL(weight_gradient_kernel, dim3(static_cast<uint32_t>(sums)), dim3(kGradThreads), 0, s, a, (a.features + rows - 1) / rows);
     return hipGetLastError();
 }
 

@@ -12,7 +12,7 @@ sys.path.insert(0, HERE)
 
 from test_host_memory import Library  # noqa: E402
 
-OK, ARGUMENT, SHAPE, WORKSPACE, HIP = 0, -1, -2, -3, -5
+OK, ARGUMENT, SHAPE, WORKSPACE, HIP = 0, -1, -2, -4, -5
 P = 1 << 20   # an address that is aligned and never read
 
 
@@ -103,7 +103,33 @@ def a_call_that_no_launch_holds_is_refused_before_the_first(L):
         refused_or_launched(L, exchange("combine", (1 << 22) - 256, 8, 4, 1 << 14, weights=weights), False)
 
 
-CASES = [a_call_that_no_launch_holds_is_refused_before_the_first]
+def a_workspace_is_given_for_sizes_that_the_call_takes(L):
+    """expert_combine_workspace_bytes: 0 where no call of these sizes forms gradients of weights, and what it needs to both sides."""
+    p = ctypes.c_void_p(P)
+    top = (1 << 31) - 1
+
+    def call(features, batch, k, room):
+        n = ctypes.c_size_t(1 << 62)   # (placements of any size)
+        return L.lib.expert_combine_backward(p, 8, p, batch, p, n, p, batch, features, 1024, batch, k, 8, p, p, p, ctypes.c_size_t(room), None)
+
+    def rows(features, batch):   # of features in one sum, at least
+        rows = 16
+        while rows > 4 and -(-features // rows) * -(-batch // 1024) < 512:
+            rows //= 2
+        return rows
+
+    for features, batch, k in ((1, 1 << 29, 1), (1, 1 << 28, 2), (100, (1 << 30) - 1, 2), (1, top, 32), (1, 1 << 30, 1), (top, 100, 1), (top - 14, 1, 1), (top, top, 1), (1 << 30, 1, 1),
+                               (1 << 20, 1 << 22, 1), (0, 5, 1), (5, 0, 1), (-1, 5, 1), (5, -1, 1), (5, 5, 0), (5, 5, 33)):
+        assert L.lib.expert_combine_workspace_bytes(features, batch, k) == 0, (features, batch, k)
+        assert L.lib.nerva_last_error() != b""
+        assert call(features, batch, k, 1 << 62) in (ARGUMENT, SHAPE), (features, batch, k)
+    for features, batch, k in ((1, (1 << 29) - 64, 1), (1, (1 << 24) - 2, 32), (4096, 8192, 4), (1501, 777, 4), (1, 1, 1), (2047, 4096, 28), (1 << 20, 100, 1)):
+        need = L.lib.expert_combine_workspace_bytes(features, batch, k)
+        assert need == -(-features // rows(features, batch)) * batch * k * 4
+        assert call(features, batch, k, need) == OK and call(features, batch, k, need - 4) == WORKSPACE, (features, batch, k, L.lib.nerva_last_error())
+
+
+CASES = [a_call_that_no_launch_holds_is_refused_before_the_first, a_workspace_is_given_for_sizes_that_the_call_takes]
 
 
 @pytest.fixture(scope="module")
