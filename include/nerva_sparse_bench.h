@@ -46,7 +46,7 @@ int sparse_linear_routes(const nerva_layer *layer, int32_t batch, int32_t *route
  * 1 keeps every later layer on the sparse route, 0 sends every layer of at least 64 x 64 down the dense one. */
 int nerva_set_dense_threshold(float density);
 
-/* Per-kernel timing of mlp_train_step with HIP events, for benchmarks.  After
+/* Per-kernel timing of mlp_train_step (or mlp_train_step_clipped) with HIP events, for benchmarks.  After
  * mlp_profile_enable(mlp, max_steps > 0) the next max_steps training steps record an event
  * before every kernel launch and one after the last, on the step's stream (events are created
  * on the fly: a profiled step allocates, must not be captured in a graph, and runs slower than
@@ -54,7 +54,8 @@ int nerva_set_dense_threshold(float density);
  * a step (in launch order), the elapsed milliseconds from its event to the next one, summed over
  * the recorded steps (the launches of a step run back to back, so the slots add up to the step); the slots keep their
  * meaning until the next mlp_profile_enable.  mlp_profile_enable(mlp, 0) switches timing off
- * and frees the events.  Slot names look like "spmm_forward[0]", "sddmm_update[2]".
+ * and frees the events.  Slot names look like "spmm_forward[0]", "sddmm_update[2]".  The recorded steps are all mlp_train_step or all
+ * mlp_train_step_clipped, as the first of them is; the other call returns NERVA_ERR_ARGUMENT until max_steps steps have been recorded.
  *   n_slots_host, steps_host: HOST int32; ms_sum_host: HOST double[max_slots]. */
 int mlp_profile_enable(nerva_mlp *mlp, int32_t max_steps);
 int mlp_profile_read(nerva_mlp *mlp, int32_t max_slots, int32_t *n_slots_host,

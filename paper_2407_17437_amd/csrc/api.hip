@@ -178,7 +178,7 @@ struct nerva_layer {
 // time is the span to the next event: kernels of a step run back to back on one stream, so the
 // spans add up to the step and each carries the cost of one event, not two.
 struct StepProfiler {
-    bool on = false;
+    bool on = false, clipped = false;  // clipped: the kind of the steps that are recorded, whose launches differ
     int32_t max_steps = 0, step = 0, slot = 0;
     std::vector<std::string> names;    // one per launch of a step, in launch order
     std::vector<hipEvent_t> events;    // [step][slot 0 .. n, end of step], grown while recording
@@ -1742,6 +1742,12 @@ static int train_step(nerva_mlp *mlp, const float *X, int32_t ldx, const int32_t
                       float momentum, void *workspace, const Layout &L, float *loss_out, void *stream, const ClipArgs *clip)
 {
     int rc = NERVA_OK;
+    if (mlp->prof.on && mlp->prof.step < mlp->prof.max_steps) {
+        if (mlp->prof.step > 0 && mlp->prof.clipped != (clip != nullptr))
+            return fail(NERVA_ERR_ARGUMENT, "the profile holds %d of %d steps with%s clipped gradients: a step %s them would be booked under their names", mlp->prof.step,
+                        mlp->prof.max_steps, mlp->prof.clipped ? "" : "out", mlp->prof.clipped ? "without" : "with");
+        mlp->prof.clipped = clip != nullptr;
+    }
     hipStream_t s = as_stream(stream);
     char *ws = static_cast<char *>(workspace);
     const int n = static_cast<int>(mlp->layers.size());

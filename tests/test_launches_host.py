@@ -129,7 +129,66 @@ def a_workspace_is_given_for_sizes_that_the_call_takes(L):
         assert call(features, batch, k, need) == OK and call(features, batch, k, need - 4) == WORKSPACE, (features, batch, k, L.lib.nerva_last_error())
 
 
-CASES = [a_call_that_no_launch_holds_is_refused_before_the_first, a_workspace_is_given_for_sizes_that_the_call_takes]
+class Network:
+    """A chain of layers on the runtime without a GPU, with a workspace."""
+
+    def __init__(self, L, sizes, batch, flags=0):
+        self.L, self.batch, self.layers, self.handle = L, batch, [], ctypes.c_void_p()
+        a = [ctypes.c_void_p(ctypes.addressof(h)) for h in L.host]
+        for n, (cols, rows) in enumerate(zip(sizes[:-1], sizes[1:])):
+            for side in (0, 1):
+                L.counts(side, n_blocks=8, longest_row=cols)
+            layer = ctypes.c_void_p()
+            assert L.lib.sparse_linear_create(ctypes.byref(layer), rows, cols, rows * cols // 8, a[0], a[1], a[2], None, 1 if n + 2 < len(sizes) else 0, batch, None) == OK
+            self.layers.append(layer)
+        n = len(self.layers)
+        arrays = (ctypes.c_void_p * n)(*[x.value for x in self.layers])
+        velocities = (ctypes.c_void_p * n)(*[a[3].value] * n)
+        assert L.lib.mlp_create(ctypes.byref(self.handle), n, arrays, velocities, (ctypes.c_void_p * n)(), batch, flags) == OK, L.lib.nerva_last_error()
+        self.room = L.lib.mlp_clipped_workspace_bytes(self.handle, batch)
+        self.workspace = ctypes.create_string_buffer(self.room + 256)
+        self.at = ctypes.c_void_p((ctypes.addressof(self.workspace) + 255) // 256 * 256)
+
+    def step(self, clipped=False):
+        p, f = ctypes.c_void_p(ctypes.addressof(self.L.host[3])), ctypes.c_float
+        common = (self.handle, p, self.batch, p, self.batch, f(0.1), f(0.9))
+        if clipped:
+            return self.L.lib.mlp_train_step_clipped(*common, f(1.0), self.at, ctypes.c_size_t(self.room), None, p, None)
+        return self.L.lib.mlp_train_step(*common, self.at, ctypes.c_size_t(self.room), None, None)
+
+    def profile(self, steps):
+        assert self.L.lib.mlp_profile_enable(self.handle, steps) == OK
+
+    def slots(self):
+        n, steps, ms = ctypes.c_int32(), ctypes.c_int32(), (ctypes.c_double * 256)()
+        self.L.lib.mlp_profile_slot_name.restype = ctypes.c_char_p
+        assert self.L.lib.mlp_profile_read(self.handle, 256, ctypes.byref(n), ms, ctypes.byref(steps)) == OK, self.L.lib.nerva_last_error()
+        return steps.value, [self.L.lib.mlp_profile_slot_name(self.handle, i).decode() for i in range(n.value)]
+
+
+def a_profile_is_of_one_kind_of_step(L):
+    """The slots' names are those of the first step that is recorded: the other kind, which launches something else, is refused until as many
+    steps as were asked for have been recorded."""
+    for flags in (0, 1):   # (fused and not)
+        N = Network(L, (64, 48, 32, 10), 20, flags)
+        for clipped in (True, False):
+            N.profile(3)
+            assert N.step(clipped) == OK and N.step(clipped) == OK
+            before = L.hip.fake_launches()
+            assert N.step(not clipped) == ARGUMENT and L.hip.fake_launches() == before
+            assert b"clipped" in L.lib.nerva_last_error()
+            assert N.slots()[0] == 2 and N.step(clipped) == OK
+            steps, names = N.slots()
+            assert steps == 3 and ("norm+momentum[0]" in names) == clipped
+            if clipped:
+                assert names[-3:] == ["norm+momentum[0]", "mirror_refresh[2]", "mirror_refresh[1]"] and names.count("norm+momentum[0]") == 1
+            assert N.step(not clipped) == OK and N.step(clipped) == OK     # (no longer recorded)
+            assert N.slots() == (3, names)
+        N.profile(0)
+        assert N.step(True) == OK and N.step(False) == OK and N.slots() == (0, [])
+
+
+CASES = [a_call_that_no_launch_holds_is_refused_before_the_first, a_workspace_is_given_for_sizes_that_the_call_takes, a_profile_is_of_one_kind_of_step]
 
 
 @pytest.fixture(scope="module")
