@@ -1,4 +1,4 @@
-"""Lists of gradients that name an array more than once."""
+"""Lists of gradients that name an array more than once, and longer lists than one launch, or the step of an MLP, holds at a time."""
 import numpy as np
 import pytest
 
@@ -39,3 +39,65 @@ def test_a_gradient_twice_is_clipped_once(nb, lengths, order):
         assert abs(float(norm) - want) <= want * U * 1.001
         for got, e in zip(out, expected):
             assert ((got.double() - e).abs() <= e.abs() * 2 * U * 1.01).all()
+
+
+@pytest.mark.parametrize("counts", [[60_000 + i for i in range(600)], [16_384 + i % 7 for i in range(800)]], ids=["past the cache", "in the cache"])
+def test_lists_whose_partial_sums_are_added_up_on_their_own(nb, counts):
+    """More than 2048 partial sums: more than two launches of the norm's first kernel, and one that adds up what they leave.  The workspace is as
+    large as the call asks for, and what lies behind it stays."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    assert sum(-(-n // 8192) for n in counts) > 2048
+    new = lambda scale: [scale * torch.randn(n, generator=g, device="cuda") for n in counts]
+    grads, w, v = new(1.0), new(1.0), new(0.1)
+    grads[3][77], grads[-1][-1] = 3e4, -2e4        # (first and last: no part of the sum may be left out)
+    want = float(torch.stack([x.double().square().sum() for x in grads]).sum().sqrt())
+    need = nb.gradient_norm_workspace_bytes(len(counts)) // 4
+    room, norm = torch.full((need + 256,), float("nan"), device="cuda"), torch.zeros(1, device="cuda")
+    ws, behind = room[:need], room[need:]
+    behind.fill_(7)
+    max_norm = float(np.float32(want / 5))
+    c = float(np.float32(max_norm / want))          # the kernel's factor, whose last step the sum's order in 64 bits does not reach
+    nb.gradient_norm(grads, ws, norm)
+    assert abs(float(norm) - want) <= want * U * 1.001
+    out = [torch.full_like(x, float("nan")) for x in grads]
+    norm.zero_()
+    nb.gradient_clip(grads, out, max_norm, ws, norm)
+    assert abs(float(norm) - want) <= want * U * 1.001 and all(torch.equal(a, c * x) for a, x in zip(out, grads))
+    w2, v2 = [t.clone() for t in w], [t.clone() for t in v]
+    norm.zero_()
+    nb.sgd_update_clipped(w, v, grads, 0.05, 0.9, max_norm, False, ws, norm)
+    for a, b, x in zip(w2, v2, grads):
+        nb.sgd_update_values(a, b, c * x, x.numel(), 0.05, 0.9)
+    assert abs(float(norm) - want) <= want * U * 1.001 and all(torch.equal(a, b) for a, b in zip(w + v, w2 + v2))
+    assert (behind == 7).all()
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_clipped_step_of_many_layers(nb, nesterov):
+    """35 layers, whose arrays are more than the step's own list holds: the step on all of them with one norm."""
+    import torch
+    from paper_2407_17437_amd import workloads as wl
+    batch, lr, mu = 30, 0.05, 0.9
+    sizes = (40,) + tuple(20 + 3 * (i % 5) for i in range(34)) + (10,)
+    mlp = wl.make_mlp(sizes, pattern_seed=41, value_seed=42, sparsity=0.3, bias_std=0.3)
+    flags = nb.NERVA_MLP_NESTEROV if nesterov else 0
+    A, T = nb.MLP(mlp, batch, flags), nb.MLP(mlp, batch, flags | nb.NERVA_MLP_UNFUSED)
+    n = len(A.layers)
+    assert 2 * n > 64
+    Xs, Ts = wl.make_batches(sizes[0], sizes[-1], batch, 1, seed=9)
+    X, labels = nb.to_dense(Xs[0]), torch.as_tensor(Ts[0]).cuda()
+    arrays = [x for L in A.layers for x in ((L.values, L.velocity), (L.bias, L.bias_velocity))]
+    before = [(w.clone(), v.clone()) for w, v in arrays]
+    T.train_step(X, labels, batch, lr, mu)          # its gradients are the same
+    grads = [T.view(kind, l, batch).clone() for l in range(n) for kind in ("g", "db")]
+    want = float(torch.stack([x.double().square().sum() for x in grads]).sum().sqrt())
+    assert want > 0 and all(float(x.abs().max()) > 0 for x in grads[-8:])
+    max_norm = float(np.float32(want / 4))
+    c = float(np.float32(max_norm / want))
+    A.train_step_clipped(X, labels, batch, lr, mu, max_norm)
+    assert abs(float(A.norm) - want) <= want * U * 1.001
+    for (w, v), (w2, v2), x in zip(arrays, before, grads):
+        (nb.sgd_update_values_nesterov if nesterov else nb.sgd_update_values)(w2, v2, c * x, x.numel(), lr, mu)
+        assert torch.equal(w, w2) and torch.equal(v, v2)
+    A.close(); T.close()

@@ -1,4 +1,4 @@
-"""Places of many columns in the experts' blocks."""
+"""Places of many columns in the experts' blocks, and the exchange where what it stages elsewhere has no room."""
 import numpy as np
 import pytest
 
@@ -82,3 +82,32 @@ def test_time_of_places_grows_with_the_columns(nb):
         times.append(sorted(one)[3])
     print("ms:", times, flush=True)
     assert times[1] < 8 * times[0], times
+
+
+def test_blocks_of_weighted_columns_whose_weights_have_no_room_in_lds(nb):
+    """Many choices, long tiles and 16 rows for a work-group: with the rows the weights would take more than 160 KiB, and are read where they lie."""
+    import torch
+    E, F, B, k, C = 256, 2048, 4096, 28, 300
+    g = torch.Generator(device="cuda").manual_seed(6)
+    chosen = (torch.rand(E, B, generator=g, device="cuda") + 0.2 * torch.rand(E, 1, generator=g, device="cuda")).topk(k, dim=0).indices.to(torch.int32)
+    dY, w, Ye = torch.randn(F, B, generator=g, device="cuda"), torch.randn(k, B, generator=g, device="cuda"), torch.randn(E, F, C, generator=g, device="cuda")
+    slots, _ = places(chosen.cpu().numpy(), E, C)
+    placement = torch.empty(nb.expert_placement_bytes(E, B, k) // 4, dtype=torch.int32, device="cuda")
+    nb.expert_place(chosen, E, B, k, C, None, None, placement)
+    sd = torch.as_tensor(slots).cuda()
+    j, c = torch.nonzero(sd >= 0, as_tuple=True)
+    e, s = chosen[j, c].long(), sd[j, c].long()
+    assert 0 < j.numel() < B * k
+    want = torch.zeros(E, F, C, device="cuda")
+    want[e, :, s] = (w[j, c] * dY[:, c]).t()            # (one product, rounded once: the same bits)
+    room = torch.full((nb.expert_combine_workspace_bytes(F, B, k) // 4,), float("nan"), device="cuda")
+    for with_dw in (False, True):
+        dYe, dw = torch.full((E, F, C), float("nan"), device="cuda"), torch.full((k, B), float("nan"), device="cuda")
+        nb.expert_combine_backward(Ye if with_dw else None, dY, placement, w, F, E, B, k, C, dYe, dw if with_dw else None, room if with_dw else None)
+        assert torch.equal(dYe, want)
+    sums, sizes = torch.zeros(k, B, dtype=torch.float64, device="cuda"), torch.zeros(k, B, dtype=torch.float64, device="cuda")
+    for at in torch.arange(j.numel(), device="cuda").split(8192):
+        y, d = Ye[e[at], :, s[at]].double(), dY[:, c[at]].t().double()
+        sums[j[at], c[at]], sizes[j[at], c[at]] = (y * d).sum(1), (y * d).abs().sum(1)
+    # 16 products in a sum of 32 bits, the sums of F / 16 of those in 64, rounded once
+    assert ((dw - sums).abs() <= sizes * 18 * 2.0 ** -24).all() and (dw[sd < 0] == 0).all()
