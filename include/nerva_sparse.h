@@ -341,7 +341,8 @@ int sgd_update_clipped(int32_t n, float *const *values, float *const *velocities
 enum {
     NERVA_EXPERT_SIGMOID = 1,       /* scores are sigmoids of the logits, else their softmax over all experts       */
     NERVA_EXPERT_RENORMALISE = 2,   /* weights are divided by their sum over the column's choices                   */
-    NERVA_EXPERT_GROUP_PAIR = 4     /* a group's score is the sum of its two best keys, else its best key           */
+    NERVA_EXPERT_GROUP_PAIR = 4     /* a group's score is the sum of its two best keys (the best alone, where no    */
+                                    /* other expert of it may be chosen), else its best key                         */
 };
 /* With score s_e and key q_e = s_e + bias[e] (bias for balance, may be NULL; without it and without NERVA_EXPERT_GROUP_PAIR the
  * logit itself is the key, which orders alike), the experts of a column are, best first, the k of largest key; among equal
@@ -377,8 +378,8 @@ int expert_dispatch(const float *X, int32_t ldx, const void *placement, size_t p
                     int32_t experts, int32_t batch, int32_t k, int32_t capacity, float *Xe, int32_t lde, void *stream);
 
 /* Y[f, c] = sum over the column's choices that have a place of weights[j, c] * Ye[e, f, place], in the order of the experts; 0 where
- * none has.  weights == NULL: all 1, which makes this the backward pass of expert_dispatch.  Places that hold no column are
- * not read. */
+ * none has.  weights == NULL: all 1, which makes this the backward pass of expert_dispatch.  What lies in places that hold no column does
+ * not matter, nor do the weights of choices without a place. */
 int expert_combine(const float *Ye, int32_t lde, const void *placement, size_t placement_bytes, const float *weights,
                    int32_t ldk, int32_t features, int32_t experts, int32_t batch, int32_t k, int32_t capacity,
                    float *Y, int32_t ldy, void *stream);

@@ -2187,7 +2187,7 @@ size_t expert_placement_bytes(int32_t experts, int32_t batch, int32_t k)
 static int check_placement(const void *placement, size_t placement_bytes, int32_t experts, int32_t batch, int32_t k, int32_t capacity, Placement &p)
 {
     if (!placement) return fail(NERVA_ERR_ARGUMENT, "placement is null");
-    if (capacity < 1 || capacity >= (1 << 30)) return fail(NERVA_ERR_ARGUMENT, "capacity must be positive (got %d)", capacity);
+    if (capacity < 1 || capacity >= (1 << 30)) return fail(NERVA_ERR_ARGUMENT, "capacity = %d is not in 1 .. 2^30 - 1", capacity);
     p = placement_of(const_cast<void *>(placement), experts, batch, k);
     if (reinterpret_cast<uintptr_t>(placement) % 16) return fail(NERVA_ERR_WORKSPACE, "placement must be 16-byte aligned");
     if (placement_bytes < static_cast<size_t>(p.bytes)) return fail(NERVA_ERR_WORKSPACE, "placement has %zu bytes, %lld needed", placement_bytes, (long long)p.bytes);

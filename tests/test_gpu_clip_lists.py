@@ -101,3 +101,35 @@ def test_clipped_step_of_many_layers(nb, nesterov):
         (nb.sgd_update_values_nesterov if nesterov else nb.sgd_update_values)(w2, v2, c * x, x.numel(), lr, mu)
         assert torch.equal(w, w2) and torch.equal(v, v2)
     A.close(); T.close()
+
+
+@pytest.mark.parametrize("dense", [None, 0.5])
+def test_captured_clipped_steps_of_an_mlp(nb, dense):
+    """The whole clipped step in a graph, replayed on changing batches, with plain steps between: the bits of the same steps outside a graph."""
+    import torch
+    from paper_2407_17437_amd import workloads as wl
+    batch, sizes = 64, (128, 96, 64, 10)
+    mlp = wl.make_mlp(sizes, pattern_seed=3, value_seed=4, sparsity=0.4, bias_std=0.1)
+    A, B = nb.MLP(mlp, batch, dense_from_density=dense), nb.MLP(mlp, batch, dense_from_density=dense)
+    Xs, Ts = wl.make_batches(sizes[0], sizes[-1], batch, 5, seed=8)
+    batches = [(nb.to_dense(x), torch.as_tensor(t).cuda()) for x, t in zip(Xs, Ts)]
+    X, labels = batches[0][0].clone(), batches[0][1].clone()
+    for M in (A, B):
+        M.train_step(X, labels, batch, 0.05, 0.9)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        A.train_step_clipped(X, labels, batch, 0.05, 0.9, 0.3, ldx=X.stride(0))
+    for t, (x, y) in enumerate(batches):
+        X.copy_(x)
+        labels.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        B.train_step_clipped(X, labels, batch, 0.05, 0.9, 0.3)
+        assert torch.equal(A.norm, B.norm) and float(A.norm) > 0 and torch.equal(A.loss, B.loss)
+        if t % 2:
+            for M in (A, B):
+                M.train_step(X, labels, batch, 0.05, 0.9)
+        for a, b in zip(A.layers, B.layers):
+            assert all(torch.equal(getattr(a, n), getattr(b, n)) for n in ("values", "velocity", "bias", "bias_velocity"))
+    A.close(); B.close()
