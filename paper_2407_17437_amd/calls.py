@@ -49,6 +49,12 @@ class Calls:
 
     # ---- mixtures and clipped gradients: with the looks at types, shapes and devices of csrc/fastcall.cpp
 
+    def _numbers(self, *numbers):
+        """ctypes would cut them."""
+        for n in numbers:
+            if not -2 ** 31 <= n < 2 ** 31:
+                raise OverflowError(f"{n} does not fit 32 bits")
+
     def _tensor(self, t, name, dtype):
         if not isinstance(t, torch.Tensor):
             raise TypeError("expected a tensor")
@@ -62,7 +68,9 @@ class Calls:
             return None, 0
         t = self._tensor(t, name, dtype)
         assert t.dim() == 2 and t.stride(1) == 1 and t.size(0) >= rows and t.size(1) >= columns, f"{name}: a matrix of the call's sizes with contiguous rows expected"
-        return t.data_ptr(), t.stride(0) if t.size(0) > 1 else t.size(1)
+        step = t.stride(0) if t.size(0) > 1 else t.size(1)
+        assert step < 2 ** 31, f"{name}: rows less than 2^31 entries apart expected"
+        return t.data_ptr(), step
 
     def _blocks(self, t, name, experts, features, capacity, optional=False):
         if optional and t is None:
@@ -71,7 +79,7 @@ class Calls:
         assert t.dim() == 3 and t.stride(2) == 1 and t.size(0) >= experts and t.size(1) == features and t.size(2) >= capacity, \
             f"{name}: blocks (experts, features, capacity) with contiguous rows expected"
         step = t.stride(1) if features > 1 else t.stride(0) if t.size(0) > 1 else t.size(2)
-        assert t.size(0) <= 1 or t.stride(0) == features * step, f"{name}: blocks right behind each other expected"
+        assert step < 2 ** 31 and (t.size(0) <= 1 or t.stride(0) == features * step), f"{name}: blocks right behind each other expected"
         return t.data_ptr(), step
 
     def _vector(self, t, name, n, dtype=torch.float32, optional=False):
@@ -103,6 +111,7 @@ class Calls:
         assert k <= 1 or len(set(lds)) == 1, f"{name}: the row stride of {of} expected"
 
     def route(self, Z, bias, experts, batch, k, groups, top_groups, flags, scale, chosen, weights, stream):
+        self._numbers(experts, batch, k, groups, top_groups, flags)
         z = self._sized(Z, "Z", experts, batch)
         b = self._vector(bias, "bias", experts, optional=True)
         c, ldk = self._sized(chosen, "chosen", k, batch, torch.int32)
@@ -111,6 +120,7 @@ class Calls:
         return self.lib.expert_route(*z, b, experts, batch, k, groups, top_groups, flags, scale, c, w, ldk, self.handle(stream))
 
     def route_backward(self, Z, chosen, dweights, experts, batch, k, flags, scale, dZ, stream):
+        self._numbers(experts, batch, k, flags)
         z = self._sized(Z, "Z", experts, batch)
         c, ldk = self._sized(chosen, "chosen", k, batch, torch.int32)
         w, ldw = self._sized(dweights, "dweights", k, batch)
@@ -119,6 +129,7 @@ class Calls:
         return self.lib.expert_route_backward(*z, c, w, ldk, experts, batch, k, flags, scale, *d, self.handle(stream))
 
     def place(self, chosen, experts, batch, k, capacity, slots, counts, placement, stream):
+        self._numbers(experts, batch, k, capacity)
         c, ldk = self._sized(chosen, "chosen", k, batch, torch.int32)
         s, lds = self._sized(slots, "slots", k, batch, torch.int32, True)
         n = self._vector(counts, "counts", experts, torch.int32, True)
@@ -127,12 +138,14 @@ class Calls:
         return self.lib.expert_place(c, ldk, experts, batch, k, capacity, s, n, *self._scratch(placement, "placement"), self.handle(stream))
 
     def dispatch(self, X, placement, features, experts, batch, k, capacity, Xe, stream):
+        self._numbers(features, experts, batch, k, capacity)
         x = self._sized(X, "X", features, batch)
         p = self._scratch(placement, "placement")
         xe = self._blocks(Xe, "Xe", experts, features, capacity)
         return self.lib.expert_dispatch(*x, *p, features, experts, batch, k, capacity, *xe, self.handle(stream))
 
     def combine(self, Ye, placement, weights, features, experts, batch, k, capacity, Y, stream):
+        self._numbers(features, experts, batch, k, capacity)
         ye = self._blocks(Ye, "Ye", experts, features, capacity)
         p = self._scratch(placement, "placement")
         w = self._sized(weights, "weights", k, batch, optional=True)
@@ -140,6 +153,7 @@ class Calls:
         return self.lib.expert_combine(*ye, *p, *w, features, experts, batch, k, capacity, *y, self.handle(stream))
 
     def combine_backward(self, Ye, dY, placement, weights, features, experts, batch, k, capacity, dYe, dweights, workspace, stream):
+        self._numbers(features, experts, batch, k, capacity)
         ye, lde = self._blocks(Ye, "Ye", experts, features, capacity, True)
         dy = self._sized(dY, "dY", features, batch)
         p = self._scratch(placement, "placement")
