@@ -334,7 +334,7 @@ int sgd_update_clipped(int32_t n, float *const *values, float *const *velocities
  * Block e of an operand (experts, features, lde) starts at e * features * lde; it is an operand (features, lde) of the calls
  * above with `capacity` columns, lde >= capacity.  Sizes are known before the router has run: nothing waits for the device, and the whole
  * sequence may be captured.  1 <= experts <= 1024, 1 <= k <= 32; batch * k < 2^30.  A call of which a launch would take 2^32 threads
- * is refused before anything is written (NERVA_ERR_SHAPE); none does below 2^26 columns, 2^29 choices, 2^24 features and 2^33 entries
+ * is refused before anything is written (NERVA_ERR_SHAPE); none does with up to 2^25 columns, 2^28 choices, 2^23 features and 2^32 entries
  * (features x columns).
  * Inputs and outputs of one call must not overlap; nor may, in time, calls that write a placement or a workspace and others that use it
  * (two captured graphs, say, that hold the same one). */
