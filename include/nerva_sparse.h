@@ -58,7 +58,7 @@ typedef enum nerva_status {
 typedef struct nerva_layer nerva_layer; /* one sparse linear layer: pattern, mirror, tables */
 typedef struct nerva_mlp nerva_mlp;     /* a chain of layers + optimiser state pointers     */
 
-enum { NERVA_ACT_NONE = 0, NERVA_ACT_RELU = 1 };
+enum { NERVA_ACT_NONE = 0, NERVA_ACT_RELU = 1, NERVA_ACT_SILU = 2 /* group norm only: u / (1 + exp(-u)) */ };
 
 /* Message of the last failing call on this thread ("" if none). Host pointer, valid
  * until the next failing call on the thread. */
@@ -395,6 +395,74 @@ int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32
                             size_t placement_bytes, const float *weights, int32_t ldk, int32_t features, int32_t experts,
                             int32_t batch, int32_t k, int32_t capacity, float *dYe, float *dweights,
                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- normalisation and dropout ------------------------------------------------------------
+ * What may stand between two layers of a network.  Group norm with an activation and dropout in one pass over a layer's output X
+ * (features, ldx): with m = features / groups consecutive features a group, for group g of column c
+ *     mean[g,c] = (1/m) sum of X[i,c],    rstd[g,c] = 1 / sqrt( (1/m) sum of (X[i,c] - mean)^2 + eps )
+ *     u = gamma[i] (X[i,c] - mean) rstd + beta[i],    Y[i,c] = D act(u)
+ * act: NERVA_ACT_NONE, _RELU or _SILU.  groups divides features (groups = 1: layer norm); gamma, beta: float[features], NULL for 1 and 0.
+ * D is the dropout below, with the same drop, layer and state; drop = 0: none, and state may be NULL.
+ * mean and rstd (groups, lds) are what the backward pass takes; both NULL without one.  A column's results depend on no other
+ * column.  Y may be X itself where no backward pass needs it, with ldy = ldx; other overlaps are not allowed.
+ * workspace: device scratch, 16-byte aligned, of group_norm_workspace_bytes() (may be NULL where that is 0); calls that overlap in time take one
+ * each.  group_norm_workspace_bytes is (size_t)-1 for sizes that are refused.  Sums are held in 32 bits: numbers from about 1e18 on overflow them. */
+size_t group_norm_workspace_bytes(int32_t features, int32_t groups, int32_t batch);
+int group_norm_forward(const float *X, int32_t ldx, const float *gamma, const float *beta, int32_t features, int32_t groups,
+                       int32_t batch, float eps, int32_t act, float drop, int32_t layer, const int64_t *state, float *Y,
+                       int32_t ldy, float *mean, float *rstd, int32_t lds, void *workspace, size_t workspace_bytes, void *stream);
+/* Gradients: of X, and, unless NULL, of gamma and beta (sums over all columns, added up in the same order in every call).  The arguments are those of
+ * the forward pass, with its mean and rstd; dY (features, lddy) is the gradient of Y.  The ReLU is taken to be constant at 0.
+ * dX may be dY itself, with lddx = lddy. */
+int group_norm_backward(const float *X, int32_t ldx, const float *gamma, const float *beta, const float *mean,
+                        const float *rstd, int32_t lds, const float *dY, int32_t lddy, int32_t features, int32_t groups,
+                        int32_t batch, int32_t act, float drop, int32_t layer, const int64_t *state, float *dX, int32_t lddx,
+                        float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+/* Dropout: Y[i,c] = 0 with probability drop, X[i,c] / (1 - drop) otherwise; drop in [0, 1), taken to the next multiple of 2^-16 (65535 of them at most).
+ * Which entries are dropped follows from state = {seed, step} (two int64 on the DEVICE, so that a captured step
+ * can go on drawing: the program raises step, of which the low 32 bits count, between steps), layer (a number that tells the calls of one step
+ * apart), i and c, by Philox4x32-10 with key seed and counter (c / 4, i / 2, layer, step): word c % 4, its low 16 bits for even
+ * i and its high 16 bits for odd i, are below 65536 drop where the entry is dropped.  They depend on neither ld nor batch, and no
+ * mask is stored: the backward pass is the same call on the gradient.  Y may be X itself, with ldy = ldx. */
+int dropout(const float *X, int32_t ldx, int32_t features, int32_t batch, float drop, int32_t layer, const int64_t *state,
+            float *Y, int32_t ldy, void *stream);
+
+/* ---- losses of labels: scoring, policies, preferences ------------------------------------------
+ * Columns are tokens or actions that were taken: labels int32[batch], one class of the column's logits Z (classes, ldz) each, with the
+ * log-probability
+ *     l_c = Z[labels[c],c] - log sum_i exp Z[i,c].
+ * A column does not count where its label lies outside 0 .. classes-1 or the label's logit is -inf (a closed class, or a column with no open one):
+ * l_c is 0 there and so is its gradient, whatever the column holds.  Logits of -inf have probability 0 elsewhere; NaN and +inf make the results
+ * that depend on their column NaN.  Sums over columns and everything that is done with log-probabilities are held in 64 bits.
+ * Sequences are runs of columns: starts (device, int32[sequences + 1], ascending, within 0 .. batch) holds their first columns and the end of the
+ * last; they may be empty, and columns outside belong to none.
+ * workspace: device scratch, 16-byte aligned, of label_loss_workspace_bytes() (0 for sizes that are refused); calls that overlap in time take one
+ * each.  dZ may be Z itself, with lddz = ldz; other overlaps of inputs and outputs are not allowed. */
+size_t label_loss_workspace_bytes(int32_t classes, int32_t batch, int32_t sequences);
+/* logp[c] = l_c and sums[s] = sum of l_c over sequence s, unless NULL (one of them at least is given; sequences may be 0 and starts NULL
+ * without sums). */
+int label_log_probs(const float *Z, int32_t ldz, const int32_t *labels, int32_t classes, int32_t batch, const int32_t *starts,
+                    int32_t sequences, float *logp, float *sums, void *workspace, size_t workspace_bytes, void *stream);
+/* Clipped policy loss with a KL term, and the gradient of the logits: with r = exp(l_c - old_logp[c]), q = exp(ref_logp[c] - l_c) and A = advantages[c],
+ *     loss = sum_c w_c ( -min( r A, clip(r, 1 - clip_low, 1 + clip_high) A ) + beta (q - log q - 1) )
+ *     dZ[i,c] = dloss/dl_c ( [i == labels[c]] - exp(Z[i,c]) / sum exp Z[.,c] )
+ * weights: float[batch], NULL for 1/batch; a column of weight 0 does not count.  ref_logp NULL: no KL term.  Where r lies beyond the border
+ * that A bounds it by, the first term has no gradient; on which side it lies is decided in 64 bits.
+ * logp: float[batch], l_c (may be NULL).  stats: float[4] on the device: the loss, its first term, the weighted KL term (without beta) and the
+ * weight of the columns beyond their border.  0 <= clip_low, clip_high, beta, finite. */
+int policy_loss(const float *Z, int32_t ldz, const int32_t *labels, const float *old_logp, const float *ref_logp,
+                const float *advantages, const float *weights, int32_t classes, int32_t batch, float clip_low, float clip_high,
+                float beta, float *dZ, int32_t lddz, float *logp, float *stats, void *workspace, size_t workspace_bytes,
+                void *stream);
+/* Preference loss of pairs, and the gradient of the logits: sequence 2p is preferred to sequence 2p + 1; with S_s = sum of l_c over sequence s and
+ * x_p = beta ( (S_2p - ref_sums[2p]) - (S_2p+1 - ref_sums[2p+1]) ),
+ *     loss = (1/pairs) sum_p ( (1 - smoothing) log(1 + exp(-x_p)) + smoothing log(1 + exp(x_p)) ).
+ * starts: int32[2 pairs + 1] as above.  ref_sums: float[2 pairs], such sums of a reference model (NULL: 0).  sums float[2 pairs], margins (x_p) float[pairs]
+ * and loss float[1] may be NULL.  dZ is 0 in columns that do not count or lie outside all sequences.  beta finite, smoothing in [0, 1].
+ * workspace: for 2 pairs sequences. */
+int preference_loss(const float *Z, int32_t ldz, const int32_t *labels, const int32_t *starts, const float *ref_sums,
+                    int32_t classes, int32_t batch, int32_t pairs, float beta, float smoothing, float *dZ, int32_t lddz,
+                    float *sums, float *margins, float *loss, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- MLP training step ---------------------------------------------------------------
  * mlp_create chains n_layers layers (layer l's cols = layer l-1's rows; hidden layers

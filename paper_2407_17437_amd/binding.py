@@ -20,7 +20,7 @@ LIB_PATH = os.environ.get("NERVA_SPARSE_LIB") or os.path.join(_PKG, "libnerva_sp
 
 NERVA_OK = 0
 NERVA_ERR_ARGUMENT, NERVA_ERR_SHAPE, NERVA_ERR_CSR, NERVA_ERR_WORKSPACE, NERVA_ERR_HIP = -1, -2, -3, -4, -5
-NERVA_ACT_NONE, NERVA_ACT_RELU = 0, 1
+NERVA_ACT_NONE, NERVA_ACT_RELU, NERVA_ACT_SILU = 0, 1, 2
 NERVA_PACK_MAX_LEN, NERVA_PACK_MIN_ROWS = 128, 2048
 NERVA_STAGE_ROWS, NERVA_STAGE_COLS, NERVA_STAGE_MIN_BATCH, NERVA_STAGE_RANGE_ROWS, NERVA_STAGE_QUAD = 512, 64, 128, 512, 1 << 30
 NERVA_PARTITION_BALANCED, NERVA_PARTITION_ROW_SPLIT, NERVA_PARTITION_PREFER_STAGED, NERVA_PARTITION_PREFER_DENSE_ROWS, NERVA_PARTITION_PREFER_STRIPS = range(5)
@@ -41,6 +41,8 @@ EXPORTS = [
     "gradient_norm_workspace_bytes", "gradient_norm", "gradient_clip", "sgd_update_clipped", "mlp_clipped_workspace_bytes", "mlp_train_step_clipped",
     "expert_route", "expert_route_backward", "expert_placement_bytes", "expert_place", "expert_dispatch", "expert_combine",
     "expert_combine_workspace_bytes", "expert_combine_backward",
+    "group_norm_workspace_bytes", "group_norm_forward", "group_norm_backward", "dropout",
+    "label_loss_workspace_bytes", "label_log_probs", "policy_loss", "preference_loss",
     "mlp_profile_enable", "mlp_profile_read", "mlp_profile_slot_name", "sparse_linear_partition", "sparse_linear_routes",
 ]
 
@@ -100,6 +102,14 @@ def _load() -> ctypes.CDLL:
         "expert_combine": (ctypes.c_int, [vp, i32, vp, sz, vp, i32, i32, i32, i32, i32, i32, vp, i32, vp]),
         "expert_combine_workspace_bytes": (sz, [i32, i32, i32]),
         "expert_combine_backward": (ctypes.c_int, [vp, i32, vp, i32, vp, sz, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]),
+        "group_norm_workspace_bytes": (sz, [i32, i32, i32]),
+        "group_norm_forward": (ctypes.c_int, [vp, i32, vp, vp, i32, i32, i32, f32, i32, f32, i32, vp, vp, i32, vp, vp, i32, vp, sz, vp]),
+        "group_norm_backward": (ctypes.c_int, [vp, i32, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, i32, f32, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "dropout": (ctypes.c_int, [vp, i32, i32, i32, f32, i32, vp, vp, i32, vp]),
+        "label_loss_workspace_bytes": (sz, [i32, i32, i32]),
+        "label_log_probs": (ctypes.c_int, [vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, sz, vp]),
+        "policy_loss": (ctypes.c_int, [vp, i32, vp, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, i32, vp, vp, vp, sz, vp]),
+        "preference_loss": (ctypes.c_int, [vp, i32, vp, vp, vp, i32, i32, i32, f32, f32, vp, i32, vp, vp, vp, vp, sz, vp]),
         "nerva_copy_f32": (ctypes.c_int, [vp, vp, i64, vp]),
         "sparse_linear_partition": (ctypes.c_int, [vp, i32, i32, vp, vp]),
         "sparse_linear_routes": (ctypes.c_int, [vp, i32, vp]),
@@ -152,6 +162,8 @@ try:
     _fastcall.bind_mixtures(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "expert_route", "expert_route_backward", "expert_place", "expert_dispatch", "expert_combine", "expert_combine_backward", "gradient_norm",
         "gradient_clip", "sgd_update_clipped")))
+    _fastcall.bind_losses(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "group_norm_forward", "group_norm_backward", "dropout", "label_log_probs", "policy_loss", "preference_loss")))
 except ImportError:
     from .calls import Calls
     _fastcall = Calls(lib, _stream)
@@ -430,6 +442,62 @@ def expert_combine_workspace_bytes(features: int, batch: int, k: int) -> int:
 def expert_combine_backward(Ye, dY, placement, weights, features: int, experts: int, batch: int, k: int, capacity: int, dYe, dweights, workspace,
                             stream=None) -> None:
     rc = _fastcall.combine_backward(Ye, dY, placement, weights, features, experts, batch, k, capacity, dYe, dweights, workspace, stream)
+    if rc:
+        _check(rc)
+
+
+# Normalisation, dropout and losses of labels: as above; state: int64 tensor {seed, step}.
+
+def group_norm_workspace_bytes(features: int, groups: int, batch: int) -> int:
+    n = int(lib.group_norm_workspace_bytes(features, groups, batch))
+    if n == ctypes.c_size_t(-1).value:
+        raise NervaError(NERVA_ERR_ARGUMENT, last_error())
+    return n
+
+
+def group_norm_forward(X, gamma, beta, features: int, groups: int, batch: int, eps: float, act: int, drop: float, layer: int, state, Y, mean, rstd, workspace,
+                       stream=None) -> None:
+    rc = _fastcall.norm_forward(X, gamma, beta, features, groups, batch, eps, act, drop, layer, state, Y, mean, rstd, workspace, stream)
+    if rc:
+        _check(rc)
+
+
+def group_norm_backward(X, gamma, beta, mean, rstd, dY, features: int, groups: int, batch: int, act: int, drop: float, layer: int, state, dX, dgamma, dbeta, workspace,
+                        stream=None) -> None:
+    rc = _fastcall.norm_backward(X, gamma, beta, mean, rstd, dY, features, groups, batch, act, drop, layer, state, dX, dgamma, dbeta, workspace, stream)
+    if rc:
+        _check(rc)
+
+
+def dropout(X, features: int, batch: int, drop: float, layer: int, state, Y, stream=None) -> None:
+    rc = _fastcall.dropout(X, features, batch, drop, layer, state, Y, stream)
+    if rc:
+        _check(rc)
+
+
+def label_loss_workspace_bytes(classes: int, batch: int, sequences: int) -> int:
+    n = int(lib.label_loss_workspace_bytes(classes, batch, sequences))
+    if n == 0:
+        raise NervaError(NERVA_ERR_ARGUMENT, last_error())
+    return n
+
+
+def label_log_probs(Z, labels, classes: int, batch: int, starts, sequences: int, logp, sums, workspace, stream=None) -> None:
+    rc = _fastcall.log_probs(Z, labels, classes, batch, starts, sequences, logp, sums, workspace, stream)
+    if rc:
+        _check(rc)
+
+
+def policy_loss(Z, labels, old_logp, ref_logp, advantages, weights, classes: int, batch: int, clip_low: float, clip_high: float, beta: float, dZ, logp, stats, workspace,
+                stream=None) -> None:
+    rc = _fastcall.policy(Z, labels, old_logp, ref_logp, advantages, weights, classes, batch, clip_low, clip_high, beta, dZ, logp, stats, workspace, stream)
+    if rc:
+        _check(rc)
+
+
+def preference_loss(Z, labels, starts, ref_sums, classes: int, batch: int, pairs: int, beta: float, smoothing: float, dZ, sums, margins, loss, workspace,
+                    stream=None) -> None:
+    rc = _fastcall.preference(Z, labels, starts, ref_sums, classes, batch, pairs, beta, smoothing, dZ, sums, margins, loss, workspace, stream)
     if rc:
         _check(rc)
 

@@ -58,7 +58,7 @@ class Calls:
     def _tensor(self, t, name, dtype):
         if not isinstance(t, torch.Tensor):
             raise TypeError("expected a tensor")
-        assert t.dtype == dtype, f"{name}: {'float32' if dtype == torch.float32 else dtype} expected"
+        assert t.dtype == dtype, f"{name}: {str(dtype)[6:]} expected"
         assert t.is_cuda, f"{name}: a tensor on the GPU expected"
         assert t.get_device() == torch.cuda.current_device(), f"{name}: a tensor on the current device expected"
         return t
@@ -183,3 +183,66 @@ class Calls:
         v, _ = self._arrays(velocities, "velocities", counts)
         return self.lib.sgd_update_clipped(len(counts), w, v, g, (ctypes.c_int64 * len(counts))(*counts), lr, momentum, max_norm, int(nesterov),
                                            *self._scratch(workspace, "workspace"), self._vector(norm, "norm", 1, optional=True), self.handle(stream))
+
+    # ---- normalisation, dropout and losses of labels
+
+    def norm_forward(self, X, gamma, beta, features, groups, batch, eps, act, drop, layer, state, Y, mean, rstd, workspace, stream):
+        self._numbers(features, groups, batch, act, layer)
+        x = self._sized(X, "X", features, batch)
+        g, b = self._vector(gamma, "gamma", features, optional=True), self._vector(beta, "beta", features, optional=True)
+        st = self._vector(state, "state", 2, torch.int64, True)
+        y = self._sized(Y, "Y", features, batch)
+        m, lds = self._sized(mean, "mean", groups, batch, optional=True)
+        r, ldr = self._sized(rstd, "rstd", groups, batch, optional=True)
+        if m is not None and r is not None:
+            self._same("rstd", "mean", groups, lds, ldr)
+        return self.lib.group_norm_forward(*x, g, b, features, groups, batch, eps, act, drop, layer, st, *y, m, r, lds, *self._scratch(workspace, "workspace"),
+                                           self.handle(stream))
+
+    def norm_backward(self, X, gamma, beta, mean, rstd, dY, features, groups, batch, act, drop, layer, state, dX, dgamma, dbeta, workspace, stream):
+        self._numbers(features, groups, batch, act, layer)
+        x = self._sized(X, "X", features, batch)
+        g, b = self._vector(gamma, "gamma", features, optional=True), self._vector(beta, "beta", features, optional=True)
+        m, lds = self._sized(mean, "mean", groups, batch)
+        r, ldr = self._sized(rstd, "rstd", groups, batch)
+        self._same("rstd", "mean", groups, lds, ldr)
+        dy = self._sized(dY, "dY", features, batch)
+        st = self._vector(state, "state", 2, torch.int64, True)
+        dx = self._sized(dX, "dX", features, batch)
+        dg, db = self._vector(dgamma, "dgamma", features, optional=True), self._vector(dbeta, "dbeta", features, optional=True)
+        return self.lib.group_norm_backward(*x, g, b, m, r, lds, *dy, features, groups, batch, act, drop, layer, st, *dx, dg, db, *self._scratch(workspace, "workspace"),
+                                            self.handle(stream))
+
+    def dropout(self, X, features, batch, drop, layer, state, Y, stream):
+        self._numbers(features, batch, layer)
+        x = self._sized(X, "X", features, batch)
+        st = self._vector(state, "state", 2, torch.int64, True)
+        y = self._sized(Y, "Y", features, batch)
+        return self.lib.dropout(*x, features, batch, drop, layer, st, *y, self.handle(stream))
+
+    def log_probs(self, Z, labels, classes, batch, starts, sequences, logp, sums, workspace, stream):
+        self._numbers(classes, batch, sequences)
+        z = self._sized(Z, "Z", classes, batch)
+        l, st = self._vector(labels, "labels", batch, torch.int32), self._vector(starts, "starts", sequences + 1, torch.int32, True)
+        lp, su = self._vector(logp, "logp", batch, optional=True), self._vector(sums, "sums", sequences, optional=True)
+        return self.lib.label_log_probs(*z, l, classes, batch, st, sequences, lp, su, *self._scratch(workspace, "workspace"), self.handle(stream))
+
+    def policy(self, Z, labels, old_logp, ref_logp, advantages, weights, classes, batch, clip_low, clip_high, beta, dZ, logp, stats, workspace, stream):
+        self._numbers(classes, batch)
+        z = self._sized(Z, "Z", classes, batch)
+        l, o = self._vector(labels, "labels", batch, torch.int32), self._vector(old_logp, "old_logp", batch)
+        r, a = self._vector(ref_logp, "ref_logp", batch, optional=True), self._vector(advantages, "advantages", batch)
+        w = self._vector(weights, "weights", batch, optional=True)
+        dz = self._sized(dZ, "dZ", classes, batch)
+        lp, st = self._vector(logp, "logp", batch, optional=True), self._vector(stats, "stats", 4)
+        return self.lib.policy_loss(*z, l, o, r, a, w, classes, batch, clip_low, clip_high, beta, *dz, lp, st, *self._scratch(workspace, "workspace"),
+                                    self.handle(stream))
+
+    def preference(self, Z, labels, starts, ref_sums, classes, batch, pairs, beta, smoothing, dZ, sums, margins, loss, workspace, stream):
+        self._numbers(classes, batch, pairs)
+        z = self._sized(Z, "Z", classes, batch)
+        l, st = self._vector(labels, "labels", batch, torch.int32), self._vector(starts, "starts", 2 * pairs + 1, torch.int32)
+        r = self._vector(ref_sums, "ref_sums", 2 * pairs, optional=True)
+        dz = self._sized(dZ, "dZ", classes, batch)
+        su, m, lo = self._vector(sums, "sums", 2 * pairs, optional=True), self._vector(margins, "margins", pairs, optional=True), self._vector(loss, "loss", 1, optional=True)
+        return self.lib.preference_loss(*z, l, st, r, classes, batch, pairs, beta, smoothing, *dz, su, m, lo, *self._scratch(workspace, "workspace"), self.handle(stream))

@@ -17,6 +17,8 @@
 
 #include "experts.h"
 #include "kernels.h"
+#include "loss.h"
+#include "norm.h"
 
 using namespace nerva;
 
@@ -2284,6 +2286,186 @@ int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32
         a.partial = static_cast<float *>(workspace);
     }
     return launched(launch_combine_backward(a, as_stream(stream)), "expert_combine_backward", batch);
+}
+
+// ---- normalisation and dropout --------------------------------------------------------------------
+
+static int check_aligned(const void *workspace, size_t workspace_bytes, size_t need)
+{
+    if (need == 0) return NERVA_OK;
+    if (!workspace) return fail(NERVA_ERR_ARGUMENT, "workspace is null");
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(NERVA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+    if (workspace_bytes < need) return fail(NERVA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    return NERVA_OK;
+}
+
+// an output that starts where an input does is that input
+static int check_in_place(const float *in, int32_t ldi, const float *out, int32_t ldo, const char *what)
+{
+    if (in == out && ldi != ldo) return fail(NERVA_ERR_SHAPE, "%s in place need the same leading dimension (%d and %d)", what, ldi, ldo);
+    return NERVA_OK;
+}
+
+static int check_rows(int32_t rows, const char *name)
+{
+    if (rows < 1) return fail(NERVA_ERR_ARGUMENT, "%s must be positive (got %d)", name, rows);
+    if (rows >= (1 << 30)) return fail(NERVA_ERR_SHAPE, "%s = %d: 2^30 and more are not supported", name, rows);
+    return NERVA_OK;
+}
+
+static int check_drop(float drop, int32_t layer, const int64_t *state, DropArgs &d)
+{
+    if (!(drop >= 0.f && drop < 1.f)) return fail(NERVA_ERR_ARGUMENT, "drop must lie in [0, 1) (got %g)", static_cast<double>(drop));
+    d.cut = static_cast<uint32_t>(std::min(65535.0, static_cast<double>(drop) * 65536.0 + 0.5));
+    d.scale = static_cast<float>(65536.0 / (65536.0 - d.cut));
+    d.layer = static_cast<uint32_t>(layer);
+    d.state = state;
+    if (drop > 0.f && !state) return fail(NERVA_ERR_ARGUMENT, "drop needs a state");
+    if (reinterpret_cast<uintptr_t>(state) % 8) return fail(NERVA_ERR_ARGUMENT, "state must be 8-byte aligned");
+    return NERVA_OK;
+}
+
+static int check_norm(const NormArgs &a, float drop, int32_t layer, const int64_t *state, DropArgs &d)
+{
+    int rc = check_rows(a.features, "features");
+    if (rc != NERVA_OK) return rc;
+    if (a.groups < 1 || a.features % a.groups) return fail(NERVA_ERR_ARGUMENT, "%d features cannot be cut into %d groups", a.features, a.groups);
+    if (a.act != NERVA_ACT_NONE && a.act != NERVA_ACT_RELU && a.act != NERVA_ACT_SILU) return fail(NERVA_ERR_ARGUMENT, "unknown activation %d", a.act);
+    rc = check_batch(a.batch, static_cast<int32_t>(a.ldx), "ldx");
+    if (rc == NERVA_OK && (a.mean || a.rstd)) rc = check_batch(a.batch, static_cast<int32_t>(a.lds), "lds");
+    return rc == NERVA_OK ? check_drop(drop, layer, state, d) : rc;
+}
+
+size_t group_norm_workspace_bytes(int32_t features, int32_t groups, int32_t batch)
+{
+    NormArgs a{};
+    a.features = features; a.groups = groups; a.batch = batch; a.ldx = batch;
+    if (check_norm(a, 0.f, 0, nullptr, a.drop) != NERVA_OK) return SIZE_MAX;
+    return static_cast<size_t>(norm_scratch_floats(features, groups, batch)) * 4;
+}
+
+int group_norm_forward(const float *X, int32_t ldx, const float *gamma, const float *beta, int32_t features, int32_t groups, int32_t batch,
+                       float eps, int32_t act, float drop, int32_t layer, const int64_t *state, float *Y, int32_t ldy, float *mean, float *rstd,
+                       int32_t lds, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X || !Y) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    if (!mean != !rstd) return fail(NERVA_ERR_ARGUMENT, "mean and rstd go together");
+    if (!(eps > 0.f && eps <= 3.4e38f)) return fail(NERVA_ERR_ARGUMENT, "eps must be positive and finite (got %g)", static_cast<double>(eps));
+    NormArgs a{};
+    a.X = X; a.ldx = ldx; a.gamma = gamma; a.beta = beta; a.features = features; a.groups = groups; a.batch = batch; a.act = act; a.eps = eps;
+    a.Y = Y; a.ldy = ldy; a.mean = mean; a.rstd = rstd; a.lds = lds; a.workspace = static_cast<float *>(workspace);
+    int rc = check_norm(a, drop, layer, state, a.drop);
+    if (rc == NERVA_OK) rc = check_batch(batch, ldy, "ldy");
+    if (rc == NERVA_OK) rc = check_in_place(X, ldx, Y, ldy, "X and Y");
+    if (rc == NERVA_OK) rc = check_aligned(workspace, workspace_bytes, group_norm_workspace_bytes(features, groups, batch));
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_norm_forward(a, as_stream(stream)), "group_norm_forward", batch);
+}
+
+int group_norm_backward(const float *X, int32_t ldx, const float *gamma, const float *beta, const float *mean, const float *rstd, int32_t lds,
+                        const float *dY, int32_t lddy, int32_t features, int32_t groups, int32_t batch, int32_t act, float drop, int32_t layer,
+                        const int64_t *state, float *dX, int32_t lddx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes,
+                        void *stream)
+{
+    if (!X || !mean || !rstd || !dY || !dX) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    if (dX == X) return fail(NERVA_ERR_ARGUMENT, "dX must not be X");
+    NormArgs a{};
+    a.X = X; a.ldx = ldx; a.gamma = gamma; a.beta = beta; a.features = features; a.groups = groups; a.batch = batch; a.act = act;
+    a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd); a.lds = lds; a.dY = dY; a.lddy = lddy; a.dX = dX; a.lddx = lddx;
+    a.dgamma = dgamma; a.dbeta = dbeta; a.workspace = static_cast<float *>(workspace);
+    int rc = check_norm(a, drop, layer, state, a.drop);
+    if (rc == NERVA_OK) rc = check_batch(batch, lddy, "lddy");
+    if (rc == NERVA_OK) rc = check_batch(batch, lddx, "lddx");
+    if (rc == NERVA_OK) rc = check_in_place(dY, lddy, dX, lddx, "dY and dX");
+    if (rc == NERVA_OK) rc = check_aligned(workspace, workspace_bytes, group_norm_workspace_bytes(features, groups, batch));
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_norm_backward(a, as_stream(stream)), "group_norm_backward", batch);
+}
+
+int dropout(const float *X, int32_t ldx, int32_t features, int32_t batch, float drop, int32_t layer, const int64_t *state, float *Y, int32_t ldy,
+            void *stream)
+{
+    if (!X || !Y) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    DropoutArgs a{X, ldx, Y, ldy, features, batch, {}};
+    int rc = check_rows(features, "features");
+    if (rc == NERVA_OK) rc = check_batch(batch, ldx, "ldx");
+    if (rc == NERVA_OK) rc = check_batch(batch, ldy, "ldy");
+    if (rc == NERVA_OK) rc = check_in_place(X, ldx, Y, ldy, "X and Y");
+    if (rc == NERVA_OK) rc = check_drop(drop, layer, state, a.drop);
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_dropout(a, as_stream(stream)), "dropout", batch);
+}
+
+// ---- losses of labels --------------------------------------------------------------------------------
+
+static int check_labels(const LossArgs &a, const void *workspace, size_t workspace_bytes)
+{
+    int rc = check_rows(a.classes, "classes");
+    if (rc == NERVA_OK) rc = check_batch(a.batch, static_cast<int32_t>(a.ldz), "ldz");
+    if (rc == NERVA_OK && a.dZ) rc = check_batch(a.batch, static_cast<int32_t>(a.lddz), "lddz");
+    if (rc == NERVA_OK && a.dZ) rc = check_in_place(a.Z, static_cast<int32_t>(a.ldz), a.dZ, static_cast<int32_t>(a.lddz), "Z and dZ");
+    if (rc != NERVA_OK) return rc;
+    if (a.sequences < 0 || a.sequences >= (1 << 30)) return fail(NERVA_ERR_ARGUMENT, "%d sequences", a.sequences);
+    return check_aligned(workspace, workspace_bytes, static_cast<size_t>(loss_space(nullptr, a.classes, a.batch, a.sequences).bytes));
+}
+
+static int check_factor(float x, const char *name)
+{
+    return x >= 0.f && x <= 3.4e38f ? static_cast<int>(NERVA_OK) : fail(NERVA_ERR_ARGUMENT, "%s must be finite and not negative (got %g)", name, static_cast<double>(x));
+}
+
+size_t label_loss_workspace_bytes(int32_t classes, int32_t batch, int32_t sequences)
+{
+    if (check_rows(classes, "classes") != NERVA_OK || check_batch(batch, batch, "batch") != NERVA_OK) return 0;
+    if (sequences < 0 || sequences >= (1 << 30)) return fail(NERVA_ERR_ARGUMENT, "%d sequences", sequences), 0;
+    return static_cast<size_t>(loss_space(nullptr, classes, batch, sequences).bytes);
+}
+
+int label_log_probs(const float *Z, int32_t ldz, const int32_t *labels, int32_t classes, int32_t batch, const int32_t *starts, int32_t sequences,
+                    float *logp, float *sums, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!Z || !labels || (!logp && !sums)) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    if (sums && (!starts || sequences < 1)) return fail(NERVA_ERR_ARGUMENT, "sums need sequences (got %d) and their starts", sequences);
+    LossArgs a{};
+    a.Z = Z; a.ldz = ldz; a.labels = labels; a.classes = classes; a.batch = batch; a.sequences = sequences; a.starts = starts; a.logp = logp; a.sums = sums;
+    a.workspace = workspace;
+    const int rc = check_labels(a, workspace, workspace_bytes);
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_log_probs(a, as_stream(stream)), "label_log_probs", batch);
+}
+
+int policy_loss(const float *Z, int32_t ldz, const int32_t *labels, const float *old_logp, const float *ref_logp, const float *advantages,
+                const float *weights, int32_t classes, int32_t batch, float clip_low, float clip_high, float beta, float *dZ, int32_t lddz,
+                float *logp, float *stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!Z || !labels || !old_logp || !advantages || !dZ || !stats) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    int rc = check_factor(clip_low, "clip_low");
+    if (rc == NERVA_OK) rc = check_factor(clip_high, "clip_high");
+    if (rc == NERVA_OK) rc = check_factor(beta, "beta");
+    if (rc != NERVA_OK) return rc;
+    LossArgs a{};
+    a.Z = Z; a.ldz = ldz; a.labels = labels; a.classes = classes; a.batch = batch; a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantages = advantages;
+    a.weights = weights; a.clip_low = clip_low; a.clip_high = clip_high; a.beta = beta; a.dZ = dZ; a.lddz = lddz; a.logp = logp; a.stats = stats;
+    a.workspace = workspace;
+    rc = check_labels(a, workspace, workspace_bytes);
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_policy(a, as_stream(stream)), "policy_loss", batch);
+}
+
+int preference_loss(const float *Z, int32_t ldz, const int32_t *labels, const int32_t *starts, const float *ref_sums, int32_t classes, int32_t batch,
+                    int32_t pairs, float beta, float smoothing, float *dZ, int32_t lddz, float *sums, float *margins, float *loss, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    if (!Z || !labels || !starts || !dZ) return fail(NERVA_ERR_ARGUMENT, "null argument");
+    if (pairs < 1 || pairs >= (1 << 29)) return fail(NERVA_ERR_ARGUMENT, "%d pairs", pairs);
+    if (!(beta - beta == 0.f)) return fail(NERVA_ERR_ARGUMENT, "beta must be finite");
+    if (!(smoothing >= 0.f && smoothing <= 1.f)) return fail(NERVA_ERR_ARGUMENT, "smoothing must lie in [0, 1] (got %g)", static_cast<double>(smoothing));
+    LossArgs a{};
+    a.Z = Z; a.ldz = ldz; a.labels = labels; a.classes = classes; a.batch = batch; a.sequences = 2 * pairs; a.starts = starts; a.ref_sums = ref_sums;
+    a.beta = beta; a.smoothing = smoothing; a.dZ = dZ; a.lddz = lddz; a.sums = sums; a.margins = margins; a.loss = loss; a.workspace = workspace;
+    const int rc = check_labels(a, workspace, workspace_bytes);
+    if (rc != NERVA_OK) return rc;
+    return launched(launch_preference(a, as_stream(stream)), "preference_loss", batch);
 }
 
 int nerva_copy_f32(float *dst, const float *src, int64_t n, void *stream)

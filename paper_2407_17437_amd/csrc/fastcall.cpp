@@ -285,6 +285,17 @@ using Clip = int (*)(int32_t, const float *const *, float *const *, const int64_
 using UpdateClipped = int (*)(int32_t, float *const *, float *const *, const float *const *, const int64_t *, float, float, float, int32_t, void *, size_t, float *,
                               void *);
 
+using NormForward = int (*)(const float *, int32_t, const float *, const float *, int32_t, int32_t, int32_t, float, int32_t, float, int32_t, const int64_t *, float *,
+                            int32_t, float *, float *, int32_t, void *, size_t, void *);
+using NormBackward = int (*)(const float *, int32_t, const float *, const float *, const float *, const float *, int32_t, const float *, int32_t, int32_t, int32_t,
+                             int32_t, int32_t, float, int32_t, const int64_t *, float *, int32_t, float *, float *, void *, size_t, void *);
+using Dropout = int (*)(const float *, int32_t, int32_t, int32_t, float, int32_t, const int64_t *, float *, int32_t, void *);
+using LogProbs = int (*)(const float *, int32_t, const int32_t *, int32_t, int32_t, const int32_t *, int32_t, float *, float *, void *, size_t, void *);
+using Policy = int (*)(const float *, int32_t, const int32_t *, const float *, const float *, const float *, const float *, int32_t, int32_t, float, float, float,
+                       float *, int32_t, float *, float *, void *, size_t, void *);
+using Preference = int (*)(const float *, int32_t, const int32_t *, const int32_t *, const float *, int32_t, int32_t, int32_t, float, float, float *, int32_t, float *,
+                           float *, float *, void *, size_t, void *);
+
 Route g_route;
 RouteBackward g_route_backward;
 Place g_place;
@@ -294,6 +305,12 @@ CombineBackward g_combine_backward;
 Norm g_norm;
 Clip g_clip;
 UpdateClipped g_update_clipped;
+NormForward g_norm_forward;
+NormBackward g_norm_backward;
+Dropout g_dropout;
+LogProbs g_log_probs;
+Policy g_policy;
+Preference g_preference;
 
 // Arguments by position; the first that does not fit leaves a Python exception and `ok` false.
 struct Given {
@@ -335,7 +352,7 @@ struct Given {
             return nullptr;
         }
         const at::Tensor *t = &THPVariable_Unpack(o);
-        if (t->scalar_type() != type) return refuse(name, type == at::kFloat ? "float32" : "int32"), nullptr;
+        if (t->scalar_type() != type) return refuse(name, type == at::kFloat ? "float32" : type == at::kInt ? "int32" : "int64"), nullptr;
         if (!t->is_cuda()) return refuse(name, "a tensor on the GPU"), nullptr;
         if (device < 0) device = c10::hip::current_device();
         if (t->get_device() != device) return refuse(name, "a tensor on the current device"), nullptr;
@@ -373,7 +390,7 @@ struct Given {
     T *vector(int i, const char *name, int64_t n, bool optional = false)
     {
         if (optional && none(i)) return nullptr;
-        const at::Tensor *t = tensor(v[i], name, std::is_same_v<T, float> ? at::kFloat : at::kInt);
+        const at::Tensor *t = tensor(v[i], name, std::is_same_v<T, float> ? at::kFloat : std::is_same_v<T, int64_t> ? at::kLong : at::kInt);
         if (!t) return nullptr;
         if (t->numel() < n || !t->is_contiguous()) return refuse(name, "a contiguous array of the call's size"), nullptr;
         return static_cast<T *>(t->data_ptr());
@@ -619,6 +636,136 @@ PyObject *bind_mixtures(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// (X, gamma, beta, features, groups, batch, eps, act, drop, layer, state, Y, mean, rstd, workspace, stream)
+PyObject *norm_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 16, [](Given &a) {
+        const int32_t features = a.integer(3), groups = a.integer(4), batch = a.integer(5), act = a.integer(7), layer = a.integer(9);
+        const float eps = a.real(6), drop = a.real(8);
+        int32_t ldx, ldy, lds, ldr;
+        const float *X = a.matrix<float>(0, "X", features, batch, ldx), *gamma = a.vector<float>(1, "gamma", features, true), *beta = a.vector<float>(2, "beta", features, true);
+        const int64_t *state = a.vector<int64_t>(10, "state", 2, true);
+        float *Y = a.matrix<float>(11, "Y", features, batch, ldy), *mean = a.matrix<float>(12, "mean", groups, batch, lds, true),
+              *rstd = a.matrix<float>(13, "rstd", groups, batch, ldr, true);
+        if (a.ok && mean && rstd && groups > 1 && lds != ldr) a.refuse("rstd", "the row stride of mean");
+        size_t room;
+        void *workspace = a.scratch(14, "workspace", room);
+        void *s = a.stream(15);
+        return [=] { return g_norm_forward(X, ldx, gamma, beta, features, groups, batch, eps, act, drop, layer, state, Y, ldy, mean, rstd, lds, workspace, room, s); };
+    });
+}
+
+// (X, gamma, beta, mean, rstd, dY, features, groups, batch, act, drop, layer, state, dX, dgamma, dbeta, workspace, stream)
+PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 18, [](Given &a) {
+        const int32_t features = a.integer(6), groups = a.integer(7), batch = a.integer(8), act = a.integer(9), layer = a.integer(11);
+        const float drop = a.real(10);
+        int32_t ldx, lds, ldr, lddy, lddx;
+        const float *X = a.matrix<float>(0, "X", features, batch, ldx), *gamma = a.vector<float>(1, "gamma", features, true), *beta = a.vector<float>(2, "beta", features, true);
+        const float *mean = a.matrix<float>(3, "mean", groups, batch, lds), *rstd = a.matrix<float>(4, "rstd", groups, batch, ldr);
+        if (a.ok && groups > 1 && lds != ldr) a.refuse("rstd", "the row stride of mean");
+        const float *dY = a.matrix<float>(5, "dY", features, batch, lddy);
+        const int64_t *state = a.vector<int64_t>(12, "state", 2, true);
+        float *dX = a.matrix<float>(13, "dX", features, batch, lddx), *dgamma = a.vector<float>(14, "dgamma", features, true), *dbeta = a.vector<float>(15, "dbeta", features, true);
+        size_t room;
+        void *workspace = a.scratch(16, "workspace", room);
+        void *s = a.stream(17);
+        return [=] {
+            return g_norm_backward(X, ldx, gamma, beta, mean, rstd, lds, dY, lddy, features, groups, batch, act, drop, layer, state, dX, lddx, dgamma, dbeta, workspace,
+                                   room, s);
+        };
+    });
+}
+
+// (X, features, batch, drop, layer, state, Y, stream)
+PyObject *dropout(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 8, [](Given &a) {
+        const int32_t features = a.integer(1), batch = a.integer(2), layer = a.integer(4);
+        const float drop = a.real(3);
+        int32_t ldx, ldy;
+        const float *X = a.matrix<float>(0, "X", features, batch, ldx);
+        const int64_t *state = a.vector<int64_t>(5, "state", 2, true);
+        float *Y = a.matrix<float>(6, "Y", features, batch, ldy);
+        void *s = a.stream(7);
+        return [=] { return g_dropout(X, ldx, features, batch, drop, layer, state, Y, ldy, s); };
+    });
+}
+
+// (Z, labels, classes, batch, starts, sequences, logp, sums, workspace, stream)
+PyObject *log_probs(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 10, [](Given &a) {
+        const int32_t classes = a.integer(2), batch = a.integer(3), sequences = a.integer(5);
+        int32_t ldz;
+        const float *Z = a.matrix<float>(0, "Z", classes, batch, ldz);
+        const int32_t *labels = a.vector<int32_t>(1, "labels", batch), *starts = a.vector<int32_t>(4, "starts", static_cast<int64_t>(sequences) + 1, true);
+        float *logp = a.vector<float>(6, "logp", batch, true), *sums = a.vector<float>(7, "sums", sequences, true);
+        size_t room;
+        void *workspace = a.scratch(8, "workspace", room);
+        void *s = a.stream(9);
+        return [=] { return g_log_probs(Z, ldz, labels, classes, batch, starts, sequences, logp, sums, workspace, room, s); };
+    });
+}
+
+// (Z, labels, old_logp, ref_logp, advantages, weights, classes, batch, clip_low, clip_high, beta, dZ, logp, stats, workspace, stream)
+PyObject *policy(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 16, [](Given &a) {
+        const int32_t classes = a.integer(6), batch = a.integer(7);
+        const float low = a.real(8), high = a.real(9), beta = a.real(10);
+        int32_t ldz, lddz;
+        const float *Z = a.matrix<float>(0, "Z", classes, batch, ldz);
+        const int32_t *labels = a.vector<int32_t>(1, "labels", batch);
+        const float *old = a.vector<float>(2, "old_logp", batch), *ref = a.vector<float>(3, "ref_logp", batch, true), *advantages = a.vector<float>(4, "advantages", batch),
+                    *weights = a.vector<float>(5, "weights", batch, true);
+        float *dZ = a.matrix<float>(11, "dZ", classes, batch, lddz), *logp = a.vector<float>(12, "logp", batch, true), *stats = a.vector<float>(13, "stats", 4);
+        size_t room;
+        void *workspace = a.scratch(14, "workspace", room);
+        void *s = a.stream(15);
+        return [=] { return g_policy(Z, ldz, labels, old, ref, advantages, weights, classes, batch, low, high, beta, dZ, lddz, logp, stats, workspace, room, s); };
+    });
+}
+
+// (Z, labels, starts, ref_sums, classes, batch, pairs, beta, smoothing, dZ, sums, margins, loss, workspace, stream)
+PyObject *preference(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return run_given(args, n, 15, [](Given &a) {
+        const int32_t classes = a.integer(4), batch = a.integer(5), pairs = a.integer(6);
+        const float beta = a.real(7), smoothing = a.real(8);
+        const int64_t sequences = 2 * static_cast<int64_t>(pairs);
+        int32_t ldz, lddz;
+        const float *Z = a.matrix<float>(0, "Z", classes, batch, ldz);
+        const int32_t *labels = a.vector<int32_t>(1, "labels", batch), *starts = a.vector<int32_t>(2, "starts", sequences + 1);
+        const float *ref = a.vector<float>(3, "ref_sums", sequences, true);
+        float *dZ = a.matrix<float>(9, "dZ", classes, batch, lddz), *sums = a.vector<float>(10, "sums", sequences, true), *margins = a.vector<float>(11, "margins", pairs, true),
+              *loss = a.vector<float>(12, "loss", 1, true);
+        size_t room;
+        void *workspace = a.scratch(13, "workspace", room);
+        void *s = a.stream(14);
+        return [=] { return g_preference(Z, ldz, labels, starts, ref, classes, batch, pairs, beta, smoothing, dZ, lddz, sums, margins, loss, workspace, room, s); };
+    });
+}
+
+// addresses of the six entry points above, in their order
+PyObject *bind_losses(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "six addresses expected");
+        return nullptr;
+    }
+    Args a{args};
+    g_norm_forward = reinterpret_cast<NormForward>(a.address());
+    g_norm_backward = reinterpret_cast<NormBackward>(a.address());
+    g_dropout = reinterpret_cast<Dropout>(a.address());
+    g_log_probs = reinterpret_cast<LogProbs>(a.address());
+    g_policy = reinterpret_cast<Policy>(a.address());
+    g_preference = reinterpret_cast<Preference>(a.address());
+    if (!a.ok) return nullptr;
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind)), METH_FASTCALL, nullptr},
     {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(forward)), METH_FASTCALL, nullptr},
@@ -637,6 +784,13 @@ PyMethodDef methods[] = {
     {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(norm)), METH_FASTCALL, nullptr},
     {"clip", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(clip)), METH_FASTCALL, nullptr},
     {"update_clipped", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(update_clipped)), METH_FASTCALL, nullptr},
+    {"bind_losses", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_losses)), METH_FASTCALL, nullptr},
+    {"norm_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(norm_forward)), METH_FASTCALL, nullptr},
+    {"norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(norm_backward)), METH_FASTCALL, nullptr},
+    {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(dropout)), METH_FASTCALL, nullptr},
+    {"log_probs", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(log_probs)), METH_FASTCALL, nullptr},
+    {"policy", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(policy)), METH_FASTCALL, nullptr},
+    {"preference", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(preference)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
