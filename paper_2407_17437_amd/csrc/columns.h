@@ -14,13 +14,17 @@ inline int lanes_for(int32_t batch, int most)
     return lg;
 }
 
+// Operands that together are larger than the memory-side cache: what is written would only push out what is still to be read.
+constexpr int64_t kCacheBytes = INT64_C(256) << 20;
+
 // Where a thread stands: its four columns, of which n exist.
 struct Spot {
     int q, slot, slots;      // quad in the tile; place among the threads of that quad
-    int col, n;
+    int col, n, batch;
     bool whole;              // all columns of the tile exist (the same for all threads)
+    bool past;               // results are written past the caches (the same for all threads)
 };
-__device__ __forceinline__ Spot spot_in(int64_t tile, int lg, int batch)
+__device__ __forceinline__ Spot spot_in(int64_t tile, int lg, int batch, bool past = false)
 {
     Spot p;
     p.q = threadIdx.x & ((1 << lg) - 1);
@@ -30,28 +34,40 @@ __device__ __forceinline__ Spot spot_in(int64_t tile, int lg, int batch)
     p.whole = first + (4 << lg) <= batch;
     p.col = static_cast<int>(first) + 4 * p.q;
     p.n = min(4, max(0, batch - p.col));
+    p.batch = batch;
+    p.past = past;
     return p;
 }
 
-// Four columns of a row.  Lanes that have fewer read and write one by one, so that an output may lie where the input does.
+// Four columns of a row.  In a tile that is not whole they are read and written one by one, so that an output may lie where the input does and
+// nothing beyond the batch is touched; what is read in place of a column that does not exist is the batch's last one.
 __device__ __forceinline__ float4 load_quad(const float *row, const Spot &p)
 {
-    if (p.whole || p.n == 4) return ld4(row + p.col);
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p.n > 0) x.x = row[p.col];
-    if (p.n > 1) x.y = row[p.col + 1];
-    if (p.n > 2) x.z = row[p.col + 2];
-    return x;
+    if (p.whole) return ld4(row + p.col);
+    const int last = p.batch - 1;
+    return make_float4(row[min(p.col, last)], row[min(p.col + 1, last)], row[min(p.col + 2, last)], row[min(p.col + 3, last)]);
 }
 __device__ __forceinline__ void store_quad(float *row, const Spot &p, float4 x)
 {
-    if (p.whole || p.n == 4) {
-        st4(row + p.col, x);
+    if (p.whole) {
+        if (p.past) {
+            const v4f_any r = {x.x, x.y, x.z, x.w};
+            __builtin_nontemporal_store(r, reinterpret_cast<v4f_any *>(row + p.col));
+        } else {
+            st4(row + p.col, x);
+        }
         return;
     }
     if (p.n > 0) row[p.col] = x.x;
     if (p.n > 1) row[p.col + 1] = x.y;
     if (p.n > 2) row[p.col + 2] = x.z;
+    if (p.n > 3) row[p.col + 3] = x.w;
+}
+// 0 for columns that do not exist
+__device__ __forceinline__ float4 existing(float4 x, const Spot &p)
+{
+    if (p.whole) return x;
+    return make_float4(p.n > 0 ? x.x : 0.f, p.n > 1 ? x.y : 0.f, p.n > 2 ? x.z : 0.f, p.n > 3 ? x.w : 0.f);
 }
 
 __device__ __forceinline__ float4 splat(float x) { return make_float4(x, x, x, x); }
@@ -66,17 +82,8 @@ __device__ __forceinline__ float4 shfl_xor4(float4 v, int d)
 }
 __device__ __forceinline__ float sum4(float4 v) { return (v.x + v.y) + (v.z + v.w); }
 
-// exp(x) with an error of about one unit in the last place: the product with log2(e) is formed in two parts, the second of which the exponential's
-// own argument would lose.  (v_exp_f32 of the rounded product alone is off by 2^-24 |x| relative to the result.)
-__device__ __forceinline__ float exp_of(float x)
-{
-    constexpr float hi = 1.44269504f, lo = 1.92596299e-8f;
-    const float t = x * hi;
-    const float rest = fmaf(x, lo, fmaf(x, hi, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    // (an infinite x has no rest, and beside an e of 0 or infinity there is nothing to mend)
-    return (e > 0.f && e < 3.0e38f) ? fmaf(e, rest * 0.693147181f, e) : e;
-}
+// exp(x) by one v_exp_f32: relative error 2^-24 (2 |x| + 2), of which the first part is the rounding of the argument
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.92596299e-8f, x * 1.44269504f)); }
 
 }  // namespace
 }  // namespace nerva

@@ -29,9 +29,7 @@ constexpr int kLoads = 8;              // rows in flight per thread
 constexpr int kColumns = 256;          // columns of a work-group that adds up chunks
 constexpr int64_t kBlocks = 2048;      // work-groups that the classes are cut for
 
-// exp(x), x <= 0 or NaN, by one v_exp_f32: relative error 2^-24 (2 |x| + 2)
-__device__ __forceinline__ float exp_below(float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.92596299e-8f, x * 1.44269504f)); }
-__device__ __forceinline__ float4 exp_below4(float4 x) { return make_float4(exp_below(x.x), exp_below(x.y), exp_below(x.z), exp_below(x.w)); }
+__device__ __forceinline__ float4 exp_of4(float4 x) { return make_float4(exp_of(x.x), exp_of(x.y), exp_of(x.z), exp_of(x.w)); }
 __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w)); }
 
 struct Shape {
@@ -49,10 +47,10 @@ __device__ __forceinline__ void add_rows(Running &a, const float4 (&z)[kLoads])
     float4 top = a.top;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) top = max4(top, z[u]);
-    float4 s = exp_below4(z[0] - top);
+    float4 s = exp_of4(z[0] - top);
 #pragma unroll
-    for (int u = 1; u < kLoads; ++u) s = s + exp_below4(z[u] - top);
-    a.sum = fma4(a.sum, exp_below4(a.top - top), s);
+    for (int u = 1; u < kLoads; ++u) s = s + exp_of4(z[u] - top);
+    a.sum = fma4(a.sum, exp_of4(a.top - top), s);
     a.top = top;
 }
 // over the threads with the same columns; the same in all of them
@@ -62,7 +60,7 @@ __device__ __forceinline__ Running join(Running a, int lg, float4 (*lds)[kThread
     for (int d = 1 << lg; d < kWave; d <<= 1) {
         const float4 top = max4(a.top, shfl_xor4(a.top, d));
         // (both lanes of a pair add the lower one's sum first)
-        const float4 mine = a.sum * exp_below4(a.top - top), other = shfl_xor4(mine, d);
+        const float4 mine = a.sum * exp_of4(a.top - top), other = shfl_xor4(mine, d);
         a.sum = lane & d ? other + mine : mine + other;
         a.top = top;
     }
@@ -74,7 +72,7 @@ __device__ __forceinline__ Running join(Running a, int lg, float4 (*lds)[kThread
     a.top = lds[0][q];
     for (int w = 1; w < kThreads / kWave; ++w) a.top = max4(a.top, lds[0][(w << lg) + q]);
     a.sum = splat(0.f);
-    for (int w = 0; w < kThreads / kWave; ++w) a.sum = fma4(lds[1][(w << lg) + q], exp_below4(lds[0][(w << lg) + q] - a.top), a.sum);
+    for (int w = 0; w < kThreads / kWave; ++w) a.sum = fma4(lds[1][(w << lg) + q], exp_of4(lds[0][(w << lg) + q] - a.top), a.sum);
     return a;
 }
 
@@ -308,7 +306,7 @@ __device__ void write_preference_loss(const LossArgs &a, const double *shares, i
 __device__ __forceinline__ float gradient_of(float z, const ColumnState &c, int i)
 {
     if (c.c == 0.f) return 0.f;
-    return fmaf(-c.share, exp_below(z - c.top), i == c.label ? c.c : 0.f);
+    return fmaf(-c.share, exp_of(z - c.top), i == c.label ? c.c : 0.f);
 }
 
 // One work-group: a chunk of the classes in a tile of columns.  `shares`: how many shares of the loss there are (policy: of four terms each).

@@ -10,6 +10,7 @@
 // columns and holds all of its entries in registers, so that statistics and results take one read.  Groups that are too long for that
 // are cut into chunks: one launch leaves every chunk's statistics, a second one adds them up and reads the entries again.
 #include <algorithm>
+#include <type_traits>
 
 #include "columns.h"
 #include "experts.h"
@@ -20,6 +21,7 @@ namespace {
 
 constexpr int kLanes = 3;              // log2 of the quads of a tile: 32 columns, whose rows are 128-byte lines
 constexpr int kThreadsMost = 1024;
+constexpr int kChunkThreads = 256;     // of groups that are cut into chunks
 
 // ---- the generator ----
 // Philox4x32 of 10 rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011), key = seed.  Counter (column / 4, row / 2,
@@ -66,27 +68,26 @@ __device__ __forceinline__ float4 drop(float4 x, const Bits &b, int row, const D
 
 // ---- activations ----
 constexpr int kRelu = 1, kSilu = 2;
-__device__ __forceinline__ float sigmoid_of(float u) { return 1.f / (1.f + exp_of(-u)); }
-__device__ __forceinline__ float activate(float u, int act)
+// (v_rcp_f32 is off by one unit in the last place, a division would take ten instructions.  The argument's rounding counts where exp(-u) does: below
+// 1.2 roundings for u >= 0, 2 |u| for u < 0, where the result is small.)
+__device__ __forceinline__ float sigmoid_of(float u) { return __builtin_amdgcn_rcpf(1.f + exp_of(-u)); }
+// (act is the same for all threads; a NaN stays one)
+__device__ __forceinline__ float4 activate4(float4 u, int act)
 {
-    if (act == kRelu) return u < 0.f ? 0.f : u;
-    if (act == kSilu) return u * sigmoid_of(u);
+    if (act == kRelu) return make_float4(u.x < 0.f ? 0.f : u.x, u.y < 0.f ? 0.f : u.y, u.z < 0.f ? 0.f : u.z, u.w < 0.f ? 0.f : u.w);
+    if (act == kSilu) return make_float4(u.x * sigmoid_of(u.x), u.y * sigmoid_of(u.y), u.z * sigmoid_of(u.z), u.w * sigmoid_of(u.w));
     return u;
 }
-// e act'(u)
-__device__ __forceinline__ float activate_back(float e, float u, int act)
+__device__ __forceinline__ float silu_slope(float u)
 {
-    if (act == kRelu) return u > 0.f ? e : 0.f;
-    if (act == kSilu) {
-        const float s = sigmoid_of(u);
-        return e * (s * fmaf(u, 1.f - s, 1.f));
-    }
-    return e;
+    const float s = sigmoid_of(u);
+    return s * fmaf(u, 1.f - s, 1.f);
 }
-__device__ __forceinline__ float4 activate4(float4 u, int act) { return make_float4(activate(u.x, act), activate(u.y, act), activate(u.z, act), activate(u.w, act)); }
+// e act'(u)
 __device__ __forceinline__ float4 activate_back4(float4 e, float4 u, int act)
 {
-    return make_float4(activate_back(e.x, u.x, act), activate_back(e.y, u.y, act), activate_back(e.z, u.z, act), activate_back(e.w, u.w, act));
+    if (act == kRelu) return keep_where_positive(e, u);
+    return make_float4(e.x * silu_slope(u.x), e.y * silu_slope(u.y), e.z * silu_slope(u.z), e.w * silu_slope(u.w));
 }
 
 // ---- sums down the columns ----
@@ -141,12 +142,24 @@ __device__ __forceinline__ Rows<K> rows_of(const NormArgs &a, int group, int chu
 
 struct Shape {
     int lg, chunks, slabs;
+    bool past;
     int64_t tiles;
 };
+// Tile of work-group b of n: those that share 128-byte lines (tiles of less than 32 columns) come to the same XCD, to which ids go in turn, so that its L2
+// serves a line to all of them.
+__device__ __forceinline__ int64_t near_tile(int64_t b, int64_t n, int lg)
+{
+    const int shift = kLanes - lg;
+    if (shift <= 0) return b;
+    const int64_t set = b >> (3 + shift);
+    if ((set + 1) << (3 + shift) > n) return b;
+    const int in_set = static_cast<int>(b) & ((8 << shift) - 1);
+    return (set << (3 + shift)) + ((in_set & 7) << shift) + (in_set >> 3);
+}
 
-// statistics of the entries that the work-group holds: mean and sum of squares about it
+// statistics of the entries that the work-group holds: mean and sum of squares about it; x becomes its difference from the mean
 template <int K>
-__device__ __forceinline__ void statistics(const float4 (&x)[2 * K], const Rows<K> &r, int lg, float4 (*lds)[kThreadsMost / kWave << kLanes], float4 &mean, float4 &squares)
+__device__ __forceinline__ void statistics(float4 (&x)[2 * K], const Rows<K> &r, int lg, float4 (*lds)[kThreadsMost / kWave << kLanes], float4 &mean, float4 &squares)
 {
     const int n = r.end - r.first;
     float4 s = splat(0.f);
@@ -157,8 +170,8 @@ __device__ __forceinline__ void statistics(const float4 (&x)[2 * K], const Rows<
     float4 s2 = splat(0.f);
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
-        const float4 d = x[i] - mean;
-        if (r.in(i)) s2 = fma4(d, d, s2);
+        x[i] = x[i] - mean;
+        if (r.in(i)) s2 = fma4(x[i], x[i], s2);
     }
     squares = column_sum(s2, lg, lds[1]);
 }
@@ -169,7 +182,7 @@ __device__ __forceinline__ float4 rstd_of(float4 squares, int m, float eps)
 }
 
 template <int K>
-__device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&x)[2 * K], const Rows<K> &r, const Spot &p, float4 mean, float4 rstd)
+__device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&x)[2 * K], const Rows<K> &r, const Spot &p, float4 rstd)
 {
     Drawn d{};
     if (a.drop.cut) d = drawn_from(a.drop);
@@ -177,9 +190,12 @@ __device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
         const int f = r.row(i);
-        if (a.drop.cut && !(i & 1)) bits = bits_of(d, p.col, f >> 1);
+        if (!(i & 1)) {
+            __builtin_amdgcn_sched_barrier(0);   // (a pair after the other: all at once take more registers than there are)
+            if (a.drop.cut) bits = bits_of(d, p.col, f >> 1);
+        }
         if (!r.in(i)) continue;
-        const float4 xh = (x[i] - mean) * rstd;
+        const float4 xh = x[i] * rstd;   // (x: less the mean)
         float4 y = activate4(fma4(splat(a.gamma ? a.gamma[f] : 1.f), xh, splat(a.beta ? a.beta[f] : 0.f)), a.act);
         if (a.drop.cut) y = drop(y, bits, i & 1, a.drop);
         store_quad(a.Y + f * a.ldy, p, y);
@@ -188,13 +204,13 @@ __device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&
 
 // One work-group: a chunk of a group in a tile of columns.  WHOLE: the chunk is the group.  Otherwise its statistics go to the workspace,
 // {mean, sum of squares about it} (groups, chunks, batch).
-template <int K, bool WHOLE>
-__global__ __launch_bounds__(kThreadsMost) void norm_forward_kernel(const NormArgs a, const Shape z)
+template <int K, int T, bool WHOLE>
+__global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const Shape z)
 {
     __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
-    const int64_t unit = blockIdx.x / z.chunks, tile = unit % z.tiles;
+    const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
-    const Spot p = spot_in(tile, z.lg, a.batch);
+    const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K], mean, squares;
     r.load(a.X, a.ldx, p, x);
@@ -205,7 +221,7 @@ __global__ __launch_bounds__(kThreadsMost) void norm_forward_kernel(const NormAr
             if (a.mean) store_quad(a.mean + group * a.lds, p, mean);
             if (a.rstd) store_quad(a.rstd + group * a.lds, p, rstd);
         }
-        write_forward<K>(a, x, r, p, mean, rstd);
+        write_forward<K>(a, x, r, p, rstd);
     } else if (p.slot == 0) {
         float *const at = a.workspace + 2 * (static_cast<int64_t>(group) * z.chunks + chunk) * a.batch;
         store_quad(at, p, mean);
@@ -215,41 +231,59 @@ __global__ __launch_bounds__(kThreadsMost) void norm_forward_kernel(const NormAr
 
 // the second launch of a group of several chunks
 template <int K>
-__global__ __launch_bounds__(kThreadsMost) void norm_apply_kernel(const NormArgs a, const Shape z)
+__global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArgs a, const Shape z)
 {
-    const int64_t unit = blockIdx.x / z.chunks, tile = unit % z.tiles;
+    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
-    const Spot p = spot_in(tile, z.lg, a.batch);
+    const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K];
     r.load(a.X, a.ldx, p, x);
-    // the chunks' means weighed by their rows, then all squares about the mean of the group (Chan, Golub, LeVeque 1979)
+    // the chunks' means weighed by their rows, then all squares about the mean of the group (Chan, Golub, LeVeque 1979); a thread adds up every
+    // slots-th chunk
     const int m = a.features / a.groups;
     const float *const stats = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
     float4 mean = splat(0.f), squares = splat(0.f);
-    for (int c = 0; c < z.chunks; ++c) {
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
         const Rows<K> of = rows_of<K>(a, group, c, p);
         mean = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p), mean);
     }
-    mean = 1.f / static_cast<float>(m) * mean;
-    for (int c = 0; c < z.chunks; ++c) {
+    mean = 1.f / static_cast<float>(m) * column_sum(mean, z.lg, lds[0]);
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
         const Rows<K> of = rows_of<K>(a, group, c, p);
         const float *const at = stats + 2 * static_cast<int64_t>(c) * a.batch;
         const float4 d = load_quad(at, p) - mean;
         squares = squares + fma4(static_cast<float>(of.end - of.first) * d, d, load_quad(at + a.batch, p));
     }
+    squares = column_sum(squares, z.lg, lds[1]);
     const float4 rstd = rstd_of(squares, m, a.eps);
     if (p.slot == 0 && chunk == 0) {
         if (a.mean) store_quad(a.mean + group * a.lds, p, mean);
         if (a.rstd) store_quad(a.rstd + group * a.lds, p, rstd);
     }
-    write_forward<K>(a, x, r, p, mean, rstd);
+#pragma unroll
+    for (int i = 0; i < 2 * K; ++i) x[i] = x[i] - mean;
+    write_forward<K>(a, x, r, p, rstd);
 }
 
 // ---- backward ----
+// the rows' gamma and beta
+template <int K>
+struct Affine {
+    float gamma[2 * K], beta[2 * K];
+    __device__ __forceinline__ void load(const NormArgs &a, const Rows<K> &r)
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) {
+            gamma[i] = a.gamma ? a.gamma[r.readable(i)] : 1.f;
+            beta[i] = a.beta && a.act ? a.beta[r.readable(i)] : 0.f;
+        }
+    }
+};
 // x becomes xh, g becomes h; what the rows add to the gradients of gamma and beta from this thread's columns is added to `dg` and `db`
 template <int K>
-__device__ __forceinline__ void form_h(const NormArgs &a, float4 (&x)[2 * K], float4 (&g)[2 * K], const Rows<K> &r, const Spot &p, float4 mean, float4 rstd,
+__device__ __forceinline__ void form_h(const NormArgs &a, float4 (&x)[2 * K], float4 (&g)[2 * K], const Rows<K> &r, const Affine<K> &w, const Spot &p, float4 mean, float4 rstd,
                                        float (&dg)[2 * K], float (&db)[2 * K])
 {
     Drawn d{};
@@ -257,19 +291,20 @@ __device__ __forceinline__ void form_h(const NormArgs &a, float4 (&x)[2 * K], fl
     Bits bits{};
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
-        const int f = r.readable(i);
-        if (a.drop.cut && !(i & 1)) bits = bits_of(d, p.col, r.row(i) >> 1);
+        if (!(i & 1)) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (a.drop.cut) bits = bits_of(d, p.col, r.row(i) >> 1);
+        }
         x[i] = (x[i] - mean) * rstd;
-        const float gamma = a.gamma ? a.gamma[f] : 1.f;
         float4 e = g[i];
         if (a.drop.cut) e = drop(e, bits, i & 1, a.drop);
-        if (a.act) e = activate_back4(e, fma4(splat(gamma), x[i], splat(a.beta ? a.beta[f] : 0.f)), a.act);
-        if (!r.in(i)) e = splat(0.f);
-        const float4 ex = e * x[i];
-        // (columns that do not exist hold zeros in e)
-        dg[i] += r.in(i) ? sum4(ex) : 0.f;
-        db[i] += sum4(e);
-        g[i] = gamma * e;
+        if (a.act) e = activate_back4(e, fma4(splat(w.gamma[i]), x[i], splat(w.beta[i])), a.act);
+        const float4 own = existing(e, p);
+        if (r.in(i)) {
+            dg[i] += sum4(existing(e * x[i], p));
+            db[i] += sum4(own);
+        }
+        g[i] = w.gamma[i] * e;
     }
 }
 template <int K>
@@ -300,7 +335,7 @@ __device__ __forceinline__ void write_backward(const NormArgs &a, const float4 (
 // Sums of the gradients of gamma and beta over the work-group's columns, to slab `slab` of (slabs, 2, features), or to the gradients themselves
 // where there is one slab.
 template <int K>
-__device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int n_slabs, int slab, const Rows<K> &r, const Spot &p, int lg, float (&dg)[2 * K], float (&db)[2 * K])
+__device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int n_slabs, int slab, const Rows<K> &r, int lg, float (&dg)[2 * K], float (&db)[2 * K])
 {
     if (!a.dgamma && !a.dbeta) return;
     float *const g = n_slabs == 1 ? a.dgamma : slabs + 2 * static_cast<int64_t>(slab) * a.features;
@@ -311,7 +346,7 @@ __device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int 
             dg[i] += __shfl_xor(dg[i], d, kWave);
             db[i] += __shfl_xor(db[i], d, kWave);
         }
-        if (p.q == 0 && r.in(i)) {
+        if (!(threadIdx.x & ((1 << lg) - 1)) && r.in(i)) {
             if (g) g[r.row(i)] = dg[i];
             if (b) b[r.row(i)] = db[i];
         }
@@ -320,23 +355,27 @@ __device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int 
 
 // A work-group takes the tiles slab, slab + slabs, ... of a chunk of a group.  WHOLE: the chunk is the group, and dX is written; otherwise the
 // sums of h and h xh go to the workspace, (groups, chunks, 2, batch).
-template <int K, bool WHOLE>
-__global__ __launch_bounds__(kThreadsMost) void norm_backward_kernel(const NormArgs a, const Shape z, float *slabs)
+template <int K, int T, bool WHOLE>
+__global__ __launch_bounds__(T) void norm_backward_kernel(const NormArgs a, const Shape z, float *slabs)
 {
     __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
     const int64_t unit = blockIdx.x / z.slabs;
-    const int slab = static_cast<int>(blockIdx.x % z.slabs), chunk = static_cast<int>(unit % z.chunks), group = static_cast<int>(unit / z.chunks);
+    const int slab = static_cast<int>(near_tile(blockIdx.x % z.slabs, z.slabs, z.lg)), chunk = static_cast<int>(unit % z.chunks), group = static_cast<int>(unit / z.chunks);
     float dg[2 * K], db[2 * K];
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) dg[i] = db[i] = 0.f;
+    Rows<K> r = rows_of<K>(a, group, chunk, spot_in(slab, z.lg, a.batch));
+    Affine<K> w;
+    w.load(a, r);
     for (int64_t tile = slab; tile < z.tiles; tile += z.slabs) {
-        const Spot p = spot_in(tile, z.lg, a.batch);
-        const Rows<K> r = rows_of<K>(a, group, chunk, p);
+        const Spot p = spot_in(tile, z.lg, a.batch, z.past);
+        // (rows' addresses in three operands, kept from one tile to the next, would take more registers than the entries)
+        asm volatile("" : "+v"(r.pair));
         float4 x[2 * K], g[2 * K], s, sx;
         r.load(a.X, a.ldx, p, x);
         r.load(a.dY, a.lddy, p, g);
         const float4 mean = load_quad(a.mean + group * a.lds, p), rstd = load_quad(a.rstd + group * a.lds, p);
-        form_h<K>(a, x, g, r, p, mean, rstd, dg, db);
+        form_h<K>(a, x, g, r, w, p, mean, rstd, dg, db);
         column_sums_of_h<K>(x, g, r, z.lg, lds, s, sx);
         if constexpr (WHOLE) {
             write_backward<K>(a, x, g, r, p, rstd, s, sx);
@@ -347,45 +386,60 @@ __global__ __launch_bounds__(kThreadsMost) void norm_backward_kernel(const NormA
         }
         __syncthreads();   // (the sums of the next tile go to the same memory)
     }
-    const Spot p = spot_in(0, z.lg, a.batch);
-    write_rows<K>(a, slabs, z.slabs, slab, rows_of<K>(a, group, chunk, p), p, z.lg, dg, db);
+    write_rows<K>(a, slabs, z.slabs, slab, r, z.lg, dg, db);
 }
 
 template <int K>
-__global__ __launch_bounds__(kThreadsMost) void norm_apply_backward_kernel(const NormArgs a, const Shape z)
+__global__ __launch_bounds__(kChunkThreads) void norm_apply_backward_kernel(const NormArgs a, const Shape z)
 {
-    const int64_t unit = blockIdx.x / z.chunks, tile = unit % z.tiles;
+    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
-    const Spot p = spot_in(tile, z.lg, a.batch);
+    const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K], g[2 * K];
     r.load(a.X, a.ldx, p, x);
     r.load(a.dY, a.lddy, p, g);
     const float4 mean = load_quad(a.mean + group * a.lds, p), rstd = load_quad(a.rstd + group * a.lds, p);
+    Affine<K> w;
+    w.load(a, r);
     float dg[2 * K] = {}, db[2 * K] = {};   // (left to the first launch)
-    form_h<K>(a, x, g, r, p, mean, rstd, dg, db);
+    form_h<K>(a, x, g, r, w, p, mean, rstd, dg, db);
     float4 s = splat(0.f), sx = splat(0.f);
-    const float *at = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
-    for (int c = 0; c < z.chunks; ++c, at += 2 * static_cast<int64_t>(a.batch)) {
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
+        const float *const at = a.workspace + 2 * (static_cast<int64_t>(group) * z.chunks + c) * a.batch;
         s = s + load_quad(at, p);
         sx = sx + load_quad(at + a.batch, p);
     }
+    s = column_sum(s, z.lg, lds[0]);
+    sx = column_sum(sx, z.lg, lds[1]);
     write_backward<K>(a, x, g, r, p, rstd, s, sx);
 }
 
-// The slabs' sums: 64 features a work-group, 16 waves that take every 16th slab.
-constexpr int kSlabWaves = 16;
+// The slabs' sums: 64 features a work-group, 16 waves that take every 16th slab, four at a time.
+constexpr int kSlabWaves = 16, kSlabLoads = 4;
 __global__ __launch_bounds__(kSlabWaves *kWave) void norm_slabs_kernel(const float *slabs, int n_slabs, int features, float *dgamma, float *dbeta)
 {
     __shared__ float lds[2][kSlabWaves][kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
     const int64_t f = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    const float *const at = slabs + min(f, static_cast<int64_t>(features) - 1);
     float g = 0.f, b = 0.f;
-    if (f < features)
-        for (int s = wave; s < n_slabs; s += kSlabWaves) {
-            g += slabs[2 * static_cast<int64_t>(s) * features + f];
-            b += slabs[(2 * static_cast<int64_t>(s) + 1) * features + f];
+    for (int s = wave; s < n_slabs; s += kSlabLoads * kSlabWaves) {
+        float x[2][kSlabLoads];
+#pragma unroll
+        for (int u = 0; u < kSlabLoads; ++u) {
+            const int64_t slab = 2 * static_cast<int64_t>(min(s + u * kSlabWaves, n_slabs - 1));
+            x[0][u] = at[slab * features];
+            x[1][u] = at[(slab + 1) * features];
         }
+#pragma unroll
+        for (int u = 0; u < kSlabLoads; ++u)
+            if (s + u * kSlabWaves < n_slabs) {
+                g += x[0][u];
+                b += x[1][u];
+            }
+    }
     lds[0][wave][lane] = g;
     lds[1][wave][lane] = b;
     __syncthreads();
@@ -401,9 +455,9 @@ __global__ __launch_bounds__(kSlabWaves *kWave) void norm_slabs_kernel(const flo
 // ---- dropout by itself ----
 constexpr int kDropThreads = 256;
 constexpr int kDropPairs = 2;          // pairs of rows per thread
-__global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs a, const int lg, const int64_t tiles)
+__global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs a, const int lg, const int64_t tiles, const bool past)
 {
-    const Spot p = spot_in(blockIdx.x % tiles, lg, a.batch);
+    const Spot p = spot_in(blockIdx.x % tiles, lg, a.batch, past);
     const int64_t pair0 = static_cast<int64_t>(blockIdx.x / tiles) * (kDropPairs * p.slots) + p.slot;
     if (p.n == 0) return;
     const float *const X = a.X;
@@ -431,37 +485,61 @@ struct Plan {
     Shape z;
     int threads, pairs;      // pairs: K
 };
-// `most`: pairs that a thread holds at most
-Plan plan_norm(int32_t features, int32_t groups, int32_t batch, int most)
+constexpr int64_t kFewGroups = 256;      // work-groups: one per compute unit
+struct Limits {
+    int most_pairs, most_threads;   // the most that a thread and a work-group hold of a group
+    int chunk_pairs;                // of a thread at most, where the group is longer
+    int bytes;                      // that an entry moves
+};
+constexpr Limits kForward{8, 1024, 4, 8}, kBackward{8, 512, 2, 12};
+constexpr int kGroupThreads = 256, kGroupPairs = 4;
+Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
 {
     Plan p{};
-    p.z.lg = lanes_for(batch, kLanes);
-    p.z.tiles = (batch + (INT64_C(4) << p.z.lg) - 1) >> (p.z.lg + 2);
-    const int64_t pairs = (static_cast<int64_t>(features / groups) + 1) / 2, held = pairs << p.z.lg;   // threads, of one pair each
+    const int64_t pairs = (static_cast<int64_t>(features / groups) + 1) / 2;
+    const auto tiles = [&](int lg) { return (batch + (INT64_C(4) << lg) - 1) >> (lg + 2); };
+    const int wide = lanes_for(batch, kLanes), widest = lanes_for(batch, 6);
+    p.z.lg = wide;
+    p.z.past = static_cast<int64_t>(features) * batch > kCacheBytes / l.bytes;
+    // Wider tiles for groups that leave lanes idle (groups of 8 rows, 64 groups x 4096 columns, both ways: 23.3 -> 16.1 us).  Narrower ones where there would
+    // be few work-groups, each with much to do (512 rows, 2 groups x 100 columns: 23.8 -> 13.6; 1024 rows, 1 x 1024: 30.6 -> 20.8); they would make 32 groups
+    // x 8192 columns read a line twice.
+    while (p.z.lg < widest && pairs << p.z.lg < kWave) ++p.z.lg;
+    while (p.z.lg > 0 && groups * tiles(p.z.lg) < kFewGroups && pairs << p.z.lg > kWave) --p.z.lg;
+    const bool few = groups * tiles(p.z.lg) < kFewGroups;
+    p.z.tiles = tiles(p.z.lg);
+    const int64_t held = pairs << p.z.lg;   // threads, of one pair each
     p.pairs = 1;
-    while (p.pairs < most && held > 256 * p.pairs) p.pairs *= 2;
+    while (p.pairs < kGroupPairs && held > kGroupThreads * p.pairs) p.pairs *= 2;
+    while (p.pairs < l.most_pairs && held > l.most_threads * p.pairs) p.pairs *= 2;
     int64_t threads = (held + p.pairs - 1) / p.pairs;
     threads = (threads + kWave - 1) / kWave * kWave;
     p.z.chunks = 1;
-    if (threads > kThreadsMost) {
-        // (chunks of a work-group of 256 threads)
-        p.pairs = most;
-        threads = 256;
-        const int64_t of_chunk = static_cast<int64_t>(most) * (threads >> p.z.lg);
-        p.z.chunks = static_cast<int>((pairs + of_chunk - 1) / of_chunk);
+    // In chunks what a work-group does not hold, and what few work-groups would take longer for than two launches do (8192 rows, 1 group x 32 columns,
+    // both ways: 55.7 -> 22.5 us; 8192 rows, one column: 26.2 -> 11.2).  Held whole, 8 x 1024 rows x 8192 columns take 333 us, in chunks 446.
+    if (threads > l.most_threads || (few && held > kThreadsMost)) {
+        p.z.lg = wide;
+        p.z.tiles = tiles(wide);
+        threads = kChunkThreads;
+        for (p.pairs = l.chunk_pairs;; p.pairs /= 2) {
+            const int64_t of_chunk = static_cast<int64_t>(p.pairs) * (threads >> p.z.lg);
+            p.z.chunks = static_cast<int>((pairs + of_chunk - 1) / of_chunk);
+            if (p.pairs == 1 || groups * p.z.tiles * p.z.chunks >= 2 * kFewGroups) break;
+        }
     }
     p.threads = static_cast<int>(threads);
     p.z.slabs = 1;
     return p;
 }
-constexpr int kForwardPairs = 8, kBackwardPairs = 4;
-constexpr int64_t kBackwardBlocks = 2048;
+constexpr int64_t kBackwardThreads = 2048 * 256;
 
+Plan plan_forward(int32_t features, int32_t groups, int32_t batch) { return plan_norm(features, groups, batch, kForward); }
+// Work-groups of the backward pass take tile after tile, and their sums for gamma and beta are a slab each: as many as the GPU holds about twice.
 Plan plan_backward(int32_t features, int32_t groups, int32_t batch)
 {
-    Plan p = plan_norm(features, groups, batch, kBackwardPairs);
+    Plan p = plan_norm(features, groups, batch, kBackward);
     const int64_t rows = static_cast<int64_t>(groups) * p.z.chunks;
-    p.z.slabs = static_cast<int>(std::max<int64_t>(1, std::min(p.z.tiles, kBackwardBlocks * 256 / p.threads / rows)));
+    p.z.slabs = static_cast<int>(std::max<int64_t>(1, std::min(p.z.tiles, kBackwardThreads / p.threads / rows)));
     return p;
 }
 int64_t chunk_floats(const Plan &p, int32_t groups, int32_t batch) { return p.z.chunks > 1 ? 2 * static_cast<int64_t>(groups) * p.z.chunks * batch : 0; }
@@ -470,30 +548,37 @@ int64_t chunk_floats(const Plan &p, int32_t groups, int32_t batch) { return p.z.
 
 int64_t norm_scratch_floats(int32_t features, int32_t groups, int32_t batch)
 {
-    const Plan f = plan_norm(features, groups, batch, kForwardPairs), b = plan_backward(features, groups, batch);
+    const Plan f = plan_forward(features, groups, batch), b = plan_backward(features, groups, batch);
     const int64_t slabs = b.z.slabs > 1 ? 2 * static_cast<int64_t>(b.z.slabs) * features : 0;
     return std::max(chunk_floats(f, groups, batch), chunk_floats(b, groups, batch) + slabs);
 }
 
-#define WITH_PAIRS(k, LAUNCH)                            \
-    switch (k) {                                         \
-    case 1: { constexpr int K = 1; LAUNCH; break; }      \
-    case 2: { constexpr int K = 2; LAUNCH; break; }      \
-    case 4: { constexpr int K = 4; LAUNCH; break; }      \
-    default: { constexpr int K = 8; LAUNCH; break; }     \
-    }
+template <int K>
+using Pairs = std::integral_constant<int, K>;
+// f of the pairs that a thread holds, `Most` at most
+template <int Most, typename F>
+void with_pairs(int pairs, F &&f)
+{
+    if constexpr (Most > 1)
+        if (pairs < Most) return with_pairs<Most / 2>(pairs, f);
+    f(Pairs<Most>());
+}
+// threads that the kernels of K pairs are compiled for
+constexpr int most_threads(int pairs, const Limits &l) { return pairs < kGroupPairs ? kGroupThreads : l.most_threads; }
 
 hipError_t launch_norm_forward(const NormArgs &a, hipStream_t s)
 {
-    const Plan p = plan_norm(a.features, a.groups, a.batch, kForwardPairs);
+    const Plan p = plan_forward(a.features, a.groups, a.batch);
     const int64_t blocks = p.z.tiles * a.groups * p.z.chunks;
     if (!fits_launch(blocks, p.threads)) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
     if (p.z.chunks == 1) {
-        WITH_PAIRS(p.pairs, (norm_forward_kernel<K, true><<<grid, threads, 0, s>>>(a, p.z)))
+        with_pairs<kForward.most_pairs>(p.pairs, [&](auto k) { norm_forward_kernel<k, most_threads(k, kForward), true><<<grid, threads, 0, s>>>(a, p.z); });
     } else {
-        norm_forward_kernel<kForwardPairs, false><<<grid, threads, 0, s>>>(a, p.z);
-        norm_apply_kernel<kForwardPairs><<<grid, threads, 0, s>>>(a, p.z);
+        with_pairs<kForward.chunk_pairs>(p.pairs, [&](auto k) {
+            norm_forward_kernel<k, kChunkThreads, false><<<grid, threads, 0, s>>>(a, p.z);
+            norm_apply_kernel<k><<<grid, threads, 0, s>>>(a, p.z);
+        });
     }
     return hipGetLastError();
 }
@@ -506,14 +591,13 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t s)
     float *const slabs = a.workspace + chunk_floats(p, a.groups, a.batch);
     const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
     if (p.z.chunks == 1) {
-        switch (p.pairs) {
-        case 1: norm_backward_kernel<1, true><<<grid, threads, 0, s>>>(a, p.z, slabs); break;
-        case 2: norm_backward_kernel<2, true><<<grid, threads, 0, s>>>(a, p.z, slabs); break;
-        default: norm_backward_kernel<4, true><<<grid, threads, 0, s>>>(a, p.z, slabs); break;
-        }
+        with_pairs<kBackward.most_pairs>(p.pairs, [&](auto k) { norm_backward_kernel<k, most_threads(k, kBackward), true><<<grid, threads, 0, s>>>(a, p.z, slabs); });
     } else {
-        norm_backward_kernel<kBackwardPairs, false><<<grid, threads, 0, s>>>(a, p.z, slabs);
-        norm_apply_backward_kernel<kBackwardPairs><<<static_cast<uint32_t>(rows * p.z.tiles), threads, 0, s>>>(a, p.z);
+        const dim3 every(static_cast<uint32_t>(rows * p.z.tiles));
+        with_pairs<kBackward.chunk_pairs>(p.pairs, [&](auto k) {
+            norm_backward_kernel<k, kChunkThreads, false><<<grid, threads, 0, s>>>(a, p.z, slabs);
+            norm_apply_backward_kernel<k><<<every, threads, 0, s>>>(a, p.z);
+        });
     }
     if (p.z.slabs > 1 && (a.dgamma || a.dbeta))
         norm_slabs_kernel<<<(a.features + kWave - 1) / kWave, kSlabWaves * kWave, 0, s>>>(slabs, p.z.slabs, a.features, a.dgamma, a.dbeta);
@@ -527,7 +611,7 @@ hipError_t launch_dropout(const DropoutArgs &a, hipStream_t s)
     const int64_t of_block = static_cast<int64_t>(kDropPairs) * (kDropThreads >> lg), pairs = (static_cast<int64_t>(a.features) + 1) / 2;
     const int64_t blocks = tiles * ((pairs + of_block - 1) / of_block);
     if (!fits_launch(blocks, kDropThreads)) return hipErrorInvalidConfiguration;
-    dropout_kernel<<<static_cast<uint32_t>(blocks), kDropThreads, 0, s>>>(a, lg, tiles);
+    dropout_kernel<<<static_cast<uint32_t>(blocks), kDropThreads, 0, s>>>(a, lg, tiles, 8 * static_cast<int64_t>(a.features) * a.batch > kCacheBytes);
     return hipGetLastError();
 }
 

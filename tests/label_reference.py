@@ -73,10 +73,13 @@ class Norm:
         rel = 0.5 * var_off / (var + eps) + 4 * E
         xh_off = rstd * (off + 2 * E * np.abs(x - mean)) + np.abs(xh) * rel
         u_off = np.abs(ga) * xh_off + 2 * E * (np.abs(ga * xh) + np.abs(be))
-        # (slopes of the activations stay below 1.1, of their slopes below 0.51)
+        # Slopes of the activations stay below 1.1, of their slopes below 0.51.  An exponential is off by (2 |u| + 2) E, a sigmoid s = 1 / (1 + e) by
+        # that times e / (1 + e) and 3 E for the sum and the reciprocal: below 1.2 E for u >= 0 (where (2 u + 2) e / (1 + e) has its largest value), 2 |u| E
+        # more for u < 0.  The slope s (1 + u (1 - s)) = s + u s (1 - s) has s' u as its second term, which loses as much again.
+        exp_off = (12 + 4 * np.maximum(-u, 0) * (act == 2)) * E
         y = keep * act_of(u, act)
         self.u = u.reshape(F, B)
-        self.Y, self.Y_tol = y.reshape(F, B), (keep * 1.1 * u_off + 12 * E * np.abs(y) + 1e-37).reshape(F, B)
+        self.Y, self.Y_tol = y.reshape(F, B), (keep * 1.1 * u_off + exp_off * np.abs(y) + 1e-37).reshape(F, B)
         self.mean, self.mean_tol = mean[:, 0], (off + E * np.abs(mean))[:, 0] + 1e-37
         self.rstd, self.rstd_tol = rstd[:, 0], (rstd * rel)[:, 0] + 1e-37
         if dY is None:
@@ -84,7 +87,7 @@ class Norm:
         e0 = keep * dY.astype(np.float64).reshape(groups, m, B)
         e = e0 * (slope_of(u, act) if positive is None else positive.reshape(groups, m, B))
         h = ga * e
-        e_off = np.abs(e0) * ((0.51 if act == 2 else 0) * u_off + 12 * E)
+        e_off = np.abs(e0) * ((0.51 if act == 2 else 0) * u_off + exp_off)
         h_off = np.abs(ga) * e_off + E * np.abs(h)
 
         def avg(t):
