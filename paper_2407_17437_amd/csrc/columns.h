@@ -39,6 +39,18 @@ __device__ __forceinline__ Spot spot_in(int64_t tile, int lg, int batch, bool pa
     return p;
 }
 
+// Tile of work-group b of n: those that share 128-byte lines (tiles of less than 32 columns) come to the same XCD, to which ids go in turn, so that its L2
+// serves a line to all of them.
+__device__ __forceinline__ int64_t near_tile(int64_t b, int64_t n, int lg)
+{
+    const int shift = 3 - lg;
+    if (shift <= 0) return b;
+    const int64_t set = b >> (3 + shift);
+    if ((set + 1) << (3 + shift) > n) return b;
+    const int in_set = static_cast<int>(b) & ((8 << shift) - 1);
+    return (set << (3 + shift)) + ((in_set & 7) << shift) + (in_set >> 3);
+}
+
 // Four columns of a row.  In a tile that is not whole they are read and written one by one, so that an output may lie where the input does and
 // nothing beyond the batch is touched; what is read in place of a column that does not exist is the batch's last one.
 __device__ __forceinline__ float4 load_quad(const float *row, const Spot &p)

@@ -8,10 +8,10 @@
 //                  dl = +-(sigmoid(x) - (1 - t)) beta / pairs
 //     dz_i = dl ([i == label] - p_i)
 //
-// Bound by memory: the logits are read for the sum of exponentials and, where a work-group cannot hold a column, again for the gradient.  The first
-// launch cuts the classes into chunks and leaves a maximum and a sum for each, from one pass with a running maximum; the second one, a thread per
-// column, adds them up and does what a column needs (in 64 bits: log-probabilities are added up over sequences and compared with borders, and
-// there are few of them); the last one writes the gradient.
+// Bound by memory.  Columns that a work-group can hold in registers are read once: maximum, sum, what a column needs, gradient.  Longer ones are cut into
+// chunks of classes: the first launch leaves a maximum and a sum for each, from one pass with a running maximum; the second adds them up, 16 threads
+// a column; the last one reads the logits again for the gradient.  What a column needs is done in 64 bits: log-probabilities are added up over
+// sequences and compared with borders, and there are few of them.
 #include <float.h>
 
 #include <algorithm>
@@ -23,11 +23,12 @@
 namespace nerva {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kLanes = 6;              // log2 of the quads of a tile: 256 columns
+constexpr int kThreads = 256;          // of chunks
+constexpr int kLanes = 6;              // log2 of the quads of their tiles: 256 columns
 constexpr int kLoads = 8;              // rows in flight per thread
-constexpr int kColumns = 256;          // columns of a work-group that adds up chunks
 constexpr int64_t kBlocks = 2048;      // work-groups that the classes are cut for
+constexpr int kColumns = 16, kParts = 16;   // columns of a work-group that adds up chunks, threads of a column
+constexpr int kHeldThreads = 1024, kHeldRows = 16;   // of a work-group that holds its columns
 
 __device__ __forceinline__ float4 exp_of4(float4 x) { return make_float4(exp_of(x.x), exp_of(x.y), exp_of(x.z), exp_of(x.w)); }
 __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w)); }
@@ -35,6 +36,7 @@ __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(
 struct Shape {
     int lg, chunks, rows;              // rows of a chunk
     int32_t tiles;
+    bool past;                         // results go past the caches
 };
 
 // Running maximum and sum of a thread's rows of its four columns.  The maximum starts at the lowest number, not at -inf, so that no
@@ -53,10 +55,10 @@ __device__ __forceinline__ void add_rows(Running &a, const float4 (&z)[kLoads])
     a.sum = fma4(a.sum, exp_of4(a.top - top), s);
     a.top = top;
 }
-// over the threads with the same columns; the same in all of them
-__device__ __forceinline__ Running join(Running a, int lg, float4 (*lds)[kThreads / kWave << kLanes])
+// over the threads with the same columns; the same in all of them.  lds: two float4 per wave and quad
+__device__ __forceinline__ Running join(Running a, int lg, float4 *lds)
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, q = threadIdx.x & ((1 << lg) - 1);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, q = threadIdx.x & ((1 << lg) - 1), waves = blockDim.x >> 6;
     for (int d = 1 << lg; d < kWave; d <<= 1) {
         const float4 top = max4(a.top, shfl_xor4(a.top, d));
         // (both lanes of a pair add the lower one's sum first)
@@ -64,22 +66,24 @@ __device__ __forceinline__ Running join(Running a, int lg, float4 (*lds)[kThread
         a.sum = lane & d ? other + mine : mine + other;
         a.top = top;
     }
+    if (waves == 1) return a;
+    float4 *const sums = lds + (waves << lg);
     if (lane < (1 << lg)) {
-        lds[0][(wave << lg) + lane] = a.top;
-        lds[1][(wave << lg) + lane] = a.sum;
+        lds[(wave << lg) + lane] = a.top;
+        sums[(wave << lg) + lane] = a.sum;
     }
     __syncthreads();
-    a.top = lds[0][q];
-    for (int w = 1; w < kThreads / kWave; ++w) a.top = max4(a.top, lds[0][(w << lg) + q]);
+    a.top = lds[q];
+    for (int w = 1; w < waves; ++w) a.top = max4(a.top, lds[(w << lg) + q]);
     a.sum = splat(0.f);
-    for (int w = 0; w < kThreads / kWave; ++w) a.sum = fma4(lds[1][(w << lg) + q], exp_of4(lds[0][(w << lg) + q] - a.top), a.sum);
+    for (int w = 0; w < waves; ++w) a.sum = fma4(sums[(w << lg) + q], exp_of4(lds[(w << lg) + q] - a.top), a.sum);
     return a;
 }
 
 // One work-group: a chunk of the classes in a tile of columns.
 __global__ __launch_bounds__(kThreads) void log_sum_kernel(const LossArgs a, const Shape z, float *partial)
 {
-    __shared__ float4 lds[2][kThreads / kWave << kLanes];
+    __shared__ float4 lds[2 * kThreads / kWave << kLanes];
     const int chunk = blockIdx.x % z.chunks;
     const Spot p = spot_in(blockIdx.x / z.chunks, z.lg, a.batch);
     const int first = chunk * z.rows, end = min(a.classes, first + z.rows);
@@ -100,36 +104,28 @@ __global__ __launch_bounds__(kThreads) void log_sum_kernel(const LossArgs a, con
     store_quad(at + a.batch, p, r.sum);
 }
 
-// A column's chunks added up: largest logit, sum of exponentials beyond it, and the label's log-probability (0 where the column does not count).
+// ---- what a column needs ----
 struct Column {
-    float top;
-    double sum, logp;
+    float top, at_label;     // largest logit; the label's
+    double sum, logp;        // of exp(z - top); 0 where the column does not count
     int label;
-    float at_label;
     bool counts;
 };
-__device__ __forceinline__ Column column_of(const LossArgs &a, const float *partial, int chunks, int col)
+__device__ __forceinline__ void read_label(const LossArgs &a, int col, Column &c)
 {
-    Column c;
     c.label = a.labels[col];
     const bool inside = c.label >= 0 && c.label < a.classes;
     c.at_label = inside ? a.Z[c.label * a.ldz + col] : -INFINITY;
     c.counts = inside && c.at_label != -INFINITY;
-    c.top = -FLT_MAX;
-    for (int k = 0; k < chunks; ++k) c.top = fmaxf(c.top, partial[2 * static_cast<int64_t>(k) * a.batch + col]);
-    c.sum = 0;
-    for (int k = 0; k < chunks; ++k) {
-        const float *const at = partial + 2 * static_cast<int64_t>(k) * a.batch + col;
-        c.sum += at[a.batch] * exp(static_cast<double>(at[0]) - c.top);
-    }
-    c.logp = c.counts ? static_cast<double>(c.at_label) - c.top - log(c.sum) : 0.0;
-    return c;
 }
-__device__ __forceinline__ ColumnState state_of(const Column &c, float slope)
+__device__ __forceinline__ void set_sum(Column &c, double sum)
 {
-    return {c.top, static_cast<float>(slope / c.sum), slope, c.label};
+    c.sum = sum;
+    c.logp = c.counts ? static_cast<double>(c.at_label) - c.top - log(sum) : 0.0;
 }
+__device__ __forceinline__ ColumnState state_of(const Column &c, float slope) { return {c.top, static_cast<float>(slope / c.sum), slope, c.label}; }
 
+// sum over a work-group in one fixed order; every thread gets it
 __device__ __forceinline__ double block_sum(double x, double *lds)
 {
 #pragma unroll
@@ -142,101 +138,292 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
     return s;
 }
 
+// sum of exp(z - top) of a column in 64 bits, by the whole work-group
+__device__ double exact_sum(const LossArgs &a, int col, double top, double *lds)
+{
+    double s = 0;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < a.classes; i += blockDim.x) s += exp(a.Z[i * a.ldz + col] - top);
+    return block_sum(s, lds);
+}
+
 // The clipped loss of a column.
 struct Borders {
     double low, high;        // of l - old: log(1 - clip_low), log(1 + clip_high)
     float margin;            // how far l may be off
 };
 struct PolicyTerm {
-    double surrogate, kl, slope;
+    double weight, surrogate, kl, slope;
     bool clipped, close;     // close: l does not tell on which side of its border the column lies
 };
-__device__ __forceinline__ PolicyTerm policy_term(const LossArgs &a, const Borders &b, double logp, int col)
+__device__ __forceinline__ PolicyTerm policy_term(const LossArgs &a, const Borders &b, const Column &c, int col)
 {
-    PolicyTerm t;
-    const double A = a.advantages[col], d = logp - a.old_logp[col], r = exp(d);
+    PolicyTerm t{};
+    t.weight = !c.counts ? 0 : a.weights ? static_cast<double>(a.weights[col]) : 1.0 / a.batch;
+    if (t.weight == 0) return t;
+    const double A = a.advantages[col], d = c.logp - a.old_logp[col], r = exp(d);
     const double border = A > 0 ? b.high : b.low;
     t.clipped = A > 0 ? d > border : A < 0 && d < border;
     t.close = A != 0 && fabs(d - border) <= b.margin;
     t.surrogate = -A * (!t.clipped ? r : A > 0 ? 1.0 + a.clip_high : 1.0 - a.clip_low);
     t.slope = t.clipped ? 0.0 : -A * r;
-    t.kl = 0;
     if (a.ref_logp) {
-        const double g = a.ref_logp[col] - logp, q = exp(g);
+        const double g = a.ref_logp[col] - c.logp, q = exp(g);
         t.kl = q - g - 1;
         t.slope += a.beta * (1 - q);
     }
     return t;
 }
-
-// A thread per column.  The sums of exponentials come from 32 bits; where that does not tell whether a column is clipped, the work-group forms it again
-// in 64 (some 1 column in 10^5 with ratios around 1).
-__global__ __launch_bounds__(kColumns) void policy_columns_kernel(const LossArgs a, const Shape z, const LossSpace w, const Borders b)
+// share k of a column in the loss and its terms
+__device__ __forceinline__ double policy_share(const LossArgs &a, const PolicyTerm &t, int k)
 {
-    __shared__ double lds[kColumns / kWave];
-    __shared__ int close[kColumns];
-    __shared__ float tops[kColumns];
-    const int col = blockIdx.x * kColumns + threadIdx.x;
-    Column c{};
-    double weight = 0;
-    PolicyTerm t{};
-    if (col < a.batch) {
-        c = column_of(a, w.partial, z.chunks, col);
-        weight = a.weights ? static_cast<double>(a.weights[col]) : 1.0 / a.batch;
-        if (!c.counts) weight = 0;
-        if (weight != 0) t = policy_term(a, b, c.logp, col);
-    }
-    close[threadIdx.x] = t.close;
-    tops[threadIdx.x] = c.top;
-    if (__syncthreads_or(t.close)) {
-        for (int k = 0; k < kColumns; ++k) {
-            if (!close[k]) continue;
-            const float *const Z = a.Z + blockIdx.x * kColumns + k;
-            const double top = tops[k];
-            double s = 0;
-            for (int i = threadIdx.x; i < a.classes; i += kColumns) s += exp(Z[i * a.ldz] - top);
-            s = block_sum(s, lds);
-            if (static_cast<int>(threadIdx.x) == k) {
-                c.sum = s;
-                c.logp = static_cast<double>(c.at_label) - top - log(s);
-                t = policy_term(a, b, c.logp, col);
-            }
-        }
-    }
-    if (col < a.batch) {
-        if (a.logp) a.logp[col] = static_cast<float>(c.logp);
-        w.columns[col] = state_of(c, weight != 0 ? static_cast<float>(weight * t.slope) : 0.f);
-    }
-    const bool used = weight != 0;
-    const double share[4] = {used ? weight * (t.surrogate + a.beta * t.kl) : 0, used ? weight * t.surrogate : 0, used ? weight * t.kl : 0,
-                             used && t.clipped ? weight : 0};
-    for (int k = 0; k < 4; ++k) {
-        const double s = block_sum(share[k], lds);
-        if (threadIdx.x == 0) w.shares[4 * blockIdx.x + k] = s;
-    }
+    if (t.weight == 0) return 0;
+    return t.weight * (k == 0 ? t.surrogate + a.beta * t.kl : k == 1 ? t.surrogate : k == 2 ? t.kl : t.clipped ? 1.0 : 0.0);
 }
 
+// The preference loss of a pair from its margin: the loss, and its derivative by the chosen sequence's sum times the number of pairs.
+struct PairTerm {
+    double loss, slope;
+};
+__device__ __forceinline__ PairTerm pair_term(const LossArgs &a, double x)
+{
+    // (the derivative from what is small, so that it does not vanish beside 1)
+    const double e = exp(-fabs(x)), tail = log1p(e), t = a.smoothing;
+    const double above = x > 0 ? 1 / (1 + e) : e / (1 + e), below = x > 0 ? e / (1 + e) : 1 / (1 + e);
+    return {(1 - t) * (tail + fmax(-x, 0.0)) + t * (tail + fmax(x, 0.0)), (t * above - (1 - t) * below) * a.beta};
+}
+__device__ __forceinline__ double margin_of(const LossArgs &a, int pair, double chosen, double rejected)
+{
+    if (a.ref_sums) return a.beta * ((chosen - a.ref_sums[2 * pair]) - (rejected - a.ref_sums[2 * pair + 1]));
+    return a.beta * (chosen - rejected);
+}
 // first column and end of a sequence, whatever `starts` holds
 __device__ __forceinline__ int2 columns_of(const LossArgs &a, int sequence)
 {
     const int from = min(max(a.starts[sequence], 0), a.batch);
     return make_int2(from, min(max(a.starts[sequence + 1], from), a.batch));
 }
+__device__ __forceinline__ bool in_sequences(const LossArgs &a, int col) { return col >= a.starts[0] && col < a.starts[a.sequences]; }
 
-// A thread per column: log-probabilities, and for the gradient of the preference loss what is not the pair's.
-__global__ __launch_bounds__(kColumns) void log_prob_columns_kernel(const LossArgs a, const Shape z, const LossSpace w, const bool gradient)
+__device__ __forceinline__ float gradient_of(float z, const ColumnState &c, int i)
 {
-    const int col = blockIdx.x * kColumns + threadIdx.x;
-    if (col >= a.batch) return;
-    const Column c = column_of(a, w.partial, z.chunks, col);
-    w.logp[col] = c.logp;
-    if (a.logp) a.logp[col] = static_cast<float>(c.logp);
-    if (gradient) {
-        const bool held = col >= a.starts[0] && col < a.starts[a.sequences];
-        w.columns[col] = state_of(c, held && c.counts ? 1.f : 0.f);
+    if (c.c == 0.f) return 0.f;
+    return fmaf(-c.share, exp_of(z - c.top), i == c.label ? c.c : 0.f);
+}
+__device__ __forceinline__ float4 gradient_of4(float4 z, const ColumnState (&c)[4], int i)
+{
+    return make_float4(gradient_of(z.x, c[0], i), gradient_of(z.y, c[1], i), gradient_of(z.z, c[2], i), gradient_of(z.w, c[3], i));
+}
+
+// ---- columns that a work-group holds ----
+enum What { kLogProbs, kPolicy, kPreference };
+
+// One work-group: all classes of a tile of columns, K rows a thread; at least as many threads as columns, of which each does what a column needs.
+// kLogProbs: log-probabilities, and the sums of sequences where there is one tile.  kPolicy: all of it (the loss's shares are left for another launch
+// where there are more tiles).  kPreference: all of it in one tile; in more, what the launches for pairs and for the gradient take.
+template <int K, What W>
+__global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, const Shape z, const LossSpace w, const Borders b)
+{
+    extern __shared__ float4 lds[];   // two per wave and quad
+    __shared__ double sums[kHeldThreads / kWave];
+    __shared__ float tops[4 << kLanes];
+    __shared__ float of_tile[4 << kLanes];
+    __shared__ int close[4 << kLanes];
+    __shared__ double logp[4 << kLanes];
+    __shared__ ColumnState states[4 << kLanes];
+    const Spot p = spot_in(near_tile(blockIdx.x, z.tiles, z.lg), z.lg, a.batch, z.past);
+    const int width = 4 << z.lg, first = p.col - 4 * p.q, j = threadIdx.x, col = first + j;
+    const bool mine = j < width && col < a.batch;
+    Column c{};
+    if (mine) read_label(a, col, c);
+    float4 x[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = load_quad(a.Z + min(p.slot + k * p.slots, a.classes - 1) * a.ldz, p);
+    Running r{splat(-FLT_MAX), splat(0.f)};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (p.slot + k * p.slots >= a.classes) x[k] = splat(-INFINITY);
+        r.top = max4(r.top, x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) r.sum = r.sum + exp_of4(x[k] - r.top);
+    r = join(r, z.lg, lds);
+    if (p.slot == 0) {
+        *reinterpret_cast<float4 *>(tops + 4 * p.q) = r.top;
+        *reinterpret_cast<float4 *>(of_tile + 4 * p.q) = r.sum;
+    }
+    __syncthreads();
+    if (mine) {
+        c.top = tops[j];
+        set_sum(c, of_tile[j]);
+        if (a.logp && W != kPolicy) a.logp[col] = static_cast<float>(c.logp);
+    }
+    if constexpr (W == kPolicy) {
+        PolicyTerm t{};
+        if (mine) t = policy_term(a, b, c, col);
+        if (j < width) close[j] = t.close;
+        if (__syncthreads_or(t.close)) {
+            // the sums of exponentials come from 32 bits; where that does not tell whether a column is clipped, it is formed again in 64
+            for (int k = 0; k < width; ++k) {
+                if (!close[k]) continue;
+                const double again = exact_sum(a, first + k, tops[k], sums);
+                if (j == k) {
+                    set_sum(c, again);
+                    t = policy_term(a, b, c, col);
+                }
+            }
+        }
+        if (mine && a.logp) a.logp[col] = static_cast<float>(c.logp);
+        if (j < width) states[j] = state_of(c, t.weight != 0 ? static_cast<float>(t.weight * t.slope) : 0.f);
+        for (int k = 0; k < 4; ++k) {
+            const double s = block_sum(policy_share(a, t, k), sums);
+            if (j == 0 && z.tiles == 1) a.stats[k] = static_cast<float>(s);
+            else if (j == 0) w.shares[4 * static_cast<int64_t>(blockIdx.x) + k] = s;
+        }
+    } else {
+        if (z.tiles > 1) {
+            if (mine) {
+                w.logp[col] = c.logp;
+                if (W == kPreference) w.columns[col] = state_of(c, in_sequences(a, col) && c.counts ? 1.f : 0.f);
+            }
+            return;
+        }
+        if (j < width) logp[j] = c.logp;
+        if constexpr (W == kPreference)
+            if (j < width) states[j] = state_of(c, 0.f);
+        __syncthreads();
+        const auto sum_of = [&](int sequence) {
+            const int2 at = columns_of(a, sequence);
+            double s = 0;
+            for (int k = at.x; k < at.y; ++k) s += logp[k];
+            if (a.sums) a.sums[sequence] = static_cast<float>(s);
+            return s;
+        };
+        if constexpr (W == kLogProbs) {
+            if (a.sums)
+                for (int k = j; k < a.sequences; k += blockDim.x) (void)sum_of(k);
+            return;
+        } else {
+            const int pairs = a.sequences / 2;
+            double loss = 0;
+            for (int k = j; k < pairs; k += blockDim.x) {
+                const double chosen = sum_of(2 * k), x = margin_of(a, k, chosen, sum_of(2 * k + 1));
+                const PairTerm t = pair_term(a, x);
+                loss += t.loss;
+                if (a.margins) a.margins[k] = static_cast<float>(x);
+                for (int side = 0; side < 2; ++side) {
+                    const int2 at = columns_of(a, 2 * k + side);
+                    for (int i = at.x; i < at.y; ++i) states[i].c = static_cast<float>((side ? -t.slope : t.slope) / pairs);
+                }
+            }
+            loss = block_sum(loss, sums);   // (and a barrier)
+            if (j == 0 && a.loss) *a.loss = static_cast<float>(loss / pairs);
+            if (j < width) states[j] = state_of(c, c.counts ? states[j].c : 0.f);
+        }
+    }
+    __syncthreads();
+    ColumnState q[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = states[4 * p.q + k];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int row = p.slot + k * p.slots;
+        if (row < a.classes) store_quad(a.dZ + row * a.lddz, p, gradient_of4(x[k], q, row));
     }
 }
 
+// ---- columns in chunks ----
+// The chunks of 16 columns added up; the columns' first threads get the result (col < batch), and all threads the largest logits in `tops`.
+__device__ __forceinline__ Column column_of(const LossArgs &a, const float *partial, int chunks, int col, int part, float *tops, double (*lds)[kColumns])
+{
+    const int at_col = min(col, a.batch - 1), lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, j = threadIdx.x & (kColumns - 1);
+    __shared__ float of_wave[kColumns * kParts / kWave][kColumns];
+    Column c{};
+    if (part == 0) read_label(a, at_col, c);
+    float top = -FLT_MAX;
+#pragma unroll 8
+    for (int k = part; k < chunks; k += kParts) top = fmaxf(top, partial[2 * static_cast<int64_t>(k) * a.batch + at_col]);
+    for (int d = kColumns; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    if (lane < kColumns) of_wave[wave][j] = top;
+    __syncthreads();
+    for (int w = 0; w < kColumns * kParts / kWave; ++w) top = fmaxf(top, of_wave[w][j]);
+    double sum = 0;
+#pragma unroll 8
+    for (int k = part; k < chunks; k += kParts) {
+        const float *const at = partial + 2 * static_cast<int64_t>(k) * a.batch + at_col;
+        sum += at[a.batch] * exp(static_cast<double>(at[0]) - top);
+    }
+    for (int d = kColumns; d < kWave; d <<= 1) sum += __shfl_xor(sum, d, kWave);
+    if (lane < kColumns) lds[wave][j] = sum;
+    if (part == 0) tops[j] = top;
+    __syncthreads();
+    sum = 0;
+    for (int w = 0; w < kColumns * kParts / kWave; ++w) sum += lds[w][j];
+    c.top = top;
+    if (part == 0) set_sum(c, sum);
+    return c;
+}
+
+__global__ __launch_bounds__(kColumns *kParts) void policy_columns_kernel(const LossArgs a, const Shape z, const LossSpace w, const Borders b)
+{
+    __shared__ double lds[kColumns * kParts / kWave][kColumns], sums[kColumns * kParts / kWave];
+    __shared__ float tops[kColumns];
+    __shared__ int close[kColumns];
+    const int j = threadIdx.x & (kColumns - 1), part = threadIdx.x / kColumns, col = blockIdx.x * kColumns + j;
+    const bool mine = part == 0 && col < a.batch;
+    Column c = column_of(a, w.partial, z.chunks, col, part, tops, lds);
+    PolicyTerm t{};
+    if (mine) t = policy_term(a, b, c, col);
+    if (part == 0) close[j] = t.close;
+    if (__syncthreads_or(t.close)) {
+        // as above, in 64 bits (some 4 columns in 10^5 with ratios around 1)
+        for (int k = 0; k < kColumns; ++k) {
+            if (!close[k]) continue;
+            const double again = exact_sum(a, blockIdx.x * kColumns + k, tops[k], sums);
+            if (part == 0 && j == k) {
+                set_sum(c, again);
+                t = policy_term(a, b, c, col);
+            }
+        }
+    }
+    if (mine) {
+        if (a.logp) a.logp[col] = static_cast<float>(c.logp);
+        w.columns[col] = state_of(c, t.weight != 0 ? static_cast<float>(t.weight * t.slope) : 0.f);
+    }
+    if (threadIdx.x >= kWave) return;
+    for (int k = 0; k < 4; ++k) {
+        double s = policy_share(a, t, k);
+        for (int d = 1; d < kColumns; d <<= 1) s += __shfl_xor(s, d, kWave);
+        if (threadIdx.x == 0) w.shares[4 * static_cast<int64_t>(blockIdx.x) + k] = s;
+    }
+}
+
+// log-probabilities, and for the gradient of the preference loss what is not the pair's
+__global__ __launch_bounds__(kColumns *kParts) void log_prob_columns_kernel(const LossArgs a, const Shape z, const LossSpace w, const bool gradient)
+{
+    __shared__ double lds[kColumns * kParts / kWave][kColumns], logp[kColumns];
+    __shared__ float tops[kColumns];
+    const int j = threadIdx.x & (kColumns - 1), part = threadIdx.x / kColumns, col = blockIdx.x * kColumns + j;
+    const Column c = column_of(a, w.partial, z.chunks, col, part, tops, lds);
+    if (part == 0) {
+        logp[j] = c.logp;
+        if (col < a.batch) {
+            w.logp[col] = c.logp;
+            if (a.logp) a.logp[col] = static_cast<float>(c.logp);
+            if (gradient) w.columns[col] = state_of(c, in_sequences(a, col) && c.counts ? 1.f : 0.f);
+        }
+    }
+    if (gradient || gridDim.x > 1 || !a.sums) return;
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.sequences; k += blockDim.x) {
+        const int2 at = columns_of(a, k);
+        double s = 0;
+        for (int i = at.x; i < at.y; ++i) s += logp[i];
+        a.sums[k] = static_cast<float>(s);
+    }
+}
+
+// ---- sequences ----
 constexpr int kSequenceThreads = 1024;
 __device__ __forceinline__ double sequence_sum(const LossArgs &a, const double *logp, int2 at, double *lds)
 {
@@ -262,19 +449,15 @@ __global__ __launch_bounds__(kSequenceThreads) void pairs_kernel(const LossArgs 
         at[k] = columns_of(a, 2 * pair + k);
         s[k] = sequence_sum(a, w.logp, at[k], lds);
     }
-    double beyond = s[0] - s[1];
-    if (a.ref_sums) beyond = (s[0] - a.ref_sums[2 * pair]) - (s[1] - a.ref_sums[2 * pair + 1]);
-    const double x = a.beta * beyond, tail = log1p(exp(-fabs(x))), t = a.smoothing;
-    // (the derivative from what is small, so that it does not vanish beside 1)
-    const double e = exp(-fabs(x)), above = x > 0 ? 1 / (1 + e) : e / (1 + e), below = x > 0 ? e / (1 + e) : 1 / (1 + e);
-    const double slope = (t * above - (1 - t) * below) * a.beta / gridDim.x;
+    const double x = margin_of(a, pair, s[0], s[1]);
+    const PairTerm t = pair_term(a, x);
     if (threadIdx.x == 0) {
         if (a.sums) a.sums[2 * pair] = static_cast<float>(s[0]), a.sums[2 * pair + 1] = static_cast<float>(s[1]);
         if (a.margins) a.margins[pair] = static_cast<float>(x);
-        w.shares[pair] = (1 - t) * (tail + fmax(-x, 0.0)) + t * (tail + fmax(x, 0.0));
+        w.shares[pair] = t.loss;
     }
     for (int k = 0; k < 2; ++k) {
-        const float c = static_cast<float>(k ? -slope : slope);
+        const float c = static_cast<float>((k ? -t.slope : t.slope) / gridDim.x);
         for (int col = at[k].x + threadIdx.x; col < at[k].y; col += blockDim.x) {
             ColumnState q = w.columns[col];
             if (q.c == 0.f) continue;
@@ -286,38 +469,37 @@ __global__ __launch_bounds__(kSequenceThreads) void pairs_kernel(const LossArgs 
 }
 
 // the shares of the loss, added up by one wave in one fixed order
-__device__ void write_policy_stats(const LossArgs &a, const double *shares, int blocks)
+__device__ __forceinline__ double wave_sum(const double *v, int n, int step)
+{
+    double s = 0;
+#pragma unroll 4
+    for (int b = threadIdx.x; b < n; b += kWave) s += v[static_cast<int64_t>(step) * b];
+    for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
+    return s;
+}
+__device__ __forceinline__ void write_stats(const LossArgs &a, const double *shares, int n)
 {
     for (int k = 0; k < 4; ++k) {
-        double s = 0;
-        for (int b = threadIdx.x; b < blocks; b += kWave) s += shares[4 * static_cast<int64_t>(b) + k];
-        for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
+        const double s = wave_sum(shares + k, n, 4);
         if (threadIdx.x == 0) a.stats[k] = static_cast<float>(s);
     }
 }
-__device__ void write_preference_loss(const LossArgs &a, const double *shares, int pairs)
-{
-    double s = 0;
-    for (int b = threadIdx.x; b < pairs; b += kWave) s += shares[b];
-    for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
-    if (threadIdx.x == 0 && a.loss) *a.loss = static_cast<float>(s / pairs);
-}
+__global__ __launch_bounds__(kWave) void stats_kernel(const LossArgs a, const double *shares, const int n) { write_stats(a, shares, n); }
 
-__device__ __forceinline__ float gradient_of(float z, const ColumnState &c, int i)
-{
-    if (c.c == 0.f) return 0.f;
-    return fmaf(-c.share, exp_of(z - c.top), i == c.label ? c.c : 0.f);
-}
-
-// One work-group: a chunk of the classes in a tile of columns.  `shares`: how many shares of the loss there are (policy: of four terms each).
+// One work-group: a chunk of the classes in a tile of columns, from the last one read to the first.  `shares`: how many shares of the loss there are
+// (policy: of four terms each).
 __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArgs a, const Shape z, const LossSpace w, const int shares)
 {
     if (blockIdx.x == 0 && threadIdx.x < kWave) {
-        if (a.stats) write_policy_stats(a, w.shares, shares);
-        else write_preference_loss(a, w.shares, shares);
+        if (a.stats) {
+            write_stats(a, w.shares, shares);
+        } else if (a.loss) {
+            const double s = wave_sum(w.shares, shares, 1);
+            if (threadIdx.x == 0) *a.loss = static_cast<float>(s / shares);
+        }
     }
-    const int chunk = blockIdx.x % z.chunks;
-    const Spot p = spot_in(blockIdx.x / z.chunks, z.lg, a.batch);
+    const int unit = gridDim.x - 1 - blockIdx.x, chunk = unit % z.chunks;
+    const Spot p = spot_in(unit / z.chunks, z.lg, a.batch, z.past);
     if (p.n == 0) return;
     const int first = chunk * z.rows, end = min(a.classes, first + z.rows);
     ColumnState c[4];
@@ -330,16 +512,18 @@ __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArg
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int row = i + u * p.slots;
-            if (row < end)
-                store_quad(a.dZ + row * a.lddz, p, make_float4(gradient_of(x[u].x, c[0], row), gradient_of(x[u].y, c[1], row), gradient_of(x[u].z, c[2], row),
-                                                               gradient_of(x[u].w, c[3], row)));
+            if (row < end) store_quad(a.dZ + row * a.lddz, p, gradient_of4(x[u], c, row));
         }
     }
 }
 
-Shape shape_of(int32_t classes, int32_t batch)
+// ---- launches ----
+constexpr int64_t kFewTiles = 256;       // one per compute unit
+
+// Of columns that are cut into chunks.
+Shape chunks_of(int32_t classes, int32_t batch)
 {
-    Shape z;
+    Shape z{};
     z.lg = lanes_for(batch, kLanes);
     z.tiles = static_cast<int32_t>((batch + (INT64_C(4) << z.lg) - 1) >> (z.lg + 2));
     const int step = kLoads * (kThreads >> z.lg);
@@ -347,9 +531,49 @@ Shape shape_of(int32_t classes, int32_t batch)
     const int64_t steps = (most + std::min(most, want) - 1) / std::min(most, want);      // of kLoads rows a thread
     z.rows = static_cast<int>(std::min<int64_t>(steps * step, classes));
     z.chunks = static_cast<int>((static_cast<int64_t>(classes) + z.rows - 1) / z.rows);
+    z.past = 8 * static_cast<int64_t>(classes) * batch > kCacheBytes;
     return z;
 }
+
+// Of columns that a work-group holds.
+struct Held {
+    Shape z;
+    int rows, threads;       // rows: of a thread; 0 where the columns are cut into chunks
+};
+Held held_of(int32_t classes, int32_t batch)
+{
+    Held h{};
+    const auto tiles = [&](int lg) { return (batch + (INT64_C(4) << lg) - 1) >> (lg + 2); };
+    const auto held = [&](int lg) { return static_cast<int64_t>(classes) << lg; };
+    int lg = lanes_for(batch, kLanes);
+    // one tile for all, with no launch for the sums behind it; or tiles of 32 columns, wider ones where they leave lanes idle, narrower ones where there
+    // would be few
+    if (tiles(lg) > 1 || held(lg) > 4 * kHeldThreads) {
+        const int widest = lg;
+        lg = lanes_for(batch, 3);
+        while (lg < widest && held(lg) < kWave) ++lg;
+        while (lg > 0 && tiles(lg) < kFewTiles && held(lg) > kWave) --lg;
+    }
+    h.z.lg = lg;
+    h.z.tiles = static_cast<int32_t>(tiles(lg));
+    h.z.past = 8 * static_cast<int64_t>(classes) * batch > kCacheBytes;
+    if (held(lg) > kHeldRows * kHeldThreads || (h.z.tiles < kFewTiles && held(lg) > 4 * kHeldThreads)) return h;
+    h.rows = 1;
+    while (h.rows < kHeldRows && held(lg) > (h.rows < 4 ? 256 : kHeldThreads) * h.rows) h.rows *= 2;
+    const int64_t threads = std::max<int64_t>((held(lg) + h.rows - 1) / h.rows, 4 << lg);
+    h.threads = static_cast<int>((threads + kWave - 1) / kWave * kWave);
+    return h;
+}
 int column_blocks(int32_t batch) { return static_cast<int>((static_cast<int64_t>(batch) + kColumns - 1) / kColumns); }
+
+template <What W, int Most = kHeldRows>
+void launch_held(const LossArgs &a, const Held &h, const LossSpace &w, const Borders &b, hipStream_t s)
+{
+    if constexpr (Most > 1)
+        if (h.rows < Most) return launch_held<W, Most / 2>(a, h, w, b, s);
+    const int lds = 2 * static_cast<int>(sizeof(float4)) * (h.threads / kWave << h.z.lg);
+    held_kernel<Most, W><<<static_cast<uint32_t>(h.z.tiles), h.threads, lds, s>>>(a, h.z, w, b);
+}
 void launch_log_sums(const LossArgs &a, const Shape &z, const LossSpace &w, hipStream_t s)
 {
     log_sum_kernel<<<static_cast<uint32_t>(z.tiles) * z.chunks, kThreads, 0, s>>>(a, z, w.partial);
@@ -358,55 +582,81 @@ void launch_gradient(const LossArgs &a, const Shape &z, const LossSpace &w, int 
 {
     logits_gradient_kernel<<<static_cast<uint32_t>(z.tiles) * z.chunks, kThreads, 0, s>>>(a, z, w, shares);
 }
+bool too_large(const Held &h, const Shape &z, int32_t batch, int32_t sequences)
+{
+    return (h.rows && !fits_launch(h.z.tiles, h.threads)) || !fits_launch(static_cast<int64_t>(z.tiles) * z.chunks, kThreads) || (!h.rows && !fits_launch(column_blocks(batch), kColumns * kParts)) ||
+           !fits_launch(sequences, kSequenceThreads);
+}
 
 }  // namespace
 
 LossSpace loss_space(void *memory, int32_t classes, int32_t batch, int32_t sequences)
 {
-    const Shape z = shape_of(classes, batch);
+    const Held h = held_of(classes, batch);
+    const int64_t chunks = h.rows ? 0 : chunks_of(classes, batch).chunks;
     LossSpace w;
-    w.logp = static_cast<double *>(memory);
+    w.columns = static_cast<ColumnState *>(memory);
+    w.logp = reinterpret_cast<double *>(w.columns + batch);
     w.shares = w.logp + batch;
-    w.columns = reinterpret_cast<ColumnState *>(w.shares + std::max(4 * column_blocks(batch), sequences));
-    w.partial = reinterpret_cast<float *>(w.columns + batch);
-    w.bytes = reinterpret_cast<char *>(w.partial + 2 * static_cast<int64_t>(z.chunks) * batch) - static_cast<char *>(memory);
+    w.partial = reinterpret_cast<float *>(w.shares + std::max<int64_t>(4 * static_cast<int64_t>(h.rows ? h.z.tiles : column_blocks(batch)), sequences));
+    w.bytes = reinterpret_cast<char *>(w.partial + 2 * chunks * batch) - static_cast<char *>(memory);
     return w;
 }
 
 hipError_t launch_log_probs(const LossArgs &a, hipStream_t s)
 {
-    const Shape z = shape_of(a.classes, a.batch);
+    const Held h = held_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, a.sequences);
-    if (!fits_launch(static_cast<int64_t>(z.tiles) * z.chunks, kThreads) || !fits_launch(a.sequences, kSequenceThreads)) return hipErrorInvalidConfiguration;
-    launch_log_sums(a, z, w, s);
-    log_prob_columns_kernel<<<column_blocks(a.batch), kColumns, 0, s>>>(a, z, w, false);
-    if (a.sums) sequence_sums_kernel<<<a.sequences, kSequenceThreads, 0, s>>>(a, w);
+    if (too_large(h, z, a.batch, a.sequences)) return hipErrorInvalidConfiguration;
+    bool summed;
+    if (h.rows) {
+        launch_held<kLogProbs>(a, h, w, Borders{}, s);
+        summed = h.z.tiles == 1;
+    } else {
+        launch_log_sums(a, z, w, s);
+        log_prob_columns_kernel<<<column_blocks(a.batch), kColumns * kParts, 0, s>>>(a, z, w, false);
+        summed = column_blocks(a.batch) == 1;
+    }
+    if (a.sums && !summed) sequence_sums_kernel<<<a.sequences, kSequenceThreads, 0, s>>>(a, w);
     return hipGetLastError();
 }
 
 hipError_t launch_policy(const LossArgs &a, hipStream_t s)
 {
-    const Shape z = shape_of(a.classes, a.batch);
+    const Held h = held_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, 0);
-    if (!fits_launch(static_cast<int64_t>(z.tiles) * z.chunks, kThreads)) return hipErrorInvalidConfiguration;
-    // An exponential is off by 2^-24 (2 |z - top| + 2), and the mean of |z - top| over p is at most log(classes) < 22; a thread adds up eight
-    // rows, then their sum to the others'.
-    const double adds = 2.0 * (z.rows / ((kThreads >> z.lg) * kLoads) + 1) + kLoads;
+    if (too_large(h, z, a.batch, 0)) return hipErrorInvalidConfiguration;
+    // An exponential is off by 2^-24 (2 |z - top| + 2), and the mean of |z - top| over p is at most log(classes) < 21; a thread adds up eight rows, then
+    // their sum to the others' (or its 16 rows), and 10 levels and up to 16 waves follow.
+    const double adds = h.rows ? h.rows : 3.0 * (z.rows / ((kThreads >> z.lg) * kLoads) + 1) + kLoads;
     const Borders b{a.clip_low < 1.f ? log1p(-static_cast<double>(a.clip_low)) : -INFINITY, log1p(static_cast<double>(a.clip_high)),
-                    static_cast<float>((64 + adds) / (1 << 24))};
+                    static_cast<float>((2 * 21 + 2 + 10 * 4 + 16 * 4 + adds) / (1 << 24))};
+    if (h.rows) {
+        launch_held<kPolicy>(a, h, w, b, s);
+        if (h.z.tiles > 1) stats_kernel<<<1, kWave, 0, s>>>(a, w.shares, h.z.tiles);
+        return hipGetLastError();
+    }
     launch_log_sums(a, z, w, s);
-    policy_columns_kernel<<<column_blocks(a.batch), kColumns, 0, s>>>(a, z, w, b);
+    policy_columns_kernel<<<column_blocks(a.batch), kColumns * kParts, 0, s>>>(a, z, w, b);
     launch_gradient(a, z, w, column_blocks(a.batch), s);
     return hipGetLastError();
 }
 
 hipError_t launch_preference(const LossArgs &a, hipStream_t s)
 {
-    const Shape z = shape_of(a.classes, a.batch);
+    const Held h = held_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, a.sequences);
-    if (!fits_launch(static_cast<int64_t>(z.tiles) * z.chunks, kThreads) || !fits_launch(a.sequences / 2, kSequenceThreads)) return hipErrorInvalidConfiguration;
-    launch_log_sums(a, z, w, s);
-    log_prob_columns_kernel<<<column_blocks(a.batch), kColumns, 0, s>>>(a, z, w, true);
+    if (too_large(h, z, a.batch, a.sequences / 2)) return hipErrorInvalidConfiguration;
+    if (h.rows) {
+        launch_held<kPreference>(a, h, w, Borders{}, s);
+        if (h.z.tiles == 1) return hipGetLastError();
+    } else {
+        launch_log_sums(a, z, w, s);
+        log_prob_columns_kernel<<<column_blocks(a.batch), kColumns * kParts, 0, s>>>(a, z, w, true);
+    }
     pairs_kernel<<<a.sequences / 2, kSequenceThreads, 0, s>>>(a, w);
     launch_gradient(a, z, w, a.sequences / 2, s);
     return hipGetLastError();

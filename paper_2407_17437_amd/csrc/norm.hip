@@ -145,18 +145,6 @@ struct Shape {
     bool past;
     int64_t tiles;
 };
-// Tile of work-group b of n: those that share 128-byte lines (tiles of less than 32 columns) come to the same XCD, to which ids go in turn, so that its L2
-// serves a line to all of them.
-__device__ __forceinline__ int64_t near_tile(int64_t b, int64_t n, int lg)
-{
-    const int shift = kLanes - lg;
-    if (shift <= 0) return b;
-    const int64_t set = b >> (3 + shift);
-    if ((set + 1) << (3 + shift) > n) return b;
-    const int in_set = static_cast<int>(b) & ((8 << shift) - 1);
-    return (set << (3 + shift)) + ((in_set & 7) << shift) + (in_set >> 3);
-}
-
 // statistics of the entries that the work-group holds: mean and sum of squares about it; x becomes its difference from the mean
 template <int K>
 __device__ __forceinline__ void statistics(float4 (&x)[2 * K], const Rows<K> &r, int lg, float4 (*lds)[kThreadsMost / kWave << kLanes], float4 &mean, float4 &squares)
