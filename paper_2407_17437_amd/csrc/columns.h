@@ -59,6 +59,17 @@ __device__ __forceinline__ float4 load_quad(const float *row, const Spot &p)
     const int last = p.batch - 1;
     return make_float4(row[min(p.col, last)], row[min(p.col + 1, last)], row[min(p.col + 2, last)], row[min(p.col + 3, last)]);
 }
+// The same, with no more reads than columns where the batch has one to three (0 in the others).
+__device__ __forceinline__ float4 load_few(const float *row, const Spot &p)
+{
+    if (p.whole) return ld4(row + p.col);
+    const int last = p.batch - 1;
+    float4 x = make_float4(row[min(p.col, last)], 0.f, 0.f, 0.f);
+    if (p.batch > 1) x.y = row[min(p.col + 1, last)];
+    if (p.batch > 2) x.z = row[min(p.col + 2, last)];
+    if (p.batch > 3) x.w = row[min(p.col + 3, last)];
+    return x;
+}
 __device__ __forceinline__ void store_quad(float *row, const Spot &p, float4 x)
 {
     if (p.whole) {

@@ -106,6 +106,9 @@ __device__ __forceinline__ float4 column_sum(float4 v, int lg, float4 *lds)
     return s;
 }
 
+// the memory of a second sum
+__device__ __forceinline__ float4 *second(float4 *lds, int lg) { return lds + (blockDim.x >> 6 << lg); }
+
 // A thread's rows: K pairs, `slots` pairs apart, of which those in [first, end) belong to its work-group's rows.  Pairs go by the rows' numbers in
 // the whole operand, as the generator's do.
 template <int K>
@@ -147,21 +150,21 @@ struct Shape {
 };
 // statistics of the entries that the work-group holds: mean and sum of squares about it; x becomes its difference from the mean
 template <int K>
-__device__ __forceinline__ void statistics(float4 (&x)[2 * K], const Rows<K> &r, int lg, float4 (*lds)[kThreadsMost / kWave << kLanes], float4 &mean, float4 &squares)
+__device__ __forceinline__ void statistics(float4 (&x)[2 * K], const Rows<K> &r, int lg, float4 *lds, float4 &mean, float4 &squares)
 {
     const int n = r.end - r.first;
     float4 s = splat(0.f);
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i)
         if (r.in(i)) s = s + x[i];
-    mean = 1.f / static_cast<float>(n) * column_sum(s, lg, lds[0]);
+    mean = 1.f / static_cast<float>(n) * column_sum(s, lg, lds);
     float4 s2 = splat(0.f);
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
         x[i] = x[i] - mean;
         if (r.in(i)) s2 = fma4(x[i], x[i], s2);
     }
-    squares = column_sum(s2, lg, lds[1]);
+    squares = column_sum(s2, lg, second(lds, lg));
 }
 __device__ __forceinline__ float4 rstd_of(float4 squares, int m, float eps)
 {
@@ -169,8 +172,22 @@ __device__ __forceinline__ float4 rstd_of(float4 squares, int m, float eps)
     return make_float4(1.f / sqrtf(v.x), 1.f / sqrtf(v.y), 1.f / sqrtf(v.z), 1.f / sqrtf(v.w));
 }
 
+// the rows' gamma and beta
 template <int K>
-__device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&x)[2 * K], const Rows<K> &r, const Spot &p, float4 rstd)
+struct Affine {
+    float gamma[2 * K], beta[2 * K];
+    __device__ __forceinline__ void load(const NormArgs &a, const Rows<K> &r)
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) {
+            gamma[i] = a.gamma ? a.gamma[r.readable(i)] : 1.f;
+            beta[i] = a.beta ? a.beta[r.readable(i)] : 0.f;
+        }
+    }
+};
+// HELD: the rows' gamma and beta are in w
+template <int K, bool HELD>
+__device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&x)[2 * K], const Rows<K> &r, const Affine<K> &w, const Spot &p, float4 rstd)
 {
     Drawn d{};
     if (a.drop.cut) d = drawn_from(a.drop);
@@ -184,7 +201,8 @@ __device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&
         }
         if (!r.in(i)) continue;
         const float4 xh = x[i] * rstd;   // (x: less the mean)
-        float4 y = activate4(fma4(splat(a.gamma ? a.gamma[f] : 1.f), xh, splat(a.beta ? a.beta[f] : 0.f)), a.act);
+        const float gamma = HELD ? w.gamma[i] : a.gamma ? a.gamma[f] : 1.f, beta = HELD ? w.beta[i] : a.beta ? a.beta[f] : 0.f;
+        float4 y = activate4(fma4(splat(gamma), xh, splat(beta)), a.act);
         if (a.drop.cut) y = drop(y, bits, i & 1, a.drop);
         store_quad(a.Y + f * a.ldy, p, y);
     }
@@ -195,13 +213,16 @@ __device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&
 template <int K, int T, bool WHOLE>
 __global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const Shape z)
 {
-    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K], mean, squares;
     r.load(a.X, a.ldx, p, x);
+    constexpr bool kHeld = K <= 2;   // (asked for before the sums where there are registers for them)
+    Affine<K> w;
+    if constexpr (WHOLE && kHeld) w.load(a, r);
     statistics<K>(x, r, z.lg, lds, mean, squares);
     if constexpr (WHOLE) {
         const float4 rstd = rstd_of(squares, r.end - r.first, a.eps);
@@ -209,7 +230,7 @@ __global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const
             if (a.mean) store_quad(a.mean + group * a.lds, p, mean);
             if (a.rstd) store_quad(a.rstd + group * a.lds, p, rstd);
         }
-        write_forward<K>(a, x, r, p, rstd);
+        write_forward<K, kHeld>(a, x, r, w, p, rstd);
     } else if (p.slot == 0) {
         float *const at = a.workspace + 2 * (static_cast<int64_t>(group) * z.chunks + chunk) * a.batch;
         store_quad(at, p, mean);
@@ -221,13 +242,15 @@ __global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const
 template <int K>
 __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArgs a, const Shape z)
 {
-    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K];
     r.load(a.X, a.ldx, p, x);
+    Affine<K> w;
+    w.load(a, r);
     // the chunks' means weighed by their rows, then all squares about the mean of the group (Chan, Golub, LeVeque 1979); a thread adds up every
     // slots-th chunk
     const int m = a.features / a.groups;
@@ -237,14 +260,14 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArg
         const Rows<K> of = rows_of<K>(a, group, c, p);
         mean = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p), mean);
     }
-    mean = 1.f / static_cast<float>(m) * column_sum(mean, z.lg, lds[0]);
+    mean = 1.f / static_cast<float>(m) * column_sum(mean, z.lg, lds);
     for (int c = p.slot; c < z.chunks; c += p.slots) {
         const Rows<K> of = rows_of<K>(a, group, c, p);
         const float *const at = stats + 2 * static_cast<int64_t>(c) * a.batch;
         const float4 d = load_quad(at, p) - mean;
         squares = squares + fma4(static_cast<float>(of.end - of.first) * d, d, load_quad(at + a.batch, p));
     }
-    squares = column_sum(squares, z.lg, lds[1]);
+    squares = column_sum(squares, z.lg, second(lds, z.lg));
     const float4 rstd = rstd_of(squares, m, a.eps);
     if (p.slot == 0 && chunk == 0) {
         if (a.mean) store_quad(a.mean + group * a.lds, p, mean);
@@ -252,23 +275,10 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArg
     }
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) x[i] = x[i] - mean;
-    write_forward<K>(a, x, r, p, rstd);
+    write_forward<K, true>(a, x, r, w, p, rstd);
 }
 
 // ---- backward ----
-// the rows' gamma and beta
-template <int K>
-struct Affine {
-    float gamma[2 * K], beta[2 * K];
-    __device__ __forceinline__ void load(const NormArgs &a, const Rows<K> &r)
-    {
-#pragma unroll
-        for (int i = 0; i < 2 * K; ++i) {
-            gamma[i] = a.gamma ? a.gamma[r.readable(i)] : 1.f;
-            beta[i] = a.beta && a.act ? a.beta[r.readable(i)] : 0.f;
-        }
-    }
-};
 // x becomes xh, g becomes h; what the rows add to the gradients of gamma and beta from this thread's columns is added to `dg` and `db`
 template <int K>
 __device__ __forceinline__ void form_h(const NormArgs &a, float4 (&x)[2 * K], float4 (&g)[2 * K], const Rows<K> &r, const Affine<K> &w, const Spot &p, float4 mean, float4 rstd,
@@ -296,7 +306,7 @@ __device__ __forceinline__ void form_h(const NormArgs &a, float4 (&x)[2 * K], fl
     }
 }
 template <int K>
-__device__ __forceinline__ void column_sums_of_h(const float4 (&x)[2 * K], const float4 (&g)[2 * K], const Rows<K> &r, int lg, float4 (*lds)[kThreadsMost / kWave << kLanes],
+__device__ __forceinline__ void column_sums_of_h(const float4 (&x)[2 * K], const float4 (&g)[2 * K], const Rows<K> &r, int lg, float4 *lds,
                                                  float4 &s, float4 &sx)
 {
     float4 t = splat(0.f), tx = splat(0.f);
@@ -306,8 +316,8 @@ __device__ __forceinline__ void column_sums_of_h(const float4 (&x)[2 * K], const
             t = t + g[i];
             tx = fma4(g[i], x[i], tx);
         }
-    s = column_sum(t, lg, lds[0]);
-    sx = column_sum(tx, lg, lds[1]);
+    s = column_sum(t, lg, lds);
+    sx = column_sum(tx, lg, second(lds, lg));
 }
 template <int K>
 __device__ __forceinline__ void write_backward(const NormArgs &a, const float4 (&x)[2 * K], const float4 (&g)[2 * K], const Rows<K> &r, const Spot &p, float4 rstd, float4 s,
@@ -346,7 +356,7 @@ __device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int 
 template <int K, int T, bool WHOLE>
 __global__ __launch_bounds__(T) void norm_backward_kernel(const NormArgs a, const Shape z, float *slabs)
 {
-    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.slabs;
     const int slab = static_cast<int>(near_tile(blockIdx.x % z.slabs, z.slabs, z.lg)), chunk = static_cast<int>(unit % z.chunks), group = static_cast<int>(unit / z.chunks);
     float dg[2 * K], db[2 * K];
@@ -380,7 +390,7 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(const NormArgs a, cons
 template <int K>
 __global__ __launch_bounds__(kChunkThreads) void norm_apply_backward_kernel(const NormArgs a, const Shape z)
 {
-    __shared__ float4 lds[2][kThreadsMost / kWave << kLanes];
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
@@ -399,8 +409,8 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_backward_kernel(cons
         s = s + load_quad(at, p);
         sx = sx + load_quad(at + a.batch, p);
     }
-    s = column_sum(s, z.lg, lds[0]);
-    sx = column_sum(sx, z.lg, lds[1]);
+    s = column_sum(s, z.lg, lds);
+    sx = column_sum(sx, z.lg, second(lds, z.lg));
     write_backward<K>(a, x, g, r, p, rstd, s, sx);
 }
 
@@ -472,6 +482,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
 struct Plan {
     Shape z;
     int threads, pairs;      // pairs: K
+    int lds;                 // bytes
 };
 constexpr int64_t kFewGroups = 256;      // work-groups: one per compute unit
 struct Limits {
@@ -516,6 +527,7 @@ Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
         }
     }
     p.threads = static_cast<int>(threads);
+    p.lds = 2 * static_cast<int>(sizeof(float4)) * (p.threads / kWave << p.z.lg);
     p.z.slabs = 1;
     return p;
 }
@@ -561,11 +573,11 @@ hipError_t launch_norm_forward(const NormArgs &a, hipStream_t s)
     if (!fits_launch(blocks, p.threads)) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
     if (p.z.chunks == 1) {
-        with_pairs<kForward.most_pairs>(p.pairs, [&](auto k) { norm_forward_kernel<k, most_threads(k, kForward), true><<<grid, threads, 0, s>>>(a, p.z); });
+        with_pairs<kForward.most_pairs>(p.pairs, [&](auto k) { norm_forward_kernel<k, most_threads(k, kForward), true><<<grid, threads, p.lds, s>>>(a, p.z); });
     } else {
         with_pairs<kForward.chunk_pairs>(p.pairs, [&](auto k) {
-            norm_forward_kernel<k, kChunkThreads, false><<<grid, threads, 0, s>>>(a, p.z);
-            norm_apply_kernel<k><<<grid, threads, 0, s>>>(a, p.z);
+            norm_forward_kernel<k, kChunkThreads, false><<<grid, threads, p.lds, s>>>(a, p.z);
+            norm_apply_kernel<k><<<grid, threads, p.lds, s>>>(a, p.z);
         });
     }
     return hipGetLastError();
@@ -579,12 +591,12 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t s)
     float *const slabs = a.workspace + chunk_floats(p, a.groups, a.batch);
     const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
     if (p.z.chunks == 1) {
-        with_pairs<kBackward.most_pairs>(p.pairs, [&](auto k) { norm_backward_kernel<k, most_threads(k, kBackward), true><<<grid, threads, 0, s>>>(a, p.z, slabs); });
+        with_pairs<kBackward.most_pairs>(p.pairs, [&](auto k) { norm_backward_kernel<k, most_threads(k, kBackward), true><<<grid, threads, p.lds, s>>>(a, p.z, slabs); });
     } else {
         const dim3 every(static_cast<uint32_t>(rows * p.z.tiles));
         with_pairs<kBackward.chunk_pairs>(p.pairs, [&](auto k) {
-            norm_backward_kernel<k, kChunkThreads, false><<<grid, threads, 0, s>>>(a, p.z, slabs);
-            norm_apply_backward_kernel<k><<<every, threads, 0, s>>>(a, p.z);
+            norm_backward_kernel<k, kChunkThreads, false><<<grid, threads, p.lds, s>>>(a, p.z, slabs);
+            norm_apply_backward_kernel<k><<<every, threads, p.lds, s>>>(a, p.z);
         });
     }
     if (p.z.slabs > 1 && (a.dgamma || a.dbeta))
