@@ -406,7 +406,9 @@ int expert_combine_backward(const float *Ye, int32_t lde, const float *dY, int32
  * mean and rstd (groups, lds) are what the backward pass takes; both NULL without one.  A column's results depend on no other
  * column.  Y may be X itself where no backward pass needs it, with ldy = ldx; other overlaps are not allowed.
  * workspace: device scratch, 16-byte aligned, of group_norm_workspace_bytes() (may be NULL where that is 0); calls that overlap in time take one
- * each.  group_norm_workspace_bytes is (size_t)-1 for sizes that are refused.  Sums are held in 32 bits: numbers from about 1e18 on overflow them. */
+ * each.  group_norm_workspace_bytes is (size_t)-1 for sizes that are refused.  Sums are held in 32 bits: numbers from about 1e18 on overflow them.
+ * A call of which a launch would take 2^32 threads is refused before anything is written (NERVA_ERR_SHAPE); none does with up to 2^25 groups and 2^31
+ * entries (features x columns), or 2^34 in groups of 64 features and more. */
 size_t group_norm_workspace_bytes(int32_t features, int32_t groups, int32_t batch);
 int group_norm_forward(const float *X, int32_t ldx, const float *gamma, const float *beta, int32_t features, int32_t groups,
                        int32_t batch, float eps, int32_t act, float drop, int32_t layer, const int64_t *state, float *Y,
@@ -437,7 +439,8 @@ int dropout(const float *X, int32_t ldx, int32_t features, int32_t batch, float 
  * Sequences are runs of columns: starts (device, int32[sequences + 1], ascending, within 0 .. batch) holds their first columns and the end of the
  * last; they may be empty, and columns outside belong to none.
  * workspace: device scratch, 16-byte aligned, of label_loss_workspace_bytes() (0 for sizes that are refused); calls that overlap in time take one
- * each.  dZ may be Z itself, with lddz = ldz; other overlaps of inputs and outputs are not allowed. */
+ * each.  dZ may be Z itself, with lddz = ldz; other overlaps of inputs and outputs are not allowed.  A call of which a launch would take 2^32 threads is
+ * refused before anything is written (NERVA_ERR_SHAPE); none does with up to 2^26 columns and fewer than 2^22 sequences (or pairs). */
 size_t label_loss_workspace_bytes(int32_t classes, int32_t batch, int32_t sequences);
 /* logp[c] = l_c and sums[s] = sum of l_c over sequence s, unless NULL (one of them at least is given; sequences may be 0 and starts NULL
  * without sums). */

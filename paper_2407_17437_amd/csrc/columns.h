@@ -105,8 +105,9 @@ __device__ __forceinline__ float4 shfl_xor4(float4 v, int d)
 }
 __device__ __forceinline__ float sum4(float4 v) { return (v.x + v.y) + (v.z + v.w); }
 
-// exp(x) by one v_exp_f32: relative error 2^-24 (2 |x| + 2), of which the first part is the rounding of the argument
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.92596299e-8f, x * 1.44269504f)); }
+// exp(x) by one v_exp_f32: relative error 2^-24 (|x| + 2), of which the first part is the rounding of the argument.  (log2(e) in two parts, the smaller one first:
+// rounded to one, it makes all results too large by 1.3e-8 |x|, which a sum over many columns shows.)
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(fmaf(x, 1.44269504f, x * 1.92596299e-8f)); }
 
 }  // namespace
 }  // namespace nerva

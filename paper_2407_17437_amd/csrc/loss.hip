@@ -56,10 +56,11 @@ __device__ __forceinline__ void add_rows(Running &a, const float4 (&z)[U])
     a.sum = fma4(a.sum, exp_of4(a.top - top), s);
     a.top = top;
 }
-// over the threads with the same columns; the same in all of them.  lds: two float4 per wave and quad
+// over the threads of a chunk with the same columns; the same in all of them.  lds: two float4 per wave and quad
 __device__ __forceinline__ Running join(Running a, int lg, float4 *lds)
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, q = threadIdx.x & ((1 << lg) - 1), waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, q = threadIdx.x & ((1 << lg) - 1);
+    constexpr int waves = kThreads / kWave;
     for (int d = 1 << lg; d < kWave; d <<= 1) {
         const float4 top = max4(a.top, shfl_xor4(a.top, d));
         // (both lanes of a pair add the lower one's sum first)
@@ -67,7 +68,6 @@ __device__ __forceinline__ Running join(Running a, int lg, float4 *lds)
         a.sum = lane & d ? other + mine : mine + other;
         a.top = top;
     }
-    if (waves == 1) return a;
     float4 *const sums = lds + (waves << lg);
     if (lane < (1 << lg)) {
         lds[(wave << lg) + lane] = a.top;
@@ -207,14 +207,15 @@ __device__ __forceinline__ int2 columns_of(const LossArgs &a, int sequence)
 }
 __device__ __forceinline__ bool in_sequences(const LossArgs &a, int col) { return col >= a.starts[0] && col < a.starts[a.sequences]; }
 
-__device__ __forceinline__ float gradient_of(float z, const ColumnState &c, int i)
+// e: exp(z - top)
+__device__ __forceinline__ float gradient_of(float e, const ColumnState &c, int i)
 {
     if (c.c == 0.f) return 0.f;
-    return fmaf(-c.share, exp_of(z - c.top), i == c.label ? c.c : 0.f);
+    return fmaf(-c.share, e, i == c.label ? c.c : 0.f);
 }
-__device__ __forceinline__ float4 gradient_of4(float4 z, const ColumnState (&c)[4], int i)
+__device__ __forceinline__ float4 gradient_of4(float4 e, const ColumnState (&c)[4], int i)
 {
-    return make_float4(gradient_of(z.x, c[0], i), gradient_of(z.y, c[1], i), gradient_of(z.z, c[2], i), gradient_of(z.w, c[3], i));
+    return make_float4(gradient_of(e.x, c[0], i), gradient_of(e.y, c[1], i), gradient_of(e.z, c[2], i), gradient_of(e.w, c[3], i));
 }
 
 // ---- columns that a work-group holds ----
@@ -226,10 +227,9 @@ enum What { kLogProbs, kPolicy, kPreference };
 template <int K, What W>
 __global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, const Shape z, const LossSpace w, const Borders b)
 {
-    extern __shared__ float4 lds[];   // two per wave and quad
-    __shared__ double sums[kHeldThreads / kWave];
+    extern __shared__ float4 lds[];   // per wave and quad: maxima, then sums in 64 bits
+    __shared__ double sums[kHeldThreads / kWave], parts[(4 << kLanes) / kWave][4];
     __shared__ float tops[4 << kLanes];
-    __shared__ float of_tile[4 << kLanes];
     __shared__ int close[4 << kLanes];
     __shared__ double logp[4 << kLanes];
     __shared__ ColumnState states[4 << kLanes];
@@ -241,23 +241,41 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, co
     float4 x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = load_quad(a.Z + min(p.slot + k * p.slots, a.classes - 1) * a.ldz, p);
-    Running r{splat(-FLT_MAX), splat(0.f)};
+    const int lane = j & (kWave - 1), wave = j >> 6, waves = static_cast<int>(blockDim.x >> 6);
+    float4 top = splat(-FLT_MAX);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (p.slot + k * p.slots >= a.classes) x[k] = splat(-INFINITY);
-        r.top = max4(r.top, x[k]);
+        top = max4(top, x[k]);
     }
+    for (int d = 1 << z.lg; d < kWave; d <<= 1) top = max4(top, shfl_xor4(top, d));
+    if (waves > 1) {
+        if (lane < (1 << z.lg)) lds[(wave << z.lg) + lane] = top;
+        __syncthreads();
+        for (int u = 0; u < waves; ++u) top = max4(top, lds[(u << z.lg) + p.q]);
+    }
+    // x becomes the exponential, which the gradient takes as well; a thread's few are added up in 32 bits, the threads' sums in 64
+    float4 few = splat(0.f);
 #pragma unroll
-    for (int k = 0; k < K; ++k) r.sum = r.sum + exp_of4(x[k] - r.top);
-    r = join(r, z.lg, lds);
-    if (p.slot == 0) {
-        *reinterpret_cast<float4 *>(tops + 4 * p.q) = r.top;
-        *reinterpret_cast<float4 *>(of_tile + 4 * p.q) = r.sum;
+    for (int k = 0; k < K; ++k) {
+        x[k] = exp_of4(x[k] - top);
+        few = few + x[k];
     }
+    double part[4] = {few.x, few.y, few.z, few.w};
+    for (int d = 1 << z.lg; d < kWave; d <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) part[k] += __shfl_xor(part[k], d, kWave);
+    double *const of_waves = reinterpret_cast<double *>(lds + (waves << z.lg));
+    if (lane < (1 << z.lg))
+#pragma unroll
+        for (int k = 0; k < 4; ++k) of_waves[(wave << (z.lg + 2)) + 4 * lane + k] = part[k];
+    if (p.slot == 0) *reinterpret_cast<float4 *>(tops + 4 * p.q) = top;
     __syncthreads();
     if (mine) {
+        double sum = 0;
+        for (int u = 0; u < waves; ++u) sum += of_waves[u * width + j];
         c.top = tops[j];
-        set_sum(c, of_tile[j]);
+        set_sum(c, sum);
         if (a.logp && W != kPolicy) a.logp[col] = static_cast<float>(c.logp);
     }
     if constexpr (W == kPolicy) {
@@ -277,10 +295,24 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, co
         }
         if (mine && a.logp) a.logp[col] = static_cast<float>(c.logp);
         if (j < width) states[j] = state_of(c, t.weight != 0 ? static_cast<float>(t.weight * t.slope) : 0.f);
-        for (int k = 0; k < 4; ++k) {
-            const double s = block_sum(policy_share(a, t, k), sums);
-            if (j == 0 && z.tiles == 1) a.stats[k] = static_cast<float>(s);
-            else if (j == 0) w.shares[4 * static_cast<int64_t>(blockIdx.x) + k] = s;
+        // the four sums side by side: one after the other they take 6.7 us instead of 5.4 (10 classes x 100)
+        double share[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) share[k] = policy_share(a, t, k);
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) share[k] += __shfl_xor(share[k], d, kWave);
+        const int waves = static_cast<int>(blockDim.x >> 6), of = min(waves, (width + kWave - 1) >> 6);   // (waves that have columns)
+        if ((j & (kWave - 1)) == 0 && j >> 6 < of)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) parts[j >> 6][k] = share[k];
+        __syncthreads();
+        if (j < 4) {
+            double s = 0;
+            for (int u = 0; u < of; ++u) s += parts[u][j];
+            if (z.tiles == 1) a.stats[j] = static_cast<float>(s);
+            else w.shares[4 * static_cast<int64_t>(blockIdx.x) + j] = s;
         }
     } else {
         if (z.tiles > 1) {
@@ -330,7 +362,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, co
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int row = p.slot + k * p.slots;
-        if (row < a.classes) store_quad(a.dZ + row * a.lddz, p, gradient_of4(x[k], q, row));
+        if (row < a.classes) store_quad(a.dZ + row * a.lddz, p, gradient_of4(x[k], q, row));   // (x: exponentials)
     }
 }
 
@@ -507,6 +539,7 @@ __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArg
     ColumnState c[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) c[k] = w.columns[p.col + min(k, p.n - 1)];
+    const float4 top = make_float4(c[0].top, c[1].top, c[2].top, c[3].top);
     for (int i = first + p.slot; i < end; i += kLoads * p.slots) {
         float4 x[kLoads];
 #pragma unroll
@@ -514,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArg
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int row = i + u * p.slots;
-            if (row < end) store_quad(a.dZ + row * a.lddz, p, gradient_of4(x[u], c, row));
+            if (row < end) store_quad(a.dZ + row * a.lddz, p, gradient_of4(exp_of4(x[u] - top), c, row));
         }
     }
 }
@@ -576,7 +609,7 @@ void launch_held(const LossArgs &a, const Held &h, const LossSpace &w, const Bor
 {
     if constexpr (Most > 1)
         if (h.rows < Most) return launch_held<W, Most / 2>(a, h, w, b, s);
-    const int lds = 2 * static_cast<int>(sizeof(float4)) * (h.threads / kWave << h.z.lg);
+    const int lds = static_cast<int>(sizeof(float4) + 4 * sizeof(double)) * (h.threads / kWave << h.z.lg);
     held_kernel<Most, W><<<static_cast<uint32_t>(h.z.tiles), h.threads, lds, s>>>(a, h.z, w, b);
 }
 void launch_log_sums(const LossArgs &a, const Shape &z, const LossSpace &w, hipStream_t s)
@@ -635,9 +668,10 @@ hipError_t launch_policy(const LossArgs &a, hipStream_t s)
     const Shape z = chunks_of(a.classes, a.batch);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, 0);
     if (too_large(h, z, a.batch, 0)) return hipErrorInvalidConfiguration;
-    // An exponential is off by 2^-24 (2 |z - top| + 2), and the mean of |z - top| over p is at most log(classes) < 21; a thread adds up eight rows, then
-    // their sum to the others' (or its 16 rows), and 10 levels and up to 16 waves follow.
-    const double adds = h.rows ? h.rows : 3.0 * (z.rows / ((kThreads >> z.lg) * z.loads) + 1) + z.loads;
+    // In roundings of 2^-24: an exponential is off by |z - top| + 2, and the mean of |z - top| over p is at most log(classes) < 21 (z - top itself is
+    // rounded as well, by as much).  A thread adds up its rows, in chunks eight at a time and then their sum to the others', which takes an exponential and
+    // three roundings; ten levels of pairs and up to 16 waves follow with four each.
+    const double adds = h.rows ? h.rows : 5.0 * (z.rows / ((kThreads >> z.lg) * z.loads) + 1) + z.loads;
     const Borders b{a.clip_low < 1.f ? log1p(-static_cast<double>(a.clip_low)) : -INFINITY, log1p(static_cast<double>(a.clip_high)),
                     static_cast<float>((2 * 21 + 2 + 10 * 4 + 16 * 4 + adds) / (1 << 24))};
     if (h.rows) {

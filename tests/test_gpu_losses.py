@@ -112,6 +112,26 @@ def test_policy(nb, C, B, kind):
         assert bool((dz2 == dz).all()) and bool((stats2 == stats).all()) and bool((lp2 == lp).all())
 
 
+# one tile for all and one class more; what a work-group holds at most and a class more, in narrow tiles and in tiles that are not narrowed
+@pytest.mark.parametrize("C,B,kind", [(16, 256, "masked"), (64, 256, "plain"), (65, 256, "plain"), (64, 257, "masked"), (2048, 130, "masked"), (2049, 130, "plain"), (1024, 8200, "plain"),
+                                      (1025, 8193, "masked"), (4, 9001, "masked"), (300, 3001, "wide")])
+def test_around_the_limits(nb, C, B, kind):
+    rng = np.random.default_rng(C * 11 + B)
+    Z, labels = logits(rng, C, B, kind)
+    old, refs, A, w = policy_inputs(rng, Z, labels)
+    want = ref.Policy(Z, labels, old, refs, A, w, 0.2, 0.28, 0.04)
+    stats, lp, dz = run_policy(nb, Z, labels, old, refs, A, w, 0.2, 0.28, 0.04, (1, 2))
+    close(lp, want.L.logp, want.L.logp_tol, "logp"), close(stats, want.stats, want.stats_tol, "stats"), close(dz, want.dZ, want.dZ_tol, "dZ")
+    starts = cuts(rng, B, 14)
+    want = ref.Preference(Z, labels, starts, None, 0.02, 0.1)
+    dz, sums, margins, loss, scores, ws = blank(C, B, 3), nans(14), nans(7), nans(1), nans(14), workspace(nb, C, B, 14)
+    nb.preference_loss(matrix(Z, 5), gpu(labels), gpu(starts), None, C, B, 7, 0.02, 0.1, dz, sums, margins, loss, ws)
+    close(sums, want.sums, want.sums_tol, "sums"), close(margins, want.margins, want.margins_tol, "margins"), close(loss, np.array([want.loss]), want.loss_tol, "loss")
+    close(dz, want.dZ, want.dZ_tol, "dZ")
+    nb.label_log_probs(matrix(Z), gpu(labels), C, B, gpu(starts), 14, None, scores, ws)
+    assert bool((scores == sums).all()) and padding_untouched(dz)
+
+
 def test_policy_borders_are_decided_in_64_bits(nb):
     """Ratios that lie on their borders to within the last bits that an fp32 old log-probability can express: on both sides, and a clip of 0
     with the policy unmoved, where every column lies on its border."""

@@ -109,6 +109,20 @@ def test_norm_against_64_bits(nb, F, G, B):
         close(db, want.dbeta, want.dbeta_tol, "dbeta")
 
 
+# what a work-group holds at most, both ways, and a pair of rows more, in tiles that are not narrowed; tiles that few rows widen
+@pytest.mark.parametrize("F,G,B", [(512, 1, 8200), (1024, 1, 8201), (1026, 1, 8200), (2048, 1, 8193), (2052, 2, 4100), (256, 128, 4099), (130, 65, 5000)])
+def test_norm_of_many_columns(nb, F, G, B):
+    rng = np.random.default_rng(F + B)
+    X, gamma, beta, dY = data(rng, F, B)
+    want = ref.Norm(X, gamma, beta, G, 1e-5, 2, ref.factors(F, B, 0.1, LAYER, SEED, STEP), dY)
+    y, mean, rstd, dx, dg, db = both(nb, X, gamma, beta, dY, G, 2, 0.1, (0, 3, 0, 1, 2))
+    for got, name in ((y, "Y"), (mean, "mean"), (rstd, "rstd"), (dx, "dX")):
+        close(got, getattr(want, name), getattr(want, name + "_tol"), name)
+    # (sums over the columns: some hundred terms one after the other, of the columns' tiles, in a thread, then the slabs)
+    for got, name in ((dg, "dgamma"), (db, "dbeta")):
+        close(got, getattr(want, name), getattr(want, name + "_tol") * (1 + B / 1000), name)
+
+
 def test_relu_is_taken_from_the_same_number_both_ways(nb):
     """Entries whose argument is 0, and many close to it: dbeta counts the columns whose output is positive."""
     rng = np.random.default_rng(4)
