@@ -27,8 +27,9 @@ constexpr int kChunkThreads = 256;     // of groups that are cut into chunks
 // Philox4x32 of 10 rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011), key = seed.  Counter (column / 4, row / 2,
 // layer, step) gives the bits of four columns in two rows: word column % 4, its low half for the even row and its high half for the odd one.  So
 // an entry's bits depend on neither leading dimension nor batch nor launch.  16 bits an entry halve the generator's work, which
-// beside 8 bytes an entry is not small (some 130 cycles of a wave for 256 draws of 32 bits); the probability is a multiple of 2^-16
-// for it, and the scale is that of the multiple.
+// is not small beside 8 bytes an entry (20 products of 32 bits for 8 entries: 67 M entries normalised and dropped issue 36 instructions an
+// entry, which keep the vector units busy for some two thirds of the 105 us); the probability is a multiple of 2^-16 for it, and the scale is that of
+// the multiple.
 struct Bits {
     uint32_t x, y, z, w;
 };
@@ -145,7 +146,7 @@ __device__ __forceinline__ Rows<K> rows_of(const NormArgs &a, int group, int chu
 
 struct Shape {
     int lg, chunks, slabs;
-    bool past;
+    bool past, joined;       // joined: the first chunk's place holds what all chunks come to
     int64_t tiles;
 };
 // statistics of the entries that the work-group holds: mean and sum of squares about it; x becomes its difference from the mean
@@ -238,6 +239,66 @@ __global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const
     }
 }
 
+// A group's statistics from those of its chunks: means weighed by their rows, then all squares about the mean of the group (Chan, Golub, LeVeque 1979).
+// A thread adds up every slots-th chunk.
+template <int K>
+__device__ __forceinline__ void join_statistics(const NormArgs &a, const Shape &z, int group, const Spot &p, float4 *lds, float4 &mean, float4 &squares)
+{
+    const float *const stats = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
+    if (z.joined) {
+        mean = load_quad(stats, p);
+        squares = load_quad(stats + a.batch, p);
+        return;
+    }
+    mean = squares = splat(0.f);
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
+        const Rows<K> of = rows_of<K>(a, group, c, p);
+        mean = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p), mean);
+    }
+    mean = 1.f / static_cast<float>(a.features / a.groups) * column_sum(mean, z.lg, lds);
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
+        const Rows<K> of = rows_of<K>(a, group, c, p);
+        const float *const at = stats + 2 * static_cast<int64_t>(c) * a.batch;
+        const float4 d = load_quad(at, p) - mean;
+        squares = squares + fma4(static_cast<float>(of.end - of.first) * d, d, load_quad(at + a.batch, p));
+    }
+    squares = column_sum(squares, z.lg, second(lds, z.lg));
+}
+// the sums of h and h xh over the chunks, in the same way
+__device__ __forceinline__ void join_sums(const NormArgs &a, const Shape &z, int group, const Spot &p, float4 *lds, float4 &s, float4 &sx)
+{
+    const float *const sums = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
+    if (z.joined) {
+        s = load_quad(sums, p);
+        sx = load_quad(sums + a.batch, p);
+        return;
+    }
+    s = sx = splat(0.f);
+    for (int c = p.slot; c < z.chunks; c += p.slots) {
+        const float *const at = sums + 2 * static_cast<int64_t>(c) * a.batch;
+        s = s + load_quad(at, p);
+        sx = sx + load_quad(at + a.batch, p);
+    }
+    s = column_sum(s, z.lg, lds);
+    sx = column_sum(sx, z.lg, second(lds, z.lg));
+}
+// Groups of very many chunks: one work-group per group and tile leaves what they come to in the first one's place, before all the work-groups of the second
+// launch would add them up.
+template <int K, bool BACKWARD>
+__global__ __launch_bounds__(kChunkThreads) void norm_join_kernel(const NormArgs a, const Shape z)
+{
+    extern __shared__ float4 lds[];   // two per wave and quad
+    const int group = static_cast<int>(blockIdx.x / z.tiles);
+    const Spot p = spot_in(blockIdx.x % z.tiles, z.lg, a.batch);
+    float4 one, two;
+    if constexpr (BACKWARD) join_sums(a, z, group, p, lds, one, two);
+    else join_statistics<K>(a, z, group, p, lds, one, two);
+    if (p.slot) return;
+    float *const at = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
+    store_quad(at, p, one);
+    store_quad(at + a.batch, p, two);
+}
+
 // the second launch of a group of several chunks
 template <int K>
 __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArgs a, const Shape z)
@@ -251,23 +312,9 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArg
     r.load(a.X, a.ldx, p, x);
     Affine<K> w;
     w.load(a, r);
-    // the chunks' means weighed by their rows, then all squares about the mean of the group (Chan, Golub, LeVeque 1979); a thread adds up every
-    // slots-th chunk
     const int m = a.features / a.groups;
-    const float *const stats = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
-    float4 mean = splat(0.f), squares = splat(0.f);
-    for (int c = p.slot; c < z.chunks; c += p.slots) {
-        const Rows<K> of = rows_of<K>(a, group, c, p);
-        mean = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p), mean);
-    }
-    mean = 1.f / static_cast<float>(m) * column_sum(mean, z.lg, lds);
-    for (int c = p.slot; c < z.chunks; c += p.slots) {
-        const Rows<K> of = rows_of<K>(a, group, c, p);
-        const float *const at = stats + 2 * static_cast<int64_t>(c) * a.batch;
-        const float4 d = load_quad(at, p) - mean;
-        squares = squares + fma4(static_cast<float>(of.end - of.first) * d, d, load_quad(at + a.batch, p));
-    }
-    squares = column_sum(squares, z.lg, second(lds, z.lg));
+    float4 mean, squares;
+    join_statistics<K>(a, z, group, p, lds, mean, squares);
     const float4 rstd = rstd_of(squares, m, a.eps);
     if (p.slot == 0 && chunk == 0) {
         if (a.mean) store_quad(a.mean + group * a.lds, p, mean);
@@ -340,9 +387,14 @@ __device__ __forceinline__ void write_rows(const NormArgs &a, float *slabs, int 
     float *const b = n_slabs == 1 ? a.dbeta : slabs + (2 * static_cast<int64_t>(slab) + 1) * a.features;
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
-        for (int d = 1; d < 1 << lg; d <<= 1) {
-            dg[i] += __shfl_xor(dg[i], d, kWave);
-            db[i] += __shfl_xor(db[i], d, kWave);
+        if (lg == 3) {   // (without the local memory's crossbar: 47.3 -> 46.2 us for 8 x 1024 rows x 1024 columns, both ways)
+            dg[i] = group_sum<8>(dg[i]);
+            db[i] = group_sum<8>(db[i]);
+        } else {
+            for (int d = 1; d < 1 << lg; d <<= 1) {
+                dg[i] += __shfl_xor(dg[i], d, kWave);
+                db[i] += __shfl_xor(db[i], d, kWave);
+            }
         }
         if (!(threadIdx.x & ((1 << lg) - 1)) && r.in(i)) {
             if (g) g[r.row(i)] = dg[i];
@@ -403,14 +455,8 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_backward_kernel(cons
     w.load(a, r);
     float dg[2 * K] = {}, db[2 * K] = {};   // (left to the first launch)
     form_h<K>(a, x, g, r, w, p, mean, rstd, dg, db);
-    float4 s = splat(0.f), sx = splat(0.f);
-    for (int c = p.slot; c < z.chunks; c += p.slots) {
-        const float *const at = a.workspace + 2 * (static_cast<int64_t>(group) * z.chunks + c) * a.batch;
-        s = s + load_quad(at, p);
-        sx = sx + load_quad(at + a.batch, p);
-    }
-    s = column_sum(s, z.lg, lds);
-    sx = column_sum(sx, z.lg, second(lds, z.lg));
+    float4 s, sx;
+    join_sums(a, z, group, p, lds, s, sx);
     write_backward<K>(a, x, g, r, p, rstd, s, sx);
 }
 
@@ -485,6 +531,9 @@ struct Plan {
     int lds;                 // bytes
 };
 constexpr int64_t kFewGroups = 256;      // work-groups: one per compute unit
+// Chunks that all work-groups of the second launch would add up together, beyond which a launch of its own does it before them (300000 rows x 300 columns,
+// both ways: 1878 -> 737 us; 40000 x 300: 125 -> 112; but 100000 x 32, with 0.6 M of them: 50 -> 57).
+constexpr int64_t kManyChunks = 3 << 18;
 struct Limits {
     int most_pairs, most_threads;   // the most that a thread and a work-group hold of a group
     int chunk_pairs;                // of a thread at most, where the group is longer
@@ -502,11 +551,10 @@ Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
     p.z.lg = wide;
     p.z.past = static_cast<int64_t>(features) * batch > kCacheBytes / l.bytes;
     // Wider tiles for groups that leave lanes idle (groups of 8 rows, 64 groups x 4096 columns, both ways: 23.3 -> 16.1 us).  Narrower ones where there would
-    // be few work-groups, each with much to do (512 rows, 2 groups x 100 columns: 23.8 -> 13.6; 1024 rows, 1 x 1024: 30.6 -> 20.8); they would make 32 groups
-    // x 8192 columns read a line twice.
+    // be few work-groups, each with much to do (512 rows, 2 groups x 100 columns: 23.8 -> 13.6; 1024 rows, 1 x 1024: 30.6 -> 20.8).
     while (p.z.lg < widest && pairs << p.z.lg < kWave) ++p.z.lg;
     while (p.z.lg > 0 && groups * tiles(p.z.lg) < kFewGroups && pairs << p.z.lg > kWave) --p.z.lg;
-    // One tile for all columns, where 256 threads hold it, leaves no slabs to add up (32 rows, 32 groups x 32 columns, both ways: 12.1 -> 9.5 us; with 512
+    // One tile for all columns, where 256 threads hold it, leaves no slabs to add up (32 rows, 32 groups x 32 columns, both ways: 12.1 -> 8.7 us; with 512
     // threads 32 x 32 rows x 100 columns take 12.7 instead of 11.9).
     if (l.slabs && tiles(widest) == 1 && pairs << widest <= kGroupThreads) p.z.lg = widest;
     const bool few = groups * tiles(p.z.lg) < kFewGroups;
@@ -572,15 +620,19 @@ constexpr int most_threads(int pairs, const Limits &l) { return pairs < kGroupPa
 
 hipError_t launch_norm_forward(const NormArgs &a, hipStream_t s)
 {
-    const Plan p = plan_forward(a.features, a.groups, a.batch);
+    Plan p = plan_forward(a.features, a.groups, a.batch);
     const int64_t blocks = p.z.tiles * a.groups * p.z.chunks;
     if (!fits_launch(blocks, p.threads)) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
+    const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads), joins(static_cast<uint32_t>(p.z.tiles * a.groups));
     if (p.z.chunks == 1) {
         with_pairs<kForward.most_pairs>(p.pairs, [&](auto k) { norm_forward_kernel<k, most_threads(k, kForward), true><<<grid, threads, p.lds, s>>>(a, p.z); });
     } else {
         with_pairs<kForward.chunk_pairs>(p.pairs, [&](auto k) {
             norm_forward_kernel<k, kChunkThreads, false><<<grid, threads, p.lds, s>>>(a, p.z);
+            if (blocks * p.z.chunks > kManyChunks) {
+                norm_join_kernel<k, false><<<joins, threads, p.lds, s>>>(a, p.z);
+                p.z.joined = true;
+            }
             norm_apply_kernel<k><<<grid, threads, p.lds, s>>>(a, p.z);
         });
     }
@@ -589,17 +641,21 @@ hipError_t launch_norm_forward(const NormArgs &a, hipStream_t s)
 
 hipError_t launch_norm_backward(const NormArgs &a, hipStream_t s)
 {
-    const Plan p = plan_backward(a.features, a.groups, a.batch);
+    Plan p = plan_backward(a.features, a.groups, a.batch);
     const int64_t rows = static_cast<int64_t>(a.groups) * p.z.chunks, blocks = rows * p.z.slabs;
     if (!fits_launch(blocks, p.threads) || (p.z.chunks > 1 && !fits_launch(rows * p.z.tiles, p.threads))) return hipErrorInvalidConfiguration;
     float *const slabs = a.workspace + chunk_floats(p, a.groups, a.batch);
-    const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads);
+    const dim3 grid(static_cast<uint32_t>(blocks)), threads(p.threads), joins(static_cast<uint32_t>(p.z.tiles * a.groups));
     if (p.z.chunks == 1) {
         with_pairs<kBackward.most_pairs>(p.pairs, [&](auto k) { norm_backward_kernel<k, most_threads(k, kBackward), true><<<grid, threads, p.lds, s>>>(a, p.z, slabs); });
     } else {
         const dim3 every(static_cast<uint32_t>(rows * p.z.tiles));
         with_pairs<kBackward.chunk_pairs>(p.pairs, [&](auto k) {
             norm_backward_kernel<k, kChunkThreads, false><<<grid, threads, p.lds, s>>>(a, p.z, slabs);
+            if (rows * p.z.tiles * p.z.chunks > kManyChunks) {
+                norm_join_kernel<1, true><<<joins, threads, p.lds, s>>>(a, p.z);
+                p.z.joined = true;
+            }
             norm_apply_backward_kernel<k><<<every, threads, p.lds, s>>>(a, p.z);
         });
     }

@@ -109,6 +109,22 @@ def test_norm_against_64_bits(nb, F, G, B):
         close(db, want.dbeta, want.dbeta_tol, "dbeta")
 
 
+def test_groups_of_very_many_chunks(nb):
+    """Chunks whose sums a launch of its own adds up."""
+    rng = np.random.default_rng(12)
+    F, G, B = 160003, 1, 40
+    X, gamma, beta, dY = data(rng, F, B, offset=3.0)
+    want = ref.Norm(X, gamma, beta, G, 1e-5, 2, ref.factors(F, B, 0.1, LAYER, SEED, STEP), dY)
+    y, mean, rstd, dx, dg, db = both(nb, X, gamma, beta, dY, G, 2, 0.1, (0, 3, 0, 1, 2))
+    for got, name in ((y, "Y"), (mean, "mean"), (rstd, "rstd"), (dx, "dX"), (dg, "dgamma"), (db, "dbeta")):
+        close(got, getattr(want, name), getattr(want, name + "_tol"), name)
+    F, G, B = 2 * 60000, 2, 9
+    X, gamma, beta, dY = data(rng, F, B)
+    want = ref.Norm(X, gamma, beta, G, 1e-5, 1, np.ones((F, B)))
+    y, *_ = both(nb, X, gamma, beta, dY, G, 1, 0.0)
+    close(y, want.Y, want.Y_tol, "Y")
+
+
 # what a work-group holds at most, both ways, and a pair of rows more, in tiles that are not narrowed; tiles that few rows widen
 @pytest.mark.parametrize("F,G,B", [(512, 1, 8200), (1024, 1, 8201), (1026, 1, 8200), (2048, 1, 8193), (2052, 2, 4100), (256, 128, 4099), (130, 65, 5000)])
 def test_norm_of_many_columns(nb, F, G, B):
