@@ -26,7 +26,7 @@ namespace {
 constexpr int kThreads = 256;          // of chunks
 constexpr int kLanes = 6;              // log2 of the quads of their tiles: 256 columns
 constexpr int kLoads = 8, kFewLoads = 2;   // rows in flight per thread
-constexpr int64_t kBlocks = 4096;          // work-groups that the classes are cut for
+constexpr int64_t kBlocks = 8192;      // work-groups that the classes are cut for
 constexpr int kColumns = 16, kParts = 16;   // columns of a work-group that adds up chunks, threads of a column
 constexpr int kHeldThreads = 1024, kHeldRows = 8;    // of a work-group that holds its columns
 
@@ -81,24 +81,36 @@ __device__ __forceinline__ Running join(Running a, int lg, float4 *lds)
     return a;
 }
 
+template <int U, TileKind T>
+__device__ __forceinline__ Running sum_rows(const LossArgs &a, const Spot &p, int first, int end)
+{
+    Running r{splat(-FLT_MAX), splat(0.f)};
+    for (int i = first + p.slot; i < end; i += U * p.slots) {
+        float4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load_of<T>(a.Z + min(i + u * p.slots, end - 1) * a.ldz, p);
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = i + u * p.slots < end ? own_of<T>(x[u], p) : splat(-INFINITY);
+        add_rows(r, x);
+    }
+    return r;
+}
+// Chunk and tile of work-group b: all tiles of one chunk, then those of the next, so that those that run together read whole rows.  (All chunks of one tile first,
+// rows a power of two apart meet in few memory channels: 4096 classes x 8192, sums 40.4 instead of 33.0 us, policy loss 86 instead of 79.)
+struct Part {
+    int chunk, tile;
+};
+__device__ __forceinline__ Part part_of(int b, const Shape &z) { return {b / z.tiles, b % z.tiles}; }
 // One work-group: a chunk of the classes in a tile of columns.
 template <int U>
 __global__ __launch_bounds__(kThreads) void log_sum_kernel(const LossArgs a, const Shape z, float *partial)
 {
     __shared__ float4 lds[2 * kThreads / kWave << kLanes];
-    const int chunk = blockIdx.x % z.chunks;
-    const Spot p = spot_in(blockIdx.x / z.chunks, z.lg, a.batch);
-    const int first = chunk * z.rows, end = min(a.classes, first + z.rows);
-    Running r{splat(-FLT_MAX), splat(0.f)};
-    for (int i = first + p.slot; i < end; i += U * p.slots) {
-        float4 x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = load_few(a.Z + min(i + u * p.slots, end - 1) * a.ldz, p);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * p.slots >= end) x[u] = splat(-INFINITY);
-        add_rows(r, x);
-    }
+    const Part part = part_of(blockIdx.x, z);
+    const int chunk = part.chunk, first = chunk * z.rows, end = min(a.classes, first + z.rows);
+    const Spot p = spot_in(part.tile, z.lg, a.batch);
+    Running r;
+    with_kind(p, [&](auto kind) { r = sum_rows<U, kind>(a, p, first, end); });
     r = join(r, z.lg, lds);
     if (p.slot) return;
     float *const at = partial + 2 * static_cast<int64_t>(chunk) * a.batch;
@@ -249,8 +261,12 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(const LossArgs a, co
     PolicyInputs in{};
     if (W == kPolicy && mine) in = policy_inputs(a, col);
     float4 x[K];
+    with_kind(p, [&](auto kind) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = load_quad(a.Z + min(p.slot + k * p.slots, a.classes - 1) * a.ldz, p);
+        for (int k = 0; k < K; ++k) x[k] = load_of<kind>(a.Z + min(p.slot + k * p.slots, a.classes - 1) * a.ldz, p);
+#pragma unroll
+        for (int k = 0; k < K; ++k) x[k] = own_of<kind>(x[k], p);
+    });
     const int lane = j & (kWave - 1), wave = j >> 6, waves = static_cast<int>(blockDim.x >> 6);
     float4 top = splat(-FLT_MAX);
 #pragma unroll
@@ -541,8 +557,27 @@ __device__ __forceinline__ void write_stats(const LossArgs &a, const double *sha
 }
 __global__ __launch_bounds__(kWave) void stats_kernel(const LossArgs a, const double *shares, const int n) { write_stats(a, shares, n); }
 
+template <int U, TileKind T, bool PAST>
+__device__ __forceinline__ void write_gradient(const LossArgs &a, const LossSpace &w, const Spot &p, int first, int end)
+{
+    ColumnState c[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] = w.columns[p.col + (T == kWhole ? k : min(k, p.n - 1))];
+    const float4 top = make_float4(c[0].top, c[1].top, c[2].top, c[3].top);
+    for (int i = first + p.slot; i < end; i += U * p.slots) {
+        float4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load_of<T>(a.Z + min(i + u * p.slots, end - 1) * a.ldz, p);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = i + u * p.slots;
+            if (row < end) store_of<T, PAST>(a.dZ + row * a.lddz, p, gradient_of4(exp_of4(own_of<T>(x[u], p) - top), c, row));
+        }
+    }
+}
 // One work-group: a chunk of the classes in a tile of columns, from the last one read to the first.  `shares`: how many shares of the loss there are
 // (policy: of four terms each).
+template <int U>
 __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArgs a, const Shape z, const LossSpace w, const int shares)
 {
     if (blockIdx.x == 0 && threadIdx.x < kWave) {
@@ -553,39 +588,32 @@ __global__ __launch_bounds__(kThreads) void logits_gradient_kernel(const LossArg
             if (threadIdx.x == 0) *a.loss = static_cast<float>(s / shares);
         }
     }
-    const int unit = gridDim.x - 1 - blockIdx.x, chunk = unit % z.chunks;
-    const Spot p = spot_in(unit / z.chunks, z.lg, a.batch, z.past);
+    const Part part = part_of(gridDim.x - 1 - blockIdx.x, z);
+    const Spot p = spot_in(part.tile, z.lg, a.batch, z.past);
     if (p.n == 0) return;
-    const int first = chunk * z.rows, end = min(a.classes, first + z.rows);
-    ColumnState c[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) c[k] = w.columns[p.col + min(k, p.n - 1)];
-    const float4 top = make_float4(c[0].top, c[1].top, c[2].top, c[3].top);
-    for (int i = first + p.slot; i < end; i += kLoads * p.slots) {
-        float4 x[kLoads];
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) x[u] = load_quad(a.Z + min(i + u * p.slots, end - 1) * a.ldz, p);
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int row = i + u * p.slots;
-            if (row < end) store_quad(a.dZ + row * a.lddz, p, gradient_of4(exp_of4(x[u] - top), c, row));
-        }
-    }
+    const int first = part.chunk * z.rows, end = min(a.classes, first + z.rows);
+    // (few rows a thread: never past the caches, and little code, which small launches wait for)
+    with_kind(p, [&](auto kind) {
+        if (U == kLoads && z.past) write_gradient<U, kind, U == kLoads>(a, w, p, first, end);
+        else write_gradient<U, kind, false>(a, w, p, first, end);
+    });
 }
 
 // ---- launches ----
 constexpr int64_t kFewTiles = 256;       // one per compute unit
-constexpr int64_t kFewChunks = 128;      // in all tiles (4096 classes x 100: 19.1 -> 15.8 us; with 128 chunks already, 8192 x 100, more of them take 20.1 instead of 18.0)
+// Chunks of eight rows a thread, in all tiles, below which they are of two rows a thread: where they are added up (4096 classes x 100: 19.1 -> 15.8 us; with 128 chunks
+// already, 8192 x 100, more of them take 20.1 instead of 18.0), and where only the gradient is cut into them (1001 x 777, three launches: 15.8 -> 13.7).
+constexpr int64_t kFewSums = 128, kFewGradients = 512;
 
 // Of columns that are cut into chunks.
-Shape chunks_of(int32_t classes, int32_t batch)
+Shape chunks_of(int32_t classes, int32_t batch, bool sums)
 {
     Shape z{};
     z.lg = lanes_for(batch, kLanes);
     z.tiles = static_cast<int32_t>((batch + (INT64_C(4) << z.lg) - 1) >> (z.lg + 2));
     const auto cut = [&](int loads) { return static_cast<int64_t>(loads) * (kThreads >> z.lg); };
     // a few rows a thread where that gives more compute units something to do
-    z.loads = z.tiles * ((classes + cut(kLoads) - 1) / cut(kLoads)) < kFewChunks ? kFewLoads : kLoads;
+    z.loads = z.tiles * ((classes + cut(kLoads) - 1) / cut(kLoads)) < (sums ? kFewSums : kFewGradients) ? kFewLoads : kLoads;
     const int64_t step = cut(z.loads), most = (classes + step - 1) / step, want = std::max<int64_t>(1, kBlocks / z.tiles);
     const int64_t steps = (most + std::min(most, want) - 1) / std::min(most, want);
     z.rows = static_cast<int>(std::min<int64_t>(steps * step, classes));
@@ -641,7 +669,9 @@ void launch_log_sums(const LossArgs &a, const Shape &z, const LossSpace &w, hipS
 }
 void launch_gradient(const LossArgs &a, const Shape &z, const LossSpace &w, int shares, hipStream_t s)
 {
-    logits_gradient_kernel<<<static_cast<uint32_t>(z.tiles) * z.chunks, kThreads, 0, s>>>(a, z, w, shares);
+    const uint32_t grid = static_cast<uint32_t>(z.tiles) * z.chunks;
+    if (z.loads == kLoads) logits_gradient_kernel<kLoads><<<grid, kThreads, 0, s>>>(a, z, w, shares);
+    else logits_gradient_kernel<kFewLoads><<<grid, kThreads, 0, s>>>(a, z, w, shares);
 }
 // Threads of a work-group that adds up a sequence: few for short ones (pairs of 62 columns on average: 14.2 -> 13.3 us with the launches around), not for longer ones (512: 17.6, with few
 // 20.5).
@@ -657,7 +687,7 @@ bool too_large(const Held &h, const Shape &z, int32_t batch, int32_t sequences)
 LossSpace loss_space(void *memory, int32_t classes, int32_t batch, int32_t sequences)
 {
     const Held h = held_of(classes, batch);
-    const int64_t chunks = h.rows ? 0 : chunks_of(classes, batch).chunks;
+    const int64_t chunks = h.rows ? 0 : chunks_of(classes, batch, true).chunks;
     LossSpace w;
     w.columns = static_cast<ColumnState *>(memory);
     w.logp = reinterpret_cast<double *>(w.columns + batch);
@@ -670,7 +700,7 @@ LossSpace loss_space(void *memory, int32_t classes, int32_t batch, int32_t seque
 hipError_t launch_log_probs(const LossArgs &a, hipStream_t s)
 {
     const Held h = held_of(a.classes, a.batch);
-    const Shape z = chunks_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch, !h.rows);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, a.sequences);
     if (too_large(h, z, a.batch, a.sequences)) return hipErrorInvalidConfiguration;
     bool summed;
@@ -689,7 +719,7 @@ hipError_t launch_log_probs(const LossArgs &a, hipStream_t s)
 hipError_t launch_policy(const LossArgs &a, hipStream_t s)
 {
     const Held h = held_of(a.classes, a.batch);
-    const Shape z = chunks_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch, !h.rows);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, 0);
     if (too_large(h, z, a.batch, 0)) return hipErrorInvalidConfiguration;
     // In roundings of 2^-24: an exponential is off by |z - top| + 2, and the mean of |z - top| over p is at most log(classes) < 21 (z - top itself is
@@ -712,7 +742,7 @@ hipError_t launch_policy(const LossArgs &a, hipStream_t s)
 hipError_t launch_preference(const LossArgs &a, hipStream_t s)
 {
     const Held h = held_of(a.classes, a.batch);
-    const Shape z = chunks_of(a.classes, a.batch);
+    const Shape z = chunks_of(a.classes, a.batch, !h.rows);
     const LossSpace w = loss_space(a.workspace, a.classes, a.batch, a.sequences);
     if (too_large(h, z, a.batch, a.sequences / 2)) return hipErrorInvalidConfiguration;
     if (h.rows) {
