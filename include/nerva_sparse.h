@@ -452,7 +452,7 @@ int label_log_probs(const float *Z, int32_t ldz, const int32_t *labels, int32_t 
  * weights: float[batch], NULL for 1/batch; a column of weight 0 does not count.  ref_logp NULL: no KL term.  Where r lies beyond the border
  * that A bounds it by, the first term has no gradient; on which side it lies is decided in 64 bits.
  * logp: float[batch], l_c (may be NULL).  stats: float[4] on the device: the loss, its first term, the weighted KL term (without beta) and the
- * weight of the columns beyond their border.  0 <= clip_low, clip_high, beta, finite. */
+ * weight of the columns beyond their border.  0 <= clip_low, clip_high, beta, finite.  workspace: for 0 sequences. */
 int policy_loss(const float *Z, int32_t ldz, const int32_t *labels, const float *old_logp, const float *ref_logp,
                 const float *advantages, const float *weights, int32_t classes, int32_t batch, float clip_low, float clip_high,
                 float beta, float *dZ, int32_t lddz, float *logp, float *stats, void *workspace, size_t workspace_bytes,

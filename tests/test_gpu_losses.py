@@ -282,6 +282,51 @@ def test_captured_losses(nb):
                 assert torch.equal(a, b)
 
 
+def test_two_streams_at_once(nb):
+    """Calls that overlap, each with a workspace of its own, on streams given as an argument and as the current one."""
+    import torch
+    rng = np.random.default_rng(19)
+    C, B = 3000, 500
+    Z, labels = logits(rng, C, B, "masked")
+    inputs = [gpu(t) for t in policy_inputs(rng, Z, labels)]
+    z, lab, starts = matrix(Z, 4), gpu(labels), gpu(np.array([0, 100, 250, 400, 500], np.int32))
+    x, ga, st = matrix(rng.standard_normal((1200, B))), gpu(np.ones(1200, np.float32)), gpu(np.array([3, 4], np.int64))
+
+    def policy(ws, out, stream=None):
+        nb.policy_loss(z, lab, *inputs, C, B, 0.2, 0.3, 0.1, out[0], out[1], out[2], ws, stream)
+
+    def preference(ws, out, stream=None):
+        nb.preference_loss(z, lab, starts, None, C, B, 2, 0.1, 0.05, out[0], out[1], out[2], None, ws, stream)
+
+    def norm(ws, out, stream=None):
+        nb.group_norm_forward(x, ga, None, 1200, 1, B, 1e-5, 2, 0.3, 0, st, out[0], out[1], out[2], ws, stream)
+        nb.group_norm_backward(x, ga, None, out[1], out[2], x, 1200, 1, B, 2, 0.3, 0, st, out[3], out[4], None, ws, stream)
+    sets = [(policy, lambda: [blank(C, B), nans(B), nans(4)], lambda: workspace(nb, C, B)), (preference, lambda: [blank(C, B), nans(4), nans(2)], lambda: workspace(nb, C, B, 4)),
+            (norm, lambda: [blank(1200, B), blank(1, B), blank(1, B), blank(1200, B), nans(1200)],
+             lambda: torch.zeros(max(4, nb.group_norm_workspace_bytes(1200, 1, B) // 4), device="cuda"))]
+    alone = []
+    for call, outputs, ws in sets:
+        out = outputs()
+        call(ws(), out)
+        alone.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    runs = [[(s[1](), s[2]()) for s in sets] for _ in range(4)]
+    torch.cuda.synchronize()
+    for run in runs:
+        for k, (call, _, _) in enumerate(sets):
+            if k % 2:
+                with torch.cuda.stream(streams[k]):
+                    call(run[k][1], run[k][0])
+            else:
+                call(run[k][1], run[k][0], streams[k])
+    torch.cuda.synchronize()
+    for run in runs:
+        for k in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(run[k][0], alone[k]) if not bool(b.isnan().any()))
+            assert all(torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)) for a, b in zip(run[k][0], alone[k]))
+
+
 def test_rows_far_apart(nb):
     """Rows 2^26 entries apart: offsets beyond 32 bits."""
     import torch
