@@ -541,7 +541,10 @@ struct Limits {
     bool slabs;                     // tiles leave sums to be added up
 };
 constexpr Limits kForward{8, 1024, 4, 8, false}, kBackward{8, 512, 2, 12, true};
-constexpr int kGroupThreads = 256, kGroupPairs = 4;
+// Threads of a work-group, before a thread takes kGroupPairs pairs.  More of them where there are few work-groups: a compute unit has one, whose threads
+// each have less to do in turn (both ways, 256 -> 512 threads: 1532 rows, 2 groups x 12 columns 20.1 -> 17.0 us, 2048 rows, 1 x 553 36.2 -> 32.2; 1024
+// threads take 17.2 and 34.1).
+constexpr int kGroupThreads = 256, kFewThreads = 512, kGroupPairs = 4;
 Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
 {
     Plan p{};
@@ -561,7 +564,7 @@ Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
     p.z.tiles = tiles(p.z.lg);
     const int64_t held = pairs << p.z.lg;   // threads, of one pair each
     p.pairs = 1;
-    while (p.pairs < kGroupPairs && held > kGroupThreads * p.pairs) p.pairs *= 2;
+    while (p.pairs < kGroupPairs && held > (few ? kFewThreads : kGroupThreads) * p.pairs) p.pairs *= 2;
     while (p.pairs < l.most_pairs && held > l.most_threads * p.pairs) p.pairs *= 2;
     int64_t threads = (held + p.pairs - 1) / p.pairs;
     threads = (threads + kWave - 1) / kWave * kWave;
@@ -616,7 +619,7 @@ void with_pairs(int pairs, F &&f)
     f(Pairs<Most>());
 }
 // threads that the kernels of K pairs are compiled for
-constexpr int most_threads(int pairs, const Limits &l) { return pairs < kGroupPairs ? kGroupThreads : l.most_threads; }
+constexpr int most_threads(int pairs, const Limits &l) { return pairs < kGroupPairs ? kFewThreads : l.most_threads; }
 
 hipError_t launch_norm_forward(const NormArgs &a, hipStream_t s)
 {
