@@ -633,9 +633,14 @@ Held held_of(int32_t classes, int32_t batch)
     const auto tiles = [&](int lg) { return (batch + (INT64_C(4) << lg) - 1) >> (lg + 2); };
     const auto held = [&](int lg) { return static_cast<int64_t>(classes) << lg; };
     int lg = lanes_for(batch, kLanes);
+    // The most that a work-group holds of columns that make few tiles, in quads.  Twice as many in one tile of 8 to 128 columns (policy loss, preference loss and
+    // log-probabilities of 500 classes x 32, held and cut into chunks: 9.4, 9.4, 5.6 us and 11.6, 15.0, 11.4; 128 x 100: 11.0, 12.0, 5.5 and 12.6, 15.2, 11.3); not of fewer columns,
+    // which keep few lanes busy (4096 x 3: 20.9, 20.1, 11.3 held, 13.1, 15.2, 8.5 in chunks), nor of 256, whose narrow tiles are as fast or
+    // faster (64 x 256: 10.2, 14.1, 8.0 in one tile, 9.0, 11.1, 7.6 in 64).
+    const auto most = [&](int lg) { return (tiles(lg) == 1 && lg > 0 && lg < kLanes ? 4 : 2) * kHeldThreads; };
     // one tile for all, with no launch for the sums behind it; or tiles of 32 columns, wider ones where they leave lanes idle, narrower ones where there
     // would be few
-    if (tiles(lg) > 1 || held(lg) > 4 * kHeldThreads) {
+    if (tiles(lg) > 1 || held(lg) > most(lg)) {
         const int widest = lg;
         lg = lanes_for(batch, 3);
         while (lg < widest && held(lg) < kWave) ++lg;
@@ -644,7 +649,7 @@ Held held_of(int32_t classes, int32_t batch)
     h.z.lg = lg;
     h.z.tiles = static_cast<int32_t>(tiles(lg));
     h.z.past = 8 * static_cast<int64_t>(classes) * batch > kCacheBytes;
-    if (held(lg) > kHeldRows * kHeldThreads || (h.z.tiles < kFewTiles && held(lg) > 2 * kHeldThreads)) return h;
+    if (held(lg) > kHeldRows * kHeldThreads || (h.z.tiles < kFewTiles && held(lg) > most(lg))) return h;
     h.rows = 1;
     while (h.rows < kHeldRows && held(lg) > (h.rows < 4 ? 256 : kHeldThreads) * h.rows) h.rows *= 2;
     const int64_t threads = std::max<int64_t>((held(lg) + h.rows - 1) / h.rows, 4 << lg);
