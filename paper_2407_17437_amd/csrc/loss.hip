@@ -183,7 +183,8 @@ __device__ __forceinline__ PolicyTerm policy_term(const LossArgs &a, const Borde
     PolicyTerm t{};
     t.weight = !c.counts ? 0 : a.weights ? static_cast<double>(in.weight) : 1.0 / a.batch;
     if (t.weight == 0) return t;
-    const double A = in.advantage, d = c.logp - in.old_logp, r = exp(d);
+    // (a ratio beyond 64 bits stays a number, of which an advantage of 0 makes 0; a NaN stays one)
+    const double A = in.advantage, d = c.logp - in.old_logp, r = exp(d > 709.0 ? 709.0 : d);
     const double border = A > 0 ? b.high : b.low;
     t.clipped = A > 0 ? d > border : A < 0 && d < border;
     t.close = A != 0 && fabs(d - border) <= b.margin;
@@ -191,8 +192,8 @@ __device__ __forceinline__ PolicyTerm policy_term(const LossArgs &a, const Borde
     t.slope = t.clipped ? 0.0 : -A * r;
     if (a.ref_logp) {
         const double g = in.ref_logp - c.logp, q = exp(g);
-        t.kl = q - g - 1;
-        t.slope += a.beta * (1 - q);
+        t.kl = q > DBL_MAX ? q : q - g - 1;
+        if (a.beta != 0.f) t.slope += a.beta * (1 - q);   // (q and the term may be infinite, of which a factor of 0 takes nothing)
     }
     return t;
 }
@@ -200,7 +201,7 @@ __device__ __forceinline__ PolicyTerm policy_term(const LossArgs &a, const Borde
 __device__ __forceinline__ double policy_share(const LossArgs &a, const PolicyTerm &t, int k)
 {
     if (t.weight == 0) return 0;
-    return t.weight * (k == 0 ? t.surrogate + a.beta * t.kl : k == 1 ? t.surrogate : k == 2 ? t.kl : t.clipped ? 1.0 : 0.0);
+    return t.weight * (k == 0 ? (a.beta != 0.f ? t.surrogate + a.beta * t.kl : t.surrogate) : k == 1 ? t.surrogate : k == 2 ? t.kl : t.clipped ? 1.0 : 0.0);
 }
 
 // The preference loss of a pair from its margin: the loss, and its derivative by the chosen sequence's sum times the number of pairs.
