@@ -213,7 +213,9 @@ __device__ __forceinline__ PairTerm pair_term(const LossArgs &a, double x)
     // (the derivative from what is small, so that it does not vanish beside 1)
     const double e = exp(-fabs(x)), tail = log1p(e), t = a.smoothing;
     const double above = x > 0 ? 1 / (1 + e) : e / (1 + e), below = x > 0 ? e / (1 + e) : 1 / (1 + e);
-    return {(1 - t) * (tail + fmax(-x, 0.0)) + t * (tail + fmax(x, 0.0)), (t * above - (1 - t) * below) * a.beta};
+    // (a side that has no share takes nothing, however large its loss is)
+    const double chosen = t < 1 ? (1 - t) * (tail + fmax(-x, 0.0)) : 0.0, rejected = t > 0 ? t * (tail + fmax(x, 0.0)) : 0.0;
+    return {chosen + rejected, (t * above - (1 - t) * below) * a.beta};
 }
 __device__ __forceinline__ double margin_of(const LossArgs &a, int pair, double chosen, double rejected)
 {
