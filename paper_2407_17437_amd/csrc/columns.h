@@ -55,32 +55,9 @@ __device__ __forceinline__ int64_t near_tile(int64_t b, int64_t n, int lg)
     return (set << (3 + shift)) + ((in_set & 7) << shift) + (in_set >> 3);
 }
 
-// Four columns of a row.  In a tile that is not whole they are read and written one by one, so that an output may lie where the input does and
-// nothing beyond the batch is touched; what is read in place of a column that does not exist is the batch's last one.
-__device__ __forceinline__ float4 load_quad(const float *row, const Spot &p)
-{
-    if (p.whole) return ld4(row + p.col);
-    const int last = p.batch - 1;
-    return make_float4(row[min(p.col, last)], row[min(p.col + 1, last)], row[min(p.col + 2, last)], row[min(p.col + 3, last)]);
-}
-__device__ __forceinline__ void store_quad(float *row, const Spot &p, float4 x)
-{
-    if (p.whole) {
-        if (p.past) {
-            const v4f_any r = {x.x, x.y, x.z, x.w};
-            __builtin_nontemporal_store(r, reinterpret_cast<v4f_any *>(row + p.col));
-        } else {
-            st4(row + p.col, x);
-        }
-        return;
-    }
-    if (p.n > 0) row[p.col] = x.x;
-    if (p.n > 1) row[p.col + 1] = x.y;
-    if (p.n > 2) row[p.col + 2] = x.z;
-    if (p.n > 3) row[p.col + 3] = x.w;
-}
-// The same for loops that are compiled for each kind of tile: in one that is not whole the lane with the last columns reads the batch's last four, of which
-// `own_of` keeps its own once all reads of a loop are under way, and a batch of one to three columns takes no more reads than columns.  (Read one by one by
+// Four columns of a row, for loops that are compiled for each kind of tile.  An output may lie where the input does and nothing beyond the batch is touched: in a tile that is not
+// whole the lane with the batch's last columns reads its last four, of which `own_of` keeps the lane's own once all reads of a loop are under way (in place of columns that do not exist:
+// the batch's last one), and writes its own one by one.  A batch of one to three columns takes no more reads than columns.  (Read one by one by
 // all lanes of such a tile, the preference loss of 5000 classes x 1000 takes 30.6 us instead of 26.4.)
 enum TileKind { kWhole, kPart, kFewColumns };
 template <TileKind T>
@@ -121,6 +98,50 @@ __device__ __forceinline__ void store_of(float *row, const Spot &p, float4 x)
     if (p.n > 0) row[p.col] = x.x;
     if (p.n > 1) row[p.col + 1] = x.y;
     if (p.n > 2) row[p.col + 2] = x.z;
+}
+// The quads of N rows, row(i), in one loop for whole tiles and others, which takes less code and time than one for each kind (dropout of two operands, 1024 x 100: 5.7 us instead
+// of 6.1, 8191 x 9001: 242 instead of 251; with single reads in tiles that are not whole 6.6 and 248, 4096 x 1001 20.5 instead of 13.5, norm of 8190 rows x 777 forward
+// 21.5 instead of 20.5).
+template <int N, typename F>
+__device__ __forceinline__ void load_quads(F &&row, const Spot &p, float4 (&x)[N])
+{
+    if (p.batch >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = load_of<kPart>(row(i), p);
+        if (p.whole || !(p.batch & 3)) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = own_of<kPart>(x[i], p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = load_of<kFewColumns>(row(i), p);
+    }
+}
+__device__ __forceinline__ float4 load_quad(const float *row, const Spot &p)
+{
+    float4 x[1];
+    load_quads([&](int) { return row; }, p, x);
+    return x[0];
+}
+// A quad with single reads in a tile that is not whole: fewer registers, which norm's backward pass is short of (8192 rows in 32 groups x 8192 columns, both ways: 291 us
+// instead of 296; 1024 rows in one group, whose kernel would keep 112 bytes a thread in scratch memory: 52 instead of 59).
+__device__ __forceinline__ float4 load_singly(const float *row, const Spot &p)
+{
+    if (p.whole) return ld4(row + p.col);
+    const int last = p.batch - 1;
+    return make_float4(row[min(p.col, last)], row[min(p.col + 1, last)], row[min(p.col + 2, last)], row[min(p.col + 3, last)]);
+}
+__device__ __forceinline__ void store_quad(float *row, const Spot &p, float4 x)
+{
+    if (p.whole) {
+        if (p.past) {
+            const v4f_any r = {x.x, x.y, x.z, x.w};
+            __builtin_nontemporal_store(r, reinterpret_cast<v4f_any *>(row + p.col));
+        } else {
+            st4(row + p.col, x);
+        }
+        return;
+    }
+    store_of<kPart, false>(row, p, x);
 }
 // 0 for columns that do not exist
 __device__ __forceinline__ float4 existing(float4 x, const Spot &p)

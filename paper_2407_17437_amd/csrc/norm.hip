@@ -144,12 +144,17 @@ struct Rows {
     __device__ __forceinline__ int readable(int i) const { return min(max(row(i), first), end - 1); }
     __device__ __forceinline__ void load(const float *X, int64_t ld, const Spot &p, float4 (&x)[2 * K]) const
     {
+        load_quads([&](int i) { return X + readable(i) * ld; }, p, x);
+    }
+    // the same for the backward pass
+    __device__ __forceinline__ void load_singly(const float *X, int64_t ld, const Spot &p, float4 (&x)[2 * K]) const
+    {
         if (p.whole) {
 #pragma unroll
             for (int i = 0; i < 2 * K; ++i) x[i] = ld4(X + readable(i) * ld + p.col);
         } else {
 #pragma unroll
-            for (int i = 0; i < 2 * K; ++i) x[i] = load_quad(X + readable(i) * ld, p);
+            for (int i = 0; i < 2 * K; ++i) x[i] = nerva::load_singly(X + readable(i) * ld, p);
         }
     }
 };
@@ -318,15 +323,15 @@ __device__ __forceinline__ void join_sums(const NormArgs &a, const Shape &z, int
 {
     const float *const sums = a.workspace + 2 * static_cast<int64_t>(group) * z.chunks * a.batch;
     if (z.joined) {
-        s = load_quad(sums, p);
-        sx = load_quad(sums + a.batch, p);
+        s = load_singly(sums, p);
+        sx = load_singly(sums + a.batch, p);
         return;
     }
     s = sx = splat(0.f);
     for (int c = p.slot; c < z.chunks; c += p.slots) {
         const float *const at = sums + 2 * static_cast<int64_t>(c) * a.batch;
-        s = s + load_quad(at, p);
-        sx = sx + load_quad(at + a.batch, p);
+        s = s + load_singly(at, p);
+        sx = sx + load_singly(at + a.batch, p);
     }
     s = column_sum(s, z.lg, lds);
     sx = column_sum(sx, z.lg, second(lds, z.lg));
@@ -471,9 +476,9 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(const NormArgs a, cons
         // (rows' addresses in three operands, kept from one tile to the next, would take more registers than the entries)
         asm volatile("" : "+v"(r.pair));
         float4 x[2 * K], g[2 * K], s, sx;
-        r.load(a.X, a.ldx, p, x);
-        r.load(a.dY, a.lddy, p, g);
-        const float4 mean = load_quad(a.mean + group * a.lds, p), rstd = load_quad(a.rstd + group * a.lds, p);
+        r.load_singly(a.X, a.ldx, p, x);
+        r.load_singly(a.dY, a.lddy, p, g);
+        const float4 mean = load_singly(a.mean + group * a.lds, p), rstd = load_singly(a.rstd + group * a.lds, p);
         form_h<K>(a, x, g, r, w, p, mean, rstd, dg, db);
         column_sums_of_h<K>(x, g, r, z.lg, lds, s, sx);
         if constexpr (WHOLE) {
@@ -497,9 +502,9 @@ __global__ __launch_bounds__(kChunkThreads) void norm_apply_backward_kernel(cons
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
     const Rows<K> r = rows_of<K>(a, group, chunk, p);
     float4 x[2 * K], g[2 * K];
-    r.load(a.X, a.ldx, p, x);
-    r.load(a.dY, a.lddy, p, g);
-    const float4 mean = load_quad(a.mean + group * a.lds, p), rstd = load_quad(a.rstd + group * a.lds, p);
+    r.load_singly(a.X, a.ldx, p, x);
+    r.load_singly(a.dY, a.lddy, p, g);
+    const float4 mean = load_singly(a.mean + group * a.lds, p), rstd = load_singly(a.rstd + group * a.lds, p);
     Affine<K> w;
     w.load(a, r);
     float dg[2 * K] = {}, db[2 * K] = {};   // (left to the first launch)
@@ -553,13 +558,9 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const DropoutArgs
     const Spot p = spot_in(blockIdx.x % tiles, lg, a.batch, past);
     const int64_t pair0 = static_cast<int64_t>(blockIdx.x / tiles) * (kDropPairs * p.slots) + p.slot;
     if (p.n == 0) return;
-    const float *const X = a.X;
     float4 x[2 * kDropPairs];
-#pragma unroll
-    for (int i = 0; i < 2 * kDropPairs; ++i) {
-        const int64_t f = 2 * (pair0 + (i >> 1) * p.slots) + (i & 1);
-        if (f < a.features) x[i] = load_quad(X + f * a.ldx, p);
-    }
+    // (of rows beyond the last some row is read)
+    load_quads([&](int i) { return a.X + min(2 * (pair0 + (i >> 1) * p.slots) + (i & 1), static_cast<int64_t>(a.features) - 1) * a.ldx; }, p, x);
     Drawn d{};
     if (a.drop.cut) d = drawn_from(a.drop);
 #pragma unroll
