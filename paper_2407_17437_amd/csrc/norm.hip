@@ -107,31 +107,8 @@ __device__ __forceinline__ float4 column_sum(float4 v, int lg, float4 *lds)
     return s;
 }
 
-// the memory of a second sum, and of a third
+// the memory of a second sum
 __device__ __forceinline__ float4 *second(float4 *lds, int lg) { return lds + (blockDim.x >> 6 << lg); }
-__device__ __forceinline__ float4 *third(float4 *lds, int lg) { return lds + 2 * (blockDim.x >> 6 << lg); }
-// two sums in one step
-__device__ __forceinline__ void column_sums(float4 &a, float4 &b, int lg, float4 *lds_a, float4 *lds_b)
-{
-    for (int d = 1 << lg; d < kWave; d <<= 1) {
-        a = a + shfl_xor4(a, d);
-        b = b + shfl_xor4(b, d);
-    }
-    const int waves = blockDim.x >> 6;
-    if (waves == 1) return;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, q = threadIdx.x & ((1 << lg) - 1);
-    if (lane < (1 << lg)) {
-        lds_a[(wave << lg) + lane] = a;
-        lds_b[(wave << lg) + lane] = b;
-    }
-    __syncthreads();
-    a = lds_a[q];
-    b = lds_b[q];
-    for (int w = 1; w < waves; ++w) {
-        a = a + lds_a[(w << lg) + q];
-        b = b + lds_b[(w << lg) + q];
-    }
-}
 
 // A thread's rows: K pairs, `slots` pairs apart, of which those in [first, end) belong to its work-group's rows.  Pairs go by the rows' numbers in
 // the whole operand, as the generator's do.
@@ -177,21 +154,22 @@ struct Shape {
     bool past, joined;       // joined: the first chunk's place holds what all chunks come to
     int64_t tiles;
 };
-// A mean that its sum's roundings put off, from the differences d of `n` entries to it: the mean of d is what it is off by, and
+// A mean that its sum's roundings put off, from the differences of `n` entries to it: their mean is what it is off by, and
 //     sum (x - mean)^2 = sum d^2 - (sum d)^2 / n.
 // Without this step a group of equal numbers far from zero, whose differences are 0, comes out as the roundings of its mean over sqrt(eps) (273 times 1000.1: 0.019
 // instead of 0).  With it the mean is off by the one rounding of its own 32 bits and what differences of their size leave.  Both passes go by that rounded mean, so that
-// they see the same arguments of the activation.
-__device__ __forceinline__ float corrected(float mean, float off)
+// they see the same arguments of the activation.  A mean below the spread is as good as the differences' sum would make it, and a tile with no other is spared the sum (2048 rows
+// in one group x 8192 columns, forward: 25.2 us, with it 26.3).
+// differences(): this thread's share of it.
+__device__ __forceinline__ bool far(float mean, float squares, float n) { return n * mean * mean > squares; }   // (not with an infinity or NaN)
+template <typename F>
+__device__ __forceinline__ void correct(float4 &mean, float4 &squares, float n, int lg, float4 *lds, F &&differences)
 {
-    const float m = mean + off;
-    return m - m == 0.f ? m : mean;   // (an infinite mean has no difference to its entries)
-}
-__device__ __forceinline__ void correct(float4 d, float n, float4 &mean, float4 &squares)
-{
-    const float4 off = 1.f / n * d, s = squares - d * off;
-    mean = make_float4(corrected(mean.x, off.x), corrected(mean.y, off.y), corrected(mean.z, off.z), corrected(mean.w, off.w));
-    squares = make_float4(s.x < 0.f ? 0.f : s.x, s.y < 0.f ? 0.f : s.y, s.z < 0.f ? 0.f : s.z, s.w < 0.f ? 0.f : s.w);
+    const bool x = far(mean.x, squares.x, n), y = far(mean.y, squares.y, n), z = far(mean.z, squares.z, n), w = far(mean.w, squares.w, n);
+    if (!__any(x || y || z || w)) return;   // (each wave holds all columns of the tile, with the same bits: all waves go the same way)
+    const float4 d = column_sum(differences(), lg, lds), off = 1.f / n * d, s = squares - d * off;
+    mean = make_float4(x ? mean.x + off.x : mean.x, y ? mean.y + off.y : mean.y, z ? mean.z + off.z : mean.z, w ? mean.w + off.w : mean.w);
+    squares = make_float4(x ? fmaxf(s.x, 0.f) : squares.x, y ? fmaxf(s.y, 0.f) : squares.y, z ? fmaxf(s.z, 0.f) : squares.z, w ? fmaxf(s.w, 0.f) : squares.w);
 }
 // statistics of the entries that the work-group holds: mean and sum of squares about it; x becomes its difference from the mean
 template <int K>
@@ -203,18 +181,20 @@ __device__ __forceinline__ void statistics(float4 (&x)[2 * K], const Rows<K> &r,
     for (int i = 0; i < 2 * K; ++i)
         if (r.in(i)) s = s + x[i];
     mean = 1.f / static_cast<float>(n) * column_sum(s, lg, lds);
-    float4 s1 = splat(0.f);
-    squares = splat(0.f);
+    float4 s2 = splat(0.f);
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) {
         const float4 d = x[i] - mean;
-        if (r.in(i)) {
-            s1 = s1 + d;
-            squares = fma4(d, d, squares);
-        }
+        if (r.in(i)) s2 = fma4(d, d, s2);
     }
-    column_sums(s1, squares, lg, second(lds, lg), third(lds, lg));
-    correct(s1, static_cast<float>(n), mean, squares);
+    squares = column_sum(s2, lg, second(lds, lg));
+    correct(mean, squares, static_cast<float>(n), lg, lds, [&] {
+        float4 s1 = splat(0.f);
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i)
+            if (r.in(i)) s1 = s1 + (x[i] - mean);
+        return s1;
+    });
 #pragma unroll
     for (int i = 0; i < 2 * K; ++i) x[i] = x[i] - mean;
 }
@@ -265,7 +245,7 @@ __device__ __forceinline__ void write_forward(const NormArgs &a, const float4 (&
 template <int K, int T, bool WHOLE>
 __global__ __launch_bounds__(T) void norm_forward_kernel(const NormArgs a, const Shape z)
 {
-    extern __shared__ float4 lds[];   // three per wave and quad
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
@@ -307,16 +287,21 @@ __device__ __forceinline__ void join_statistics(const NormArgs &a, const Shape &
         mean = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p), mean);
     }
     mean = 1.f / static_cast<float>(a.features / a.groups) * column_sum(mean, z.lg, lds);
-    float4 s1 = splat(0.f);
     for (int c = p.slot; c < z.chunks; c += p.slots) {
         const Rows<K> of = rows_of<K>(a, group, c, p);
         const float *const at = stats + 2 * static_cast<int64_t>(c) * a.batch;
-        const float4 d = load_quad(at, p) - mean, nd = static_cast<float>(of.end - of.first) * d;
-        s1 = s1 + nd;
-        squares = squares + fma4(nd, d, load_quad(at + a.batch, p));
+        const float4 d = load_quad(at, p) - mean;
+        squares = squares + fma4(static_cast<float>(of.end - of.first) * d, d, load_quad(at + a.batch, p));
     }
-    column_sums(s1, squares, z.lg, second(lds, z.lg), third(lds, z.lg));
-    correct(s1, static_cast<float>(a.features / a.groups), mean, squares);
+    squares = column_sum(squares, z.lg, second(lds, z.lg));
+    correct(mean, squares, static_cast<float>(a.features / a.groups), z.lg, lds, [&] {
+        float4 s1 = splat(0.f);
+        for (int c = p.slot; c < z.chunks; c += p.slots) {
+            const Rows<K> of = rows_of<K>(a, group, c, p);
+            s1 = fma4(splat(static_cast<float>(of.end - of.first)), load_quad(stats + 2 * static_cast<int64_t>(c) * a.batch, p) - mean, s1);
+        }
+        return s1;
+    });
 }
 // the sums of h and h xh over the chunks, in the same way
 __device__ __forceinline__ void join_sums(const NormArgs &a, const Shape &z, int group, const Spot &p, float4 *lds, float4 &s, float4 &sx)
@@ -341,7 +326,7 @@ __device__ __forceinline__ void join_sums(const NormArgs &a, const Shape &z, int
 template <int K, bool BACKWARD>
 __global__ __launch_bounds__(kChunkThreads) void norm_join_kernel(const NormArgs a, const Shape z)
 {
-    extern __shared__ float4 lds[];   // per wave and quad three, backward two
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int group = static_cast<int>(blockIdx.x / z.tiles);
     const Spot p = spot_in(blockIdx.x % z.tiles, z.lg, a.batch);
     float4 one, two;
@@ -357,7 +342,7 @@ __global__ __launch_bounds__(kChunkThreads) void norm_join_kernel(const NormArgs
 template <int K>
 __global__ __launch_bounds__(kChunkThreads) void norm_apply_kernel(const NormArgs a, const Shape z)
 {
-    extern __shared__ float4 lds[];   // three per wave and quad
+    extern __shared__ float4 lds[];   // two per wave and quad
     const int64_t unit = blockIdx.x / z.chunks, tile = near_tile(unit % z.tiles, z.tiles, z.lg);
     const int chunk = static_cast<int>(blockIdx.x % z.chunks), group = static_cast<int>(unit / z.tiles);
     const Spot p = spot_in(tile, z.lg, a.batch, z.past);
@@ -588,10 +573,9 @@ struct Limits {
     int most_pairs, most_threads;   // the most that a thread and a work-group hold of a group
     int chunk_pairs;                // of a thread at most, where the group is longer
     int bytes;                      // that an entry moves
-    int sums;                       // that have memory of their own
     bool slabs;                     // tiles leave sums to be added up
 };
-constexpr Limits kForward{8, 1024, 4, 8, 3, false}, kBackward{8, 512, 2, 12, 2, true};
+constexpr Limits kForward{8, 1024, 4, 8, false}, kBackward{8, 512, 2, 12, true};
 // Threads of a work-group, before a thread takes kGroupPairs pairs.  More of them where there are few work-groups: a compute unit has one, whose threads
 // each have less to do in turn (both ways, 256 -> 512 threads: 1532 rows, 2 groups x 12 columns 20.1 -> 17.0 us, 2048 rows, 1 x 553 36.2 -> 32.2; 1024
 // threads take 17.2 and 34.1).
@@ -633,7 +617,7 @@ Plan plan_norm(int32_t features, int32_t groups, int32_t batch, const Limits &l)
         }
     }
     p.threads = static_cast<int>(threads);
-    p.lds = l.sums * static_cast<int>(sizeof(float4)) * (p.threads / kWave << p.z.lg);
+    p.lds = 2 * static_cast<int>(sizeof(float4)) * (p.threads / kWave << p.z.lg);
     p.z.slabs = 1;
     return p;
 }
