@@ -420,7 +420,8 @@ int group_norm_backward(const float *X, int32_t ldx, const float *gamma, const f
                         const float *rstd, int32_t lds, const float *dY, int32_t lddy, int32_t features, int32_t groups,
                         int32_t batch, int32_t act, float drop, int32_t layer, const int64_t *state, float *dX, int32_t lddx,
                         float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
-/* Dropout: Y[i,c] = 0 with probability drop, X[i,c] / (1 - drop) otherwise; drop in [0, 1), taken to the next multiple of 2^-16 (65535 of them at most).
+/* Dropout: Y[i,c] = 0 with probability drop, X[i,c] / (1 - drop) otherwise; drop in [0, 1), rounded to the nearest multiple of 2^-16 (65535 of them at most; a
+ * drop below 2^-17 drops nothing), and X is divided by 1 less that multiple.
  * Which entries are dropped follows from state = {seed, step} (two int64 on the DEVICE, so that a captured step
  * can go on drawing: the program raises step, of which the low 32 bits count, between steps), layer (a number that tells the calls of one step
  * apart), i and c, by Philox4x32-10 with key seed and counter (c / 4, i / 2, layer, step): word c % 4, its low 16 bits for even
