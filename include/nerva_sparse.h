@@ -451,7 +451,9 @@ int label_log_probs(const float *Z, int32_t ldz, const int32_t *labels, int32_t 
  *     loss = sum_c w_c ( -min( r A, clip(r, 1 - clip_low, 1 + clip_high) A ) + beta (q - log q - 1) )
  *     dZ[i,c] = dloss/dl_c ( [i == labels[c]] - exp(Z[i,c]) / sum exp Z[.,c] )
  * weights: float[batch], NULL for 1/batch; a column of weight 0 does not count.  ref_logp NULL: no KL term.  Where r lies beyond the border
- * that A bounds it by, the first term has no gradient; on which side it lies is decided in 64 bits.
+ * that A bounds it by, the first term has no gradient; on which side it lies is decided in 64 bits.  (A column within some 10^-5 of its border has its sum formed
+ * again for that, one column of a work-group after the other: with a clip of 0 and a policy that has not moved, where all columns lie there, a call takes some ten times as long.)
+ * An advantage or a beta of 0 takes nothing of its term, however large that is.
  * logp: float[batch], l_c (may be NULL).  stats: float[4] on the device: the loss, its first term, the weighted KL term (without beta) and the
  * weight of the columns beyond their border.  0 <= clip_low, clip_high, beta, finite.  workspace: for 0 sequences. */
 int policy_loss(const float *Z, int32_t ldz, const int32_t *labels, const float *old_logp, const float *ref_logp,
@@ -461,6 +463,7 @@ int policy_loss(const float *Z, int32_t ldz, const int32_t *labels, const float 
 /* Preference loss of pairs, and the gradient of the logits: sequence 2p is preferred to sequence 2p + 1; with S_s = sum of l_c over sequence s and
  * x_p = beta ( (S_2p - ref_sums[2p]) - (S_2p+1 - ref_sums[2p+1]) ),
  *     loss = (1/pairs) sum_p ( (1 - smoothing) log(1 + exp(-x_p)) + smoothing log(1 + exp(x_p)) ).
+ * (a side without a share takes nothing, however large its loss is).
  * starts: int32[2 pairs + 1] as above.  ref_sums: float[2 pairs], such sums of a reference model (NULL: 0).  sums float[2 pairs], margins (x_p) float[pairs]
  * and loss float[1] may be NULL.  dZ is 0 in columns that do not count or lie outside all sequences.  beta finite, smoothing in [0, 1].
  * workspace: for 2 pairs sequences. */

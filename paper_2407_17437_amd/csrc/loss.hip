@@ -28,7 +28,9 @@ constexpr int kLanes = 6;              // log2 of the quads of their tiles: 256 
 constexpr int kLoads = 8, kFewLoads = 2;   // rows in flight per thread
 constexpr int64_t kBlocks = 8192;      // work-groups that the classes are cut for
 constexpr int kColumns = 16, kParts = 16;   // columns of a work-group that adds up chunks, threads of a column
-constexpr int kHeldThreads = 1024, kHeldRows = 8;    // of a work-group that holds its columns
+// Of a work-group that holds its columns.  (Eight rows a thread take all 128 registers that 1024 threads leave, and two more of the policy loss, five of the preference loss lie
+// in scratch memory; with 16 rows 2048 classes x 8192 take 61.5 us instead of 48.5 in chunks.)
+constexpr int kHeldThreads = 1024, kHeldRows = 8;
 
 __device__ __forceinline__ float4 exp_of4(float4 x) { return make_float4(exp_of(x.x), exp_of(x.y), exp_of(x.z), exp_of(x.w)); }
 __device__ __forceinline__ float4 max4(float4 a, float4 b) { return make_float4(fmaxf(a.x, b.x), fmaxf(a.y, b.y), fmaxf(a.z, b.z), fmaxf(a.w, b.w)); }
@@ -441,7 +443,8 @@ __global__ __launch_bounds__(kColumns *kParts) void policy_columns_kernel(const 
     if (mine) t = policy_term(a, b, c, in);
     if (part == 0) close[j] = t.close;
     if (__syncthreads_or(t.close)) {
-        // as above, in 64 bits (some 4 columns in 10^5 with ratios around 1)
+        // as above, in 64 bits (some 4 columns in 10^5 with ratios around 1; all of them where clip is 0 and the policy has not moved: 3000 classes x 8192 then take 493 us
+        // instead of 57)
         for (int k = 0; k < kColumns; ++k) {
             if (!close[k]) continue;
             const double again = exact_sum(a, blockIdx.x * kColumns + k, tops[k], sums);
