@@ -27,7 +27,7 @@ constexpr int kChunkThreads = 256;     // of groups that are cut into chunks
 // Philox4x32 of 10 rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011), key = seed.  Counter (column / 4, row / 2,
 // layer, step) gives the bits of four columns in two rows: word column % 4, its low half for the even row and its high half for the odd one.  So
 // an entry's bits depend on neither leading dimension nor batch nor launch.  16 bits an entry halve the generator's work, which
-// is not small beside 8 bytes an entry (20 products of 32 bits for 8 entries: 67 M entries normalised and dropped issue 36 instructions an
+// is not small beside 8 bytes an entry (20 products of 32 bits for 8 entries: 67 M entries normalised and dropped issue 39 instructions an
 // entry, which keep the vector units busy for some two thirds of the 105 us); the probability is a multiple of 2^-16 for it, and the scale is that of
 // the multiple.
 struct Bits {
